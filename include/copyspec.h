@@ -413,6 +413,90 @@ int cs_kv_set_len_dev(cs_kv*, const int32_t* d_len /*device [B]*/, int64_t len_u
                       void* stream);
 
 /* ------------------------------------------------------------------------------------
+ * Paged cache  (Sec. 3.2, App. B.1-B.2: the block is appended to the per-layer keys and values and
+ * evaluated against them in one pass; here the cache of a stream need not be contiguous)
+ *
+ * For serving programs that hand out cache memory in pages: streams that grow unevenly, prompts
+ * that share a prefix (their tables name the same pages), a draft that is dropped again.  The
+ * pools, the table and the lengths are the caller's; the library keeps nothing between calls, so
+ * calls on different streams, with workspaces of their own, may overlap.
+ *
+ * Token t of stream b lives in slot t % page_size of page table[b][t / page_size].  len[b] is the
+ * stream's valid length L_b before its new rows; new row i sits at position L_b + i.  cs_paged_append
+ * writes the rows, cs_paged_attention lets them attend, and the caller then advances len by what it
+ * keeps (a rejected draft is a smaller advance: rows at and beyond len are dead).
+ *
+ * Table entries are only read for pages that hold tokens below L_b + rows.  An entry outside
+ * 0 .. n_pages-1 names no page: nothing is written there, and its tokens are not attended to (an
+ * evicted page).  A length is taken as 0 if it is negative, and positions at and beyond
+ * table_pages * page_size do not exist: their rows are not written, and their tokens not attended to.
+ *
+ * Rows of a call: R rows in all, those of stream b being d_row0[b] .. d_row0[b+1]-1 (device,
+ * [batch + 1], not decreasing, first entry 0).  Rows from d_row0[batch] on belong to nobody: they
+ * are not read, and their outputs are left as they were.  d_row0 NULL: R / batch rows each.
+ * A stream may have no rows.  R == 0 or batch == 0 is a no-op.
+ *
+ * Limits: page_size a power of two in 16..32768, head_dim a multiple of 8 up to 256, n_heads a multiple of
+ * n_kv_heads, table_pages * page_size <= 2^30.  Every pointer to rows or pools is aligned to 16 bytes, every
+ * stride (in elements, >= 0, at most 2^40) is a multiple of 16 bytes; the elements of one head's row are contiguous.
+ * token_stride * page_size elements of a pool must stay below 2^31 bytes.
+ * ---------------------------------------------------------------------------------- */
+typedef struct cs_pages {
+    void *k, *v;                            /* device pools of one layer, elements of `dtype` */
+    int64_t k_page, k_head, k_token;        /* strides of k, in elements */
+    int64_t v_page, v_head, v_token;        /* strides of v */
+    const int32_t* table;                   /* device [batch][table_stride], table_pages entries of a row in use */
+    int64_t table_stride;
+    const int32_t* len;                     /* device [batch] */
+    int32_t batch, table_pages, n_pages, page_size;
+    int32_t n_kv_heads, head_dim;
+    int32_t dtype;                          /* CS_F32 or CS_BF16 */
+    int32_t reserved;                       /* 0 */
+} cs_pages;
+
+/* RMSNorm of every query and key head, then the rotary embedding, in one pass over R rows of H query
+ * and KVH key heads:
+ *   y = x / sqrt(mean(x^2) + eps) * gain          (q_gain, k_gain: device float32 [head_dim]; NULL: y = x)
+ *   (y[j], y[j + rot/2]) turned by pos[r] * inv_freq[j] for j < rot/2; elements from rot on as they are
+ * inv_freq: device float64 [rot/2]; rot 0 (inv_freq and pos may be NULL): no rotation.  rot is a
+ * multiple of 8 up to head_dim.  The angle is formed in float64, norm and rotation in float32, and the result is
+ * rounded once.  in_dtype -> out_dtype: CS_F32 -> CS_F32, CS_BF16 -> CS_BF16, CS_F32 -> CS_BF16.
+ * KVH == 0: queries only.  The outputs may be the inputs (same pointers, strides and type); otherwise
+ * they must not overlap.  Strides in elements, limits as above.  Asynchronous on `stream`. */
+int cs_op_qk_norm_rope(int32_t in_dtype, int32_t out_dtype, const void* q, int64_t q_row, int64_t q_head,
+                       const void* k, int64_t k_row, int64_t k_head, int32_t R, int32_t H, int32_t KVH,
+                       int32_t head_dim, const float* q_gain, const float* k_gain, float eps,
+                       const int32_t* pos, const double* inv_freq, int32_t rot,
+                       void* q_out, int64_t q_out_row, int64_t q_out_head,
+                       void* k_out, int64_t k_out_row, int64_t k_out_head, void* stream);
+
+/* Writes R new key and value rows [R][n_kv_heads][head_dim] into the pages of their streams.  With rot > 0
+ * the keys are turned by their position on the way, as in cs_op_qk_norm_rope.  src_dtype CS_F32 (into
+ * either cache type) or CS_BF16 (into a CS_BF16 cache); rounded once.  Where two rows go to the same slot (a page
+ * named twice), either may stay.  Asynchronous on `stream`. */
+int cs_paged_append(const cs_pages* p, int32_t src_dtype, const void* k, int64_t k_row, int64_t k_head,
+                    const void* v, int64_t v_row, int64_t v_head, const int32_t* d_row0, int32_t R,
+                    const double* inv_freq, int32_t rot, void* stream);
+
+/* Attention of the new rows over the pages.  q [R][n_heads][head_dim] of the cache's type, rotated; query
+ * head h uses KV head h / (n_heads / n_kv_heads).  Row i of stream b sees the tokens t <= L_b + i
+ * whose page exists, with window > 0 only those with t > L_b + i - window; its own K/V must have been appended.
+ *   out[r][h] = sum_t softmax_t(scale * q[r][h] . k[t]) v[t]       (a row that sees nothing: 0)
+ * scale > 0 and finite.  Softmax statistics and sums are float32; in a CS_BF16 cache the
+ * probabilities are rounded to bfloat16 for the product with V.  out may be q.
+ * max_rows and max_len (host) say how many rows the longest stream brings and an upper bound of L_b + rows;
+ * 0 = not known.  They steer how the work is split, and so the workspace and the rounding, and nothing else:
+ * streams that exceed them get the same answer, later.  workspace: device, aligned to 16 bytes, at least
+ * cs_paged_attention_workspace(...) bytes for the same arguments (NULL where that is 0), used until the call's work on
+ * `stream` is done: calls that may overlap need one each.  Asynchronous on `stream`. */
+int64_t cs_paged_attention_workspace(const cs_pages* p, int32_t n_heads, int32_t has_row0, int32_t R, int32_t max_rows,
+                                     int64_t max_len);
+int cs_paged_attention(const cs_pages* p, const void* q, int64_t q_row, int64_t q_head, int32_t n_heads,
+                       const int32_t* d_row0, int32_t R, float scale, int32_t window, int32_t max_rows, int64_t max_len,
+                       void* out, int64_t out_row, int64_t out_head, void* workspace, int64_t workspace_bytes,
+                       void* stream);
+
+/* ------------------------------------------------------------------------------------
  * Instrumentation: per-kernel-class device timing with HIP events recorded on the stream
  * the kernels run on.  cs_profile_enable(mask) selects classes (0 = off, the default);
  * cs_profile_read synchronises the device and returns the summed duration and the number

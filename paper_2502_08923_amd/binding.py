@@ -7,7 +7,9 @@ binding's functions fails with an explicit error.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
+import math
 import os
 from typing import Optional, Sequence
 
@@ -31,7 +33,7 @@ EXPORTS = [
     "cs_decode_greedy", "cs_decode_merged", "cs_prefill", "cs_prefill_batch", "cs_decode_batch", "cs_index_create", "cs_index_destroy",
     "cs_index_reset", "cs_index_find_match_batch_dev", "cs_op_gemm", "cs_op_attention", "cs_op_argmax_accept",
     "cs_set_plain_kernels", "cs_set_prompt_block_rows", "cs_kv_set_len_dev", "cs_profile_enable", "cs_profile_reset",
-    "cs_profile_read",
+    "cs_profile_read", "cs_op_qk_norm_rope", "cs_paged_append", "cs_paged_attention", "cs_paged_attention_workspace",
 ]
 
 CS_PROF = {"scan": 1, "gemm": 2, "attn": 4, "attn_merge": 8, "argmax": 16, "lm_head": 32}
@@ -62,6 +64,13 @@ class cs_weights(C.Structure):
 
 class cs_stats(C.Structure):
     _fields_ = [(n, C.c_int64) for n in ("steps", "attempts", "drafted", "accepted")]
+
+
+class cs_pages(C.Structure):
+    _fields_ = ([("k", C.c_void_p), ("v", C.c_void_p)]
+                + [(n, C.c_int64) for n in ("k_page", "k_head", "k_token", "v_page", "v_head", "v_token")]
+                + [("table", C.c_void_p), ("table_stride", C.c_int64), ("len", C.c_void_p)]
+                + [(n, C.c_int32) for n in ("batch", "table_pages", "n_pages", "page_size", "n_kv_heads", "head_dim", "dtype", "reserved")])
 
 
 class cs_merged_stats(C.Structure):
@@ -127,6 +136,14 @@ def load_library(path: Optional[str] = None) -> C.CDLL:
     lib.cs_op_attention.argtypes = [vp, vp, i32, vp, i32, vp, vp]
     lib.cs_op_argmax_accept.argtypes = [vp, vp, i32, i32, i32, vp, vp, vp, vp, vp, vp]
     lib.cs_kv_set_len_dev.argtypes = [vp, vp, i64, vp]
+    f32 = C.c_float
+    lib.cs_op_qk_norm_rope.argtypes = [i32, i32, vp, i64, i64, vp, i64, i64, i32, i32, i32, i32, vp, vp, f32, vp, vp, i32,
+                                       vp, i64, i64, vp, i64, i64, vp]
+    lib.cs_paged_append.argtypes = [C.POINTER(cs_pages), i32, vp, i64, i64, vp, i64, i64, vp, i32, vp, i32, vp]
+    lib.cs_paged_attention_workspace.argtypes = [C.POINTER(cs_pages), i32, i32, i32, i32, i64]
+    lib.cs_paged_attention_workspace.restype = i64
+    lib.cs_paged_attention.argtypes = [C.POINTER(cs_pages), vp, i64, i64, i32, vp, i32, f32, i32, i32, i64, vp, i64, i64,
+                                       vp, i64, vp]
     lib.cs_profile_enable.argtypes = [i32]
     lib.cs_profile_enable.restype = None
     lib.cs_profile_reset.restype = None
@@ -612,6 +629,158 @@ def cs_op_argmax_accept(model: Model, logits: torch.Tensor, draft: torch.Tensor,
                                               draft_len.data_ptr(), acc.data_ptr(), nxt.data_ptr(),
                                               am.data_ptr(), _stream(stream)))
     return acc, nxt, am
+
+
+# ----------------------------------------------------------------------------------------
+# paged cache
+# ----------------------------------------------------------------------------------------
+
+_DTYPES = {torch.float32: CS_F32, torch.bfloat16: CS_BF16}
+
+
+def _place(tensors, stream):
+    """(context, raw stream, torch stream or None) for a call on these tensors: the device is theirs, whatever the current
+    one is, and the default stream is that device's current one."""
+    dev = None
+    for name, t in tensors:
+        if t is None:
+            continue
+        if not t.is_cuda:
+            raise TypeError(f"{name} must be a CUDA tensor")
+        if dev is None:
+            dev = t.device
+        elif t.device != dev:
+            raise ValueError(f"{name} is on {t.device}, the other tensors on {dev}")
+    if stream is not None and not hasattr(stream, "cuda_stream"):
+        stream = torch.cuda.ExternalStream(int(stream), device=dev)
+    if stream is not None and stream.device != dev:
+        raise ValueError(f"the stream belongs to {stream.device}, the tensors are on {dev}")
+    here = contextlib.nullcontext() if torch.cuda.current_device() == dev.index else torch.cuda.device(dev)
+    return here, stream
+
+
+def _rows3(t: torch.Tensor, name: str):
+    """Pointer and strides of a tensor of rows of heads (a stride that is never taken counts as 0)."""
+    if t.dim() != 3 or (t.shape[2] > 1 and t.stride(2) != 1):
+        raise TypeError(f"{name} must be [rows][heads][head_dim] with contiguous head rows")
+    if t.dtype not in _DTYPES:
+        raise TypeError(f"{name} must be float32 or bfloat16")
+    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else 0, t.stride(1) if t.shape[1] > 1 else 0
+
+
+def _vec(t: Optional[torch.Tensor], name: str, dtype, n: int):
+    if t is None:
+        return None
+    if t.dtype != dtype or t.dim() != 1 or t.shape[0] != n or (n > 1 and t.stride(0) != 1):
+        raise TypeError(f"{name} must be a contiguous {dtype} tensor of {n} elements")
+    return t.data_ptr()
+
+
+class Pages:
+    """cs_pages: the caller's pools, page table and lengths of one layer of a paged cache.  k and v: [n_pages][n_kv_heads]
+    [page_size][head_dim], bfloat16 or float32, any strides with contiguous head rows (a token-major pool is passed
+    transposed); table: int32 [batch][pages]; length: int32 [batch].  The tensors stay the caller's: tables and lengths
+    may be changed in place between calls."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, table: torch.Tensor, length: torch.Tensor):
+        _place((("k", k), ("v", v), ("table", table), ("length", length)), None)
+        if k.dim() != 4 or k.shape != v.shape or k.dtype != v.dtype or k.dtype not in _DTYPES:
+            raise TypeError("k and v must be [n_pages][n_kv_heads][page_size][head_dim] of one type, float32 or bfloat16")
+        if k.stride(3) != 1 or v.stride(3) != 1:
+            raise TypeError("the elements of a head's row must be contiguous")
+        if table.dtype != torch.int32 or table.dim() != 2 or (table.shape[1] > 1 and table.stride(1) != 1):
+            raise TypeError("table must be int32 [batch][pages] with contiguous rows")
+        _vec(length, "length", torch.int32, table.shape[0])
+        self.k, self.v, self.table, self.length = k, v, table, length
+        self.dtype = k.dtype
+        st = [[t.stride(d) if t.shape[d] > 1 else (0 if d < 2 else t.shape[3]) for d in range(3)] for t in (k, v)]
+        self.c = cs_pages(k.data_ptr(), v.data_ptr(), *st[0], *st[1], table.data_ptr(),
+                          table.stride(0) if table.shape[0] > 1 else table.shape[1], length.data_ptr(), table.shape[0],
+                          table.shape[1], k.shape[0], k.shape[2], k.shape[1], k.shape[3], _DTYPES[k.dtype], 0)
+
+    def _row0(self, row0: Optional[torch.Tensor]):
+        return _vec(row0, "row0", torch.int32, self.table.shape[0] + 1)
+
+
+def cs_op_qk_norm_rope(q: torch.Tensor, k: Optional[torch.Tensor] = None, pos: Optional[torch.Tensor] = None,
+                       inv_freq: Optional[torch.Tensor] = None, q_gain: Optional[torch.Tensor] = None,
+                       k_gain: Optional[torch.Tensor] = None, eps: float = 1e-6, out_dtype: Optional[torch.dtype] = None,
+                       out=None, stream=None):
+    """q [R][H][hd], k [R][KVH][hd] or None: RMSNorm of every head (a gain of None: no norm) and rotation by
+    pos[r] * inv_freq[j] (float64 [rot/2]; None: no rotation).  Returns (q, k) rows in new tensors, or in
+    out = (q_out, k_out), which may be the inputs."""
+    here, st = _place((("q", q), ("k", k), ("pos", pos), ("inv_freq", inv_freq), ("q_gain", q_gain), ("k_gain", k_gain))
+                      + (() if out is None else (("out[0]", out[0]), ("out[1]", out[1]))), stream)
+    qp = _rows3(q, "q")
+    R, H, hd = q.shape
+    kp, KVH = (None, 0, 0), 0
+    if k is not None:
+        kp, KVH = _rows3(k, "k"), k.shape[1]
+        if k.shape[0] != R or k.shape[2] != hd or k.dtype != q.dtype:
+            raise ValueError("q and k must have the same rows, head_dim and type")
+    rot = 0 if inv_freq is None else 2 * inv_freq.numel()
+    if rot and pos is None:
+        raise ValueError("a rotation needs positions")
+    with here, (torch.cuda.stream(st) if st is not None else contextlib.nullcontext()):
+        if out is None:
+            dt = out_dtype or q.dtype
+            out = (torch.empty((R, H, hd), dtype=dt, device=q.device),
+                   None if k is None else torch.empty((R, KVH, hd), dtype=dt, device=q.device))
+        qo, ko = out
+        if qo.shape != q.shape or (k is not None and (ko is None or ko.shape != k.shape or ko.dtype != qo.dtype)) \
+                or (out_dtype is not None and qo.dtype != out_dtype):
+            raise ValueError("out must be (q_out, k_out) in the shapes of q and k and of one type")
+        qop, kop = _rows3(qo, "out[0]"), (None, 0, 0) if k is None else _rows3(ko, "out[1]")
+        _check(load_library().cs_op_qk_norm_rope(
+            _DTYPES[q.dtype], _DTYPES[qo.dtype], *qp, *kp, R, H, KVH, hd, _vec(q_gain, "q_gain", torch.float32, hd),
+            _vec(k_gain, "k_gain", torch.float32, hd), eps, _vec(pos, "pos", torch.int32, R),
+            _vec(inv_freq, "inv_freq", torch.float64, rot // 2), rot, *qop, *kop, _stream(None)))
+    return out
+
+
+def cs_paged_append(pages: Pages, k: torch.Tensor, v: torch.Tensor, row0: Optional[torch.Tensor] = None,
+                    inv_freq: Optional[torch.Tensor] = None, stream=None):
+    """New rows k, v [R][KVH][hd] into the pages of their streams, at positions length[b] + i; keys are rotated on the way
+    if inv_freq (float64 [rot/2]) is given.  row0: int32 [batch + 1] offsets of the streams' rows, None: equal shares."""
+    here, st = _place((("pages", pages.k), ("k", k), ("v", v), ("row0", row0), ("inv_freq", inv_freq)), stream)
+    if k.shape != v.shape or k.dtype != v.dtype or k.dim() != 3 or tuple(k.shape[1:]) != (pages.c.n_kv_heads, pages.c.head_dim):
+        raise ValueError("k and v must be [rows][n_kv_heads][head_dim] of one type")
+    rot = 0 if inv_freq is None else 2 * inv_freq.numel()
+    with here, (torch.cuda.stream(st) if st is not None else contextlib.nullcontext()):
+        _check(load_library().cs_paged_append(C.byref(pages.c), _DTYPES.get(k.dtype, -1), *_rows3(k, "k"), *_rows3(v, "v"),
+                                              pages._row0(row0), k.shape[0], _vec(inv_freq, "inv_freq", torch.float64, rot // 2),
+                                              rot, _stream(None)))
+
+
+def cs_paged_attention(pages: Pages, q: torch.Tensor, row0: Optional[torch.Tensor] = None, scale: Optional[float] = None,
+                       window: int = 0, max_rows: int = 0, max_len: int = 0, out: Optional[torch.Tensor] = None,
+                       workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """q [R][H][hd] of the cache's type, rotated.  Returns [R][H][hd] (in `out` if given, which may be q; rows behind the last
+    stream are left as they were).  scale: 1/sqrt(head_dim) by default.  max_rows, max_len: hints, see copyspec.h.
+    workspace: uint8 tensor of at least the size that cs_paged_attention_workspace asks for; by default one is allocated
+    for the call."""
+    here, st = _place((("pages", pages.k), ("q", q), ("row0", row0), ("out", out), ("workspace", workspace)), stream)
+    if q.dtype != pages.dtype:
+        raise TypeError(f"q must have the cache's type, {pages.dtype}")
+    qp = _rows3(q, "q")
+    R, H, hd = q.shape
+    if hd != pages.c.head_dim:
+        raise ValueError("q must have the cache's head_dim")
+    lib, r0 = load_library(), pages._row0(row0)
+    with here, (torch.cuda.stream(st) if st is not None else contextlib.nullcontext()):
+        if out is None:
+            out = torch.empty((R, H, hd), dtype=q.dtype, device=q.device)
+        elif out.shape != q.shape or out.dtype != q.dtype:
+            raise ValueError("out must have the shape and type of q")
+        need = lib.cs_paged_attention_workspace(C.byref(pages.c), H, 1 if r0 else 0, R, max_rows, max_len)
+        if need < 0:
+            _check(need)
+        if workspace is None and need > 0:
+            workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+        _check(lib.cs_paged_attention(C.byref(pages.c), *qp, H, r0, R, 1.0 / math.sqrt(hd) if scale is None else scale, window,
+                                      max_rows, max_len, *_rows3(out, "out"), _ptr(workspace),
+                                      0 if workspace is None else workspace.numel() * workspace.element_size(), _stream(None)))
+    return out
 
 
 # ----------------------------------------------------------------------------------------

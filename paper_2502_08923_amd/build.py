@@ -10,7 +10,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libcopyspec.so")
-SOURCES = ["cs_api.hip", "cs_scan.hip", "cs_index.hip", "cs_elem.hip", "cs_gemm.hip", "cs_attn.hip"]
+SOURCES = ["cs_api.hip", "cs_scan.hip", "cs_index.hip", "cs_elem.hip", "cs_gemm.hip", "cs_attn.hip",
+           "cs_paged.hip", "cs_paged_attn.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fno-gpu-rdc",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
