@@ -250,22 +250,8 @@ __global__ __launch_bounds__(THREADS) void k_attn_plain_lanes(const QT* __restri
 // tuned bf16 kernel
 // -------------------------------------------------------------------------------------
 #define FA_NT 3            // 16-row query tiles per wave  (48 query rows)
-// max over the four lanes {c, c+16, c+32, c+48} that share a query row, with the row-swap
-// instructions of gfx950 (two register swaps and two max) instead of two round trips through
-// the LDS crossbar: swapping x with itself leaves (low half, low half) and (high half, high
-// half) in the two results, whose max is the reduction over lanes 32 apart; then 16 apart.
-__device__ __forceinline__ float fa_row4_max(float x) {
-    const unsigned u = __float_as_uint(x);
-    const auto r32 = __builtin_amdgcn_permlane32_swap(u, u, false, false);
-    const float m = fmaxf(__uint_as_float(r32[0]), __uint_as_float(r32[1]));
-    const unsigned v = __float_as_uint(m);
-    const auto r16 = __builtin_amdgcn_permlane16_swap(v, v, false, false);
-    return fmaxf(__uint_as_float(r16[0]), __uint_as_float(r16[1]));
-}
-
 #define FA_QROWS (16 * FA_NT)
 static_assert(FA_QROWS == CS_ATTN_GROUP, "the host counts query groups in these rows");
-#define FA_RESCALE_LOG2 8.0f
 #define FA_OPAD 4          // LDS row padding (floats) of the in-workgroup merge buffers
 
 // attention output element: float16 outputs feed the output projection and are saturated

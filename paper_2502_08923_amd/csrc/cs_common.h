@@ -333,3 +333,19 @@ __device__ __forceinline__ float cs_wave_max(float v) {
     for (int o = 32; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
     return v;
 }
+
+// ---- the running softmax of the attention kernels -------------------------------------------
+// max over the four lanes {c, c+16, c+32, c+48} that share a query row, with the row-swap
+// instructions of gfx950 (two register swaps and two max) instead of two round trips through
+// the LDS crossbar: swapping x with itself leaves (low half, low half) and (high half, high
+// half) in the two results, whose max is the reduction over lanes 32 apart; then 16 apart.
+__device__ __forceinline__ float fa_row4_max(float x) {
+    const unsigned u = __float_as_uint(x);
+    const auto r32 = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    const float m = fmaxf(__uint_as_float(r32[0]), __uint_as_float(r32[1]));
+    const unsigned v = __float_as_uint(m);
+    const auto r16 = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    return fmaxf(__uint_as_float(r16[0]), __uint_as_float(r16[1]));
+}
+// The reference maximum follows the true one only when it is left behind by more than 2^8 (see the kernels).
+#define FA_RESCALE_LOG2 8.0f

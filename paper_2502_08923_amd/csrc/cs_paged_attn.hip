@@ -80,6 +80,434 @@ __global__ __launch_bounds__(256) void k_paged_plain(cs_pages_dev D, pa_args A) 
         if (lane + 64 * u < hd) cs_st(out, lane + 64 * u, l > 0.f ? o[u] / l : 0.f);
 }
 
+// ---- which query rows a workgroup has ----------------------------------------------------
+// The G * rows query rows of a stream's KV head (row n: block row n / G, head n % G of the group) are cut into tiles of TR.
+// Streams with qr_lo < G * rows <= qr_hi take part in a launch.
+struct pa_tile {
+    int b, n0, QR;            // stream, first query row, query rows of the stream
+    int row0, rows, L;        // its first row, rows, length
+};
+struct pa_plan {
+    int TR, qr_lo, qr_hi;
+    int nsplit, nsplit_all;   // token ranges of this launch, and of the workspace
+    int chunk;                // tokens of a range; the last one takes what is left
+    int tiles_per;            // tiles of a stream where all have the same rows, else 0
+    float* po;                // [nsplit_all][R][H][hd] partial outputs
+    float2* pml;              // [nsplit_all][R][H] (maximum, sum); sum < 0 in range 0: the output is there already
+};
+#define PA_DONE (-1.0f)
+
+__device__ __forceinline__ bool pa_find_tile(const cs_pages_dev& D, int G, const pa_plan& P, int tile, pa_tile& o) {
+    int b = -1, k = 0;
+    if (P.tiles_per) {
+        b = tile / P.tiles_per;
+        k = tile - b * P.tiles_per;
+        if (b >= D.p.batch) return false;
+    } else {
+        const int lane = threadIdx.x & 63;
+        int base = 0;
+        for (int b0 = 0; b0 < D.p.batch; b0 += 64) {
+            int n = 0;
+            if (b0 + lane < D.p.batch) {
+                const int64_t qr = (int64_t)cs_stream_rows(D, b0 + lane).y * G;
+                n = qr > P.qr_lo && qr <= P.qr_hi ? (int)((qr + P.TR - 1) / P.TR) : 0;
+            }
+            int incl = n;
+#pragma unroll
+            for (int s = 1; s < 64; s <<= 1) {
+                const int v = __shfl_up(incl, s, 64);
+                incl += lane >= s ? v : 0;
+            }
+            const unsigned long long past = __ballot(base + incl > tile);
+            if (past) {
+                const int l = __ffsll(past) - 1;
+                b = b0 + l;
+                k = tile - base - (__shfl(incl, l, 64) - __shfl(n, l, 64));
+                break;
+            }
+            base += __shfl(incl, 63, 64);
+        }
+        if (b < 0) return false;
+    }
+    b = __builtin_amdgcn_readfirstlane(b);
+    const int2 sr = cs_stream_rows(D, b);
+    o.b = b;
+    o.row0 = __builtin_amdgcn_readfirstlane(sr.x);
+    o.rows = __builtin_amdgcn_readfirstlane(sr.y);
+    o.QR = o.rows * G;
+    o.n0 = __builtin_amdgcn_readfirstlane(k) * P.TR;
+    o.L = __builtin_amdgcn_readfirstlane(cs_stream_len(D, b));
+    return o.n0 < o.QR;
+}
+
+// The (max, sum, O) triples of W waves side by side in LDS -> the tile's rows: the output itself where the tokens are in one
+// range, else this range's partial result.
+template <int W, int HD, int ROWS>
+__device__ __forceinline__ void pa_finish(const cs_pages_dev& D, const pa_args& A, const pa_plan& P, const pa_tile& T, int kvh, int split,
+                                          int n_rows, const float* s_o, const float2* s_ml, int tid, int n_threads) {
+    constexpr int OROW = HD + 4;
+    const int hd = D.p.head_dim;
+#pragma unroll 1
+    for (int idx = tid; idx < n_rows * (HD / 4); idx += n_threads) {
+        const int n = idx / (HD / 4), d = idx % (HD / 4) * 4;
+        float2 ml[W];
+        float M = -INFINITY;
+#pragma unroll
+        for (int w = 0; w < W; ++w) {
+            ml[w] = s_ml[w * ROWS + n];
+            M = fmaxf(M, ml[w].x);
+        }
+        const float Ms = M == -INFINITY ? 0.f : M;
+        f32x4 o = (f32x4){0.f, 0.f, 0.f, 0.f};
+        float l = 0.f;
+#pragma unroll
+        for (int w = 0; w < W; ++w) {
+            const float f = __builtin_amdgcn_exp2f(ml[w].x - Ms);
+            o += f * *reinterpret_cast<const f32x4*>(&s_o[(w * ROWS + n) * OROW + d]);
+            l += f * ml[w].y;
+        }
+        const int i = (T.n0 + n) / A.G, h = kvh * A.G + T.n0 + n - i * A.G;
+        const int64_t r = T.row0 + i, rh = r * A.H + h;
+        if (P.nsplit == 1) {
+            const float inv = l > 0.f ? 1.0f / l : 0.f;           // a row that sees nothing: 0
+            if (d < hd) {
+                typedef __bf16 bf16x4_t __attribute__((ext_vector_type(4)));
+                *reinterpret_cast<bf16x4_t*>((bf16_t*)A.out + r * A.out_row + h * A.out_head + d) =
+                    (bf16x4_t){(bf16_t)(o[0] * inv), (bf16_t)(o[1] * inv), (bf16_t)(o[2] * inv), (bf16_t)(o[3] * inv)};
+            }
+            if (P.nsplit_all > 1 && d == 0) P.pml[rh] = make_float2(0.f, PA_DONE);
+            continue;
+        }
+        const int64_t at = (int64_t)split * D.R * A.H + rh;
+        if (d < hd) *reinterpret_cast<f32x4*>(P.po + at * hd + d) = o;
+        if (d == 0) {
+            P.pml[at] = make_float2(M, l);
+            if (split == 0)
+                for (int s = P.nsplit; s < P.nsplit_all; ++s) P.pml[(int64_t)s * D.R * A.H + rh] = make_float2(-INFINITY, 0.f);
+        }
+    }
+}
+
+// ---- few query rows: the stream of keys and values is the bound ---------------------------------
+// Four waves share a tile of up to 48 query rows and take the 32-token blocks of a token range in turn; keys, values,
+// scores and outputs stay in registers:
+//   S^T[token][row] = K . Q^T           A = 16 key rows (a lane: 8 features of one), B = query rows
+//   O^T[feature][row] += V^T . P^T      A = 16 features of 32 tokens, B = the probabilities as S^T left them
+// The k index of the second product may run over the block's tokens in any order that both operands share, so lane (c, g) takes
+// the tokens 4g..4g+3 of either 16-token half, which are the rows of S^T it holds already.  A lane loads 16 bytes of those eight
+// value rows (8 features of each) and turns the 8 x 8 square with 32 byte permutes into eight A fragments: fragment u has
+// feature 8c + u in row c.  So the values lie in the pages as they come, and a wave's load takes whole rows.
+// A page holds whole 16-token halves, so every load has one page and a uniform base: a buffer whose size ends with the last
+// token.  Loads past it, and of pages that do not exist, return zeros and cost no traffic, and none sits behind a branch.
+#define PN_WAVES 4
+template <int HD>
+struct pn_kbuf { bf16x8 k[2][HD / 32]; };
+template <int HD>
+struct pn_vbuf { unsigned v[8][HD / 32]; };     // [row j][dword]: row 4g + j % 4 of half j / 4
+
+template <int HD, int NT>
+__global__ __launch_bounds__(64 * PN_WAVES) void k_paged_narrow(cs_pages_dev D, pa_args A, pa_plan P) {
+    constexpr int KS = HD / 32, MT = HD / 16, VD = HD / 32;
+    constexpr int VW = HD == 64 ? 2 : 4;                // dwords of one value load
+    constexpr int VL = VD / VW;                         // loads per value row
+    constexpr int VF = 2 * VW;                          // features of one value load
+    constexpr int ROWS = 16 * NT, OROW = HD + 4, QROW = HD * 2 + 16;
+    constexpr int MERGE_BYTES = PN_WAVES * ROWS * (OROW * 4 + 8), Q_BYTES = ROWS * QROW;
+    __shared__ __attribute__((aligned(16))) unsigned char smem[MERGE_BYTES > Q_BYTES ? MERGE_BYTES : Q_BYTES];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int c = lane & 15, g = lane >> 4;
+    const int split = blockIdx.x % P.nsplit, item = blockIdx.x / P.nsplit;
+    const int KVH = D.p.n_kv_heads, kvh = item % KVH;
+    pa_tile T;
+    if (!pa_find_tile(D, A.G, P, item / KVH, T)) return;
+    const int hd = D.p.head_dim;
+    const int n_rows = min(ROWS, T.QR - T.n0);          // live query rows of the tile
+    const int i_lo = T.n0 / A.G, i_hi = (T.n0 + n_rows - 1) / A.G;
+    const int n_tok = min(T.L + i_hi + 1, D.cap);       // tokens that the tile's last row sees
+    const int base = A.window ? max(0, T.L + i_lo - A.window + 1) & ~31 : 0;
+    const int w_begin = (int)min((int64_t)base + (int64_t)split * P.chunk, (int64_t)n_tok);
+    const int t_end = split == P.nsplit - 1 ? n_tok : (int)min((int64_t)w_begin + P.chunk, (int64_t)n_tok);
+    // blocks between these need no mask
+    const int open_lo = A.window ? T.L + i_hi - A.window + 1 : 0, open_hi = min(T.L + i_lo + 1, D.cap);
+
+    // query rows into LDS
+    for (int idx = tid; idx < ROWS * (HD / 8); idx += 64 * PN_WAVES) {
+        const int n = idx / (HD / 8), seg = idx % (HD / 8);
+        bf16x8 v = (bf16x8){0, 0, 0, 0, 0, 0, 0, 0};
+        if (n < n_rows && seg * 8 < hd) {
+            const int i = (T.n0 + n) / A.G, h = kvh * A.G + T.n0 + n - i * A.G;
+            v = *reinterpret_cast<const bf16x8*>((const bf16_t*)A.q + (T.row0 + i) * A.q_row + h * A.q_head + seg * 8);
+        }
+        *reinterpret_cast<bf16x8*>(smem + n * QROW + seg * 16) = v;
+    }
+    int q_last[NT], q_first[NT];                        // tokens that the lane's query rows see
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+        const int n = nt * 16 + c, i = (T.n0 + n) / A.G;
+        q_last[nt] = n < n_rows ? T.L + i : -1;
+        q_first[nt] = A.window ? T.L + i - A.window + 1 : 0;
+    }
+
+    const bf16_t* Kh = (const bf16_t*)D.p.k + kvh * D.p.k_head;
+    const bf16_t* Vh = (const bf16_t*)D.p.v + kvh * D.p.v_head;
+    const int32_t* tab = D.p.table + T.b * D.p.table_stride;
+    constexpr unsigned NOWHERE = 0x80000000u;
+    const unsigned kts = (unsigned)D.p.k_token * 2, vts = (unsigned)D.p.v_token * 2;      // bytes per token
+    unsigned koff[KS], voff[4][VL];
+#pragma unroll
+    for (int s = 0; s < KS; ++s) koff[s] = s * 32 + g * 8 < hd ? c * kts + s * 64 + g * 16 : NOWHERE;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int x = 0; x < VL; ++x) voff[j][x] = x * 16 * VF + c * VF < hd ? (4 * g + j) * vts + (x * 16 + c) * VF * 2 : NOWHERE;
+
+    f32x4 oacc[MT][NT], lacc[NT];
+    float m_run[NT];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+        m_run[nt] = -INFINITY;
+        lacc[nt] = (f32x4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) oacc[mt][nt] = (f32x4){0.f, 0.f, 0.f, 0.f};
+    }
+    const bf16_t one = (bf16_t)1.0f;
+    const bf16x8 ones = (bf16x8){one, one, one, one, one, one, one, one};
+    const float scale2 = A.scale2;
+    __syncthreads();
+
+    constexpr int STEP = 32 * PN_WAVES;
+    // a lane holds the pages of one of the wave's next 64 blocks
+    for (int seg0 = w_begin; seg0 < t_end; seg0 += 64 * STEP) {
+        const int t_begin = seg0 + 32 * wave;
+        const int n_all = t_begin < t_end ? min(64, (t_end - t_begin + STEP - 1) / STEP) : 0;
+        int page0 = -1, page1 = -1;
+        {
+            const int64_t tb = (int64_t)t_begin + (int64_t)lane * STEP;
+            if (tb < t_end) {
+                page0 = tab[tb >> D.page_log2];
+                const int e1 = (int)((tb + 16) >> D.page_log2);
+                page1 = e1 < D.p.table_pages ? tab[e1] : -1;
+            }
+            page0 = (unsigned)page0 < (unsigned)D.p.n_pages ? page0 : -1;
+            page1 = (unsigned)page1 < (unsigned)D.p.n_pages ? page1 : -1;
+        }
+        auto at = [&](int i) { return t_begin + i * STEP; };
+        auto page_of = [&](int i, int a) { return __builtin_amdgcn_readlane(a ? page1 : page0, i); };
+        auto buffer = [&](const bf16_t* head, int64_t page_stride, unsigned ts, int i, int a) {
+            const int t = at(i) + 16 * a, page = i < n_all ? page_of(i, a) : -1;
+            const int live = min(16, n_tok - t);
+            const unsigned bytes = page >= 0 && live > 0 ? (live - 1) * ts + hd * 2 : 0;
+            const char* p = (const char*)(head + (page >= 0 ? page : 0) * page_stride) + (int64_t)(t & (D.p.page_size - 1)) * ts;
+            return __builtin_amdgcn_make_buffer_rsrc((void*)p, 0, (int)bytes, CS_BUFFER_WORD3);
+        };
+        auto ldk = [&](pn_kbuf<HD>& buf, int i) {
+#pragma unroll
+            for (int a = 0; a < 2; ++a) {
+                const auto rs = buffer(Kh, D.p.k_page, kts, i, a);
+#pragma unroll
+                for (int s = 0; s < KS; ++s) buf.k[a][s] = __builtin_bit_cast(bf16x8, __builtin_amdgcn_raw_buffer_load_b128(rs, koff[s], 0, 0));
+            }
+        };
+        auto ldv = [&](pn_vbuf<HD>& buf, int i) {
+#pragma unroll
+            for (int a = 0; a < 2; ++a) {
+                const auto rs = buffer(Vh, D.p.v_page, vts, i, a);
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+#pragma unroll
+                    for (int x = 0; x < VL; ++x) {
+                        if constexpr (VW == 4) {
+                            const auto t = __builtin_amdgcn_raw_buffer_load_b128(rs, voff[j][x], 0, 0);
+#pragma unroll
+                            for (int d = 0; d < 4; ++d) buf.v[4 * a + j][x * 4 + d] = t[d];
+                        } else {
+                            const auto t = __builtin_amdgcn_raw_buffer_load_b64(rs, voff[j][x], 0, 0);
+#pragma unroll
+                            for (int d = 0; d < 2; ++d) buf.v[4 * a + j][x * 2 + d] = t[d];
+                        }
+                    }
+            }
+        };
+        auto block = [&](pn_kbuf<HD>& kb, pn_vbuf<HD>& vb, int i) {
+            f32x4 sacc[2][NT];
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                f32x4 z0 = (f32x4){0.f, 0.f, 0.f, 0.f}, z1 = z0;
+#pragma unroll
+                for (int s = 0; s < KS; ++s) {
+                    const bf16x8 qb = *reinterpret_cast<const bf16x8*>(smem + (nt * 16 + c) * QROW + s * 64 + g * 16);
+                    z0 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kb.k[0][s], qb, z0, 0, 0, 0);
+                    z1 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kb.k[1][s], qb, z1, 0, 0, 0);
+                }
+                sacc[0][nt] = z0;
+                sacc[1][nt] = z1;
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            ldk(kb, i + 2);
+            __builtin_amdgcn_sched_barrier(0);
+            const int t0 = at(i), p0 = page_of(i, 0), p1 = page_of(i, 1);
+            if (t0 < open_lo || t0 + 32 > open_hi || p0 < 0 || p1 < 0) {
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int a = 0; a < 2; ++a)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            const int t = t0 + 16 * a + 4 * g + j;
+                            const bool sees = t <= q_last[nt] && t >= q_first[nt] && t < D.cap && (a ? p1 : p0) >= 0;
+                            sacc[a][nt][j] = sees ? sacc[a][nt][j] : -INFINITY;
+                        }
+            }
+            bool moved = false;
+            float alpha[NT];
+            bf16x8 pb[NT];
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                float sv[8];
+#pragma unroll
+                for (int a = 0; a < 2; ++a)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) sv[4 * a + j] = sacc[a][nt][j];
+                float mx = fmaxf(fmaxf(sv[0], sv[1]), sv[2]);
+                mx = fmaxf(fmaxf(mx, sv[3]), sv[4]);
+                mx = fmaxf(fmaxf(mx, sv[5]), fmaxf(sv[6], sv[7]));
+                mx = fa_row4_max(mx) * scale2;
+                // the reference maximum follows the true one only when it is left behind by 2^8: probabilities stay
+                // below 256, O and the row sum stay consistent, and O is rescaled a handful of times per wave
+                const bool up = mx > m_run[nt] + FA_RESCALE_LOG2;
+                const float m_new = up ? mx : m_run[nt];
+                const float m_safe = m_new == -INFINITY ? 0.f : m_new;
+                alpha[nt] = up ? __builtin_amdgcn_exp2f(m_run[nt] - m_safe) : 1.0f;
+                moved |= up;
+                m_run[nt] = m_new;
+                // rounded to bfloat16, the type of V in the product; the row sum is that of the rounded values
+#pragma unroll
+                for (int j = 0; j < 8; ++j) pb[nt][j] = (bf16_t)__builtin_amdgcn_exp2f(fmaf(sv[j], scale2, -m_safe));
+            }
+            if (__any(moved)) {
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+                    asm volatile("" : "+a"(lacc[nt]));
+                    lacc[nt] *= alpha[nt];
+#pragma unroll
+                    for (int mt = 0; mt < MT; ++mt) {
+                        asm volatile("" : "+a"(oacc[mt][nt]));
+                        oacc[mt][nt] *= alpha[nt];
+                    }
+                }
+            }
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) lacc[nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pb[nt], lacc[nt], 0, 0, 0);
+#pragma unroll
+            for (int d = 0; d < VD; ++d) {
+                // dword d of the eight rows: features 2d and 2d + 1 of the lane's
+                unsigned lo[4], hi[4];
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    lo[r] = __builtin_amdgcn_perm(vb.v[2 * r + 1][d], vb.v[2 * r][d], 0x05040100u);
+                    hi[r] = __builtin_amdgcn_perm(vb.v[2 * r + 1][d], vb.v[2 * r][d], 0x07060302u);
+                }
+                typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+                const bf16x8 fl = __builtin_bit_cast(bf16x8, (u32x4){lo[0], lo[1], lo[2], lo[3]});
+                const bf16x8 fh = __builtin_bit_cast(bf16x8, (u32x4){hi[0], hi[1], hi[2], hi[3]});
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+                    oacc[2 * d][nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fl, pb[nt], oacc[2 * d][nt], 0, 0, 0);
+                    oacc[2 * d + 1][nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fh, pb[nt], oacc[2 * d + 1][nt], 0, 0, 0);
+                }
+            }
+            // accumulators stay in the accumulation registers, the vector registers are for the stages
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                asm volatile("" : "+a"(lacc[nt]));
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt) asm volatile("" : "+a"(oacc[mt][nt]));
+            }
+        };
+        pn_kbuf<HD> k0, k1;
+        pn_vbuf<HD> v0, v1;
+        __builtin_amdgcn_sched_barrier(0);
+        ldk(k0, 0);
+        __builtin_amdgcn_sched_barrier(0);
+        ldv(v0, 0);
+        __builtin_amdgcn_sched_barrier(0);
+        ldk(k1, 1);
+        __builtin_amdgcn_sched_barrier(0);
+        int i = 0;
+        for (; i + 1 < n_all; i += 2) {             // (no way out in the middle: it would spoil the load counts)
+            ldv(v1, i + 1);
+            __builtin_amdgcn_sched_barrier(0);
+            block(k0, v0, i);
+            ldv(v0, i + 2);
+            __builtin_amdgcn_sched_barrier(0);
+            block(k1, v1, i + 1);
+        }
+        if (i < n_all) block(k0, v0, i);
+    }
+    __syncthreads();             // every wave is done with the query tile: LDS changes hands
+
+    // the waves' (max, sum, O) side by side in LDS, combined by all threads.  oacc[x*2*VW + u][nt][j]: query row nt*16 + c, feature
+    // (x*16 + 4g + j) * VF + u
+    float* s_o = reinterpret_cast<float*>(smem);                               // [waves][ROWS][OROW]
+    float2* s_ml = reinterpret_cast<float2*>(s_o + PN_WAVES * ROWS * OROW);    // [waves][ROWS]
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+        const int n = wave * ROWS + nt * 16 + c;
+        if (g == 0) s_ml[n] = make_float2(m_run[nt], lacc[nt][0]);
+#pragma unroll
+        for (int x = 0; x < VL; ++x)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int u = 0; u < VF; u += 4) {
+                    const int mt = x * VF + u;
+                    *reinterpret_cast<f32x4*>(&s_o[n * OROW + (x * 16 + 4 * g + j) * VF + u]) =
+                        (f32x4){oacc[mt][nt][j], oacc[mt + 1][nt][j], oacc[mt + 2][nt][j], oacc[mt + 3][nt][j]};
+                }
+    }
+    __syncthreads();
+    pa_finish<PN_WAVES, HD, ROWS>(D, A, P, T, kvh, split, n_rows, s_o, s_ml, tid, 64 * PN_WAVES);
+}
+
+// ---- joining token ranges ---------------------------------------------------------------------
+// out[r][h] = sum_s 2^(m_s - M) O_s / sum_s 2^(m_s - M) l_s.  2^lanes_log2 lanes have a row's hd features, four each; a lane reads
+// the (max, sum) pairs of every lanes-th range, and the weights go round by shuffles.
+template <typename T>
+__global__ __launch_bounds__(256) void k_paged_merge(const float* __restrict__ po, const float2* __restrict__ pml, int nsplit, int64_t n_rh, int H,
+                                                     int hd, int lanes_log2, const int32_t* __restrict__ row0_end, T* __restrict__ out,
+                                                     int64_t out_row, int64_t out_head) {
+    const int lanes = 1 << lanes_log2, sub = threadIdx.x & (lanes - 1), d = sub * 4;
+    const int64_t rh = (int64_t)blockIdx.x * (256 >> lanes_log2) + (threadIdx.x >> lanes_log2);
+    if (rh >= n_rh) return;
+    const int r = (int)(rh / H), h = (int)(rh % H);
+    if (row0_end && r >= *row0_end) return;                       // behind the last stream
+    if (pml[rh].y < 0.f) return;                                  // written by the kernel itself
+    float M = -INFINITY;
+    for (int s = sub; s < nsplit; s += lanes) M = fmaxf(M, pml[s * n_rh + rh].x);
+    for (int o = lanes >> 1; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor(M, o, 64));
+    const float Ms = M == -INFINITY ? 0.f : M;
+    f32x4 acc = (f32x4){0.f, 0.f, 0.f, 0.f};
+    float l = 0.f;
+    for (int s0 = 0; s0 < nsplit; s0 += lanes) {
+        float2 ml = make_float2(-INFINITY, 0.f);
+        if (s0 + sub < nsplit) ml = pml[(s0 + sub) * n_rh + rh];
+        const float w = __builtin_amdgcn_exp2f(ml.x - Ms);
+        const float wl = w * ml.y;
+        const int n = min(lanes, nsplit - s0);
+        for (int s = 0; s < n; ++s) {
+            const int src = (threadIdx.x & 63 & ~(lanes - 1)) + s;
+            const float ws = __shfl(w, src, 64);
+            l += __shfl(wl, src, 64);
+            if (ws != 0.f && d < hd) acc += ws * *reinterpret_cast<const f32x4*>(po + ((s0 + s) * n_rh + rh) * hd + d);
+        }
+    }
+    if (d >= hd) return;
+    const float inv = l > 0.f ? 1.0f / l : 0.f;
+    T* o = out + r * out_row + h * out_head + d;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) cs_st(o, j, acc[j] * inv);
+}
+
 // ---- entry points --------------------------------------------------------------------------
 static int check_shape(const char* who, const cs_pages* p, int32_t n_heads, int32_t R, int32_t max_rows, int64_t max_len) {
     CS_TRY(cs_check_pages(who, p));
@@ -91,13 +519,48 @@ static int check_shape(const char* who, const cs_pages* p, int32_t n_heads, int3
     return CS_OK;
 }
 
+// How a call is cut: the same for the workspace and the launch.
+struct pa_cut {
+    int hdt, nt, tiles, tiles_per, nsplit, chunk;
+    int64_t part_floats, bytes;
+};
+static pa_cut pa_make_cut(const cs_pages* p, int H, bool has_row0, int R, int max_rows, int64_t max_len, int window) {
+    pa_cut c;
+    const int KVH = p->n_kv_heads, G = H / KVH, B = p->batch, cap = p->table_pages * p->page_size;
+    const int rows = has_row0 ? (max_rows ? std::min(max_rows, R) : R) : R / B;
+    const int64_t qr = (int64_t)rows * G;
+    c.hdt = p->head_dim <= 64 ? 64 : p->head_dim <= 128 ? 128 : 256;
+    c.nt = (int)std::min<int64_t>(c.hdt == 256 ? 1 : 3, cs_ceil_div(qr, 16));
+    const int TR = 16 * c.nt;
+    c.tiles_per = has_row0 ? 0 : (int)cs_ceil_div(qr, TR);
+    const int64_t tiles = has_row0 ? (int64_t)R * G / TR + std::min(B, R) : (int64_t)B * c.tiles_per;
+    c.tiles = (int)tiles;
+    const int64_t len = max_len && max_len < cap ? max_len : cap;
+    const int64_t span = window ? std::min<int64_t>(len, (int64_t)window + rows + 32) : len;
+    const int64_t items = tiles * KVH, want = 1024, min_chunk = 256;
+    auto ranges = [&](int64_t tokens) { return std::max<int64_t>(1, std::min<int64_t>(cs_ceil_div(want, items), tokens / min_chunk)); };
+    c.chunk = (int)cs_round_up(cs_ceil_div(span, ranges(span)), 128);
+    c.nsplit = (int)cs_ceil_div(span, c.chunk);
+    const int64_t rh = (int64_t)R * H, room = ranges(len);      // (a window only takes ranges away)
+    c.part_floats = room > 1 ? cs_round_up(room * rh * p->head_dim, 4) : 0;
+    c.bytes = room > 1 ? c.part_floats * 4 + room * rh * 8 : 0;
+    return c;
+}
+
 extern "C" int64_t cs_paged_attention_workspace(const cs_pages* p, int32_t n_heads, int32_t has_row0, int32_t R, int32_t max_rows,
                                                 int64_t max_len) {
     const char* who = "cs_paged_attention_workspace";
     CS_TRY(check_shape(who, p, n_heads, R, max_rows, max_len));
     CS_REQUIRE(has_row0 || p->batch == 0 || R % p->batch == 0, CS_E_ARG, "%s: R rows cannot be shared out among %d streams without d_row0",
                who, p->batch);
-    return 0;
+    if (R == 0 || p->batch == 0 || p->dtype != CS_BF16) return 0;
+    return pa_make_cut(p, n_heads, has_row0 != 0, R, max_rows, max_len, 0).bytes;
+}
+
+template <int HD, int NT>
+static int pn_launch(const cs_pages_dev& D, const pa_args& A, const pa_plan& P, unsigned grid, hipStream_t s) {
+    k_paged_narrow<HD, NT><<<grid, 64 * PN_WAVES, 0, s>>>(D, A, P);
+    return cs_launch_ok("k_paged_narrow");
 }
 
 extern "C" int cs_paged_attention(const cs_pages* p, const void* q, int64_t q_row, int64_t q_head, int32_t n_heads,
@@ -116,8 +579,29 @@ extern "C" int cs_paged_attention(const cs_pages* p, const void* q, int64_t q_ro
     CS_TRY(cs_check_rows(who, "out", out, out_row, out_head, esz));
     pa_args A = {q, q_row, q_head, out, out_row, out_head, n_heads, n_heads / p->n_kv_heads, window, scale * 1.4426950408889634f};
     hipStream_t s = (hipStream_t)stream;
-    const unsigned grid = (unsigned)cs_ceil_div((int64_t)R * n_heads, 4);
-    if (p->dtype == CS_BF16) k_paged_plain<bf16_t><<<grid, 256, 0, s>>>(D, A);
-    else k_paged_plain<float><<<grid, 256, 0, s>>>(D, A);
-    return cs_launch_ok("k_paged_plain");
+    if (p->dtype == CS_F32) {
+        k_paged_plain<float><<<(unsigned)cs_ceil_div((int64_t)R * n_heads, 4), 256, 0, s>>>(D, A);
+        return cs_launch_ok("k_paged_plain");
+    }
+    pa_cut c = pa_make_cut(p, n_heads, d_row0 != nullptr, R, max_rows, max_len, window);
+    CS_REQUIRE(c.bytes <= 0 || (workspace && workspace_bytes >= c.bytes), CS_E_CAPACITY, "%s: the workspace has %lld bytes, %lld are needed",
+               who, (long long)(workspace ? workspace_bytes : 0), (long long)c.bytes);
+    CS_REQUIRE(((uintptr_t)workspace & 15) == 0, CS_E_ARG, "%s: the workspace is not aligned to 16 bytes", who);
+    pa_plan P = {16 * c.nt, 0, 0x7fffffff, c.nsplit, c.nsplit, c.chunk, c.tiles_per, (float*)workspace, (float2*)((float*)workspace + c.part_floats)};
+    const int64_t grid = (int64_t)c.tiles * p->n_kv_heads * c.nsplit;
+    CS_REQUIRE(grid <= 0x7fffffff, CS_E_UNSUPPORTED, "%s: too many tiles", who);
+    int rc = CS_E_STATE;
+#define PN(HD_, NT_) if (c.hdt == HD_ && c.nt == NT_) rc = pn_launch<HD_, NT_>(D, A, P, (unsigned)grid, s)
+    PN(64, 1); PN(64, 2); PN(64, 3); PN(128, 1); PN(128, 2); PN(128, 3); PN(256, 1);
+#undef PN
+    CS_TRY(rc);
+    if (c.nsplit > 1) {
+        int lanes = 0;
+        while (4 << lanes < p->head_dim) ++lanes;
+        const int64_t rh = (int64_t)R * n_heads;
+        k_paged_merge<bf16_t><<<(unsigned)cs_ceil_div(rh, 256 >> lanes), 256, 0, s>>>(P.po, P.pml, c.nsplit, rh, n_heads, p->head_dim, lanes,
+                                                                             d_row0 ? d_row0 + p->batch : nullptr, (bf16_t*)out, out_row, out_head);
+        return cs_launch_ok("k_paged_merge");
+    }
+    return CS_OK;
 }

@@ -93,6 +93,14 @@ def test_attention_refuses(lib, bad):
     assert attention(lib, **bad) in (-2, -6)
 
 
+def test_attention_refuses_a_small_workspace(lib):
+    p = pages(table_pages=1 << 16, table_stride=1 << 16)
+    need = lib.cs_paged_attention_workspace(C.byref(p), 32, 1, 4, 1, 1 << 20)
+    assert need > 0                                        # two streams of a million tokens are split
+    for ws, size in ((A, need - 1), (None, need), (A + 4, need), (A, 0)):
+        assert attention(lib, p, max_rows=1, max_len=1 << 20, ws=ws, ws_bytes=size) in (-2, -3)
+
+
 def test_nothing_to_do_is_no_error(lib):
     assert append(lib, R=0) == 0 and attention(lib, R=0) == 0 and norm_rope(lib, R=0) == 0
     assert append(lib, pages(batch=0)) == 0 and attention(lib, pages(batch=0)) == 0
