@@ -6,6 +6,7 @@
 // One pass over the tokens with the running maximum and sum of the softmax in float32.
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "cs_paged.h"
 
@@ -469,6 +470,314 @@ __global__ __launch_bounds__(64 * PN_WAVES) void k_paged_narrow(cs_pages_dev D, 
     pa_finish<PN_WAVES, HD, ROWS>(D, A, P, T, kvh, split, n_rows, s_o, s_ml, tid, 64 * PN_WAVES);
 }
 
+// ---- many query rows: the matrix cores and the vector unit are the bound -----------------------------
+// Eight waves have 16 * NT query rows each and walk the tokens together: every 32-token block goes once from its pages to LDS and
+// serves all of them.  Each wave requests its share of a block (1 KB pieces, direct to LDS) into a ring of stages, so several
+// blocks are in flight while one is multiplied; the requests and the waits on them are counted exactly, by hand, and the
+// kernel has no other vector memory load in its loop but the page numbers of the next 64 blocks.
+//   keys: one piece = 16 tokens x 32 features in fragment order, a lane's 16 bytes are what it multiplies
+//   values: one piece = 16 tokens x 32 features as two 16 x 16 squares of 32-byte rows, which the transposing LDS read
+//   (four tokens of one feature per lane) takes apart without bank conflicts
+// The products, the softmax and the order of tokens in the probabilities are those of the kernel above.
+#define PW_WAVES 8
+template <int HD, int NT>
+__global__ __launch_bounds__(64 * PW_WAVES) void k_paged_wide(cs_pages_dev D, pa_args A, pa_plan P) {
+    constexpr int KS = HD / 32, MT = HD / 16;
+    constexpr int WROWS = 16 * NT, TR = PW_WAVES * WROWS;
+    constexpr int NLOAD = 4 * KS, LD = NLOAD / PW_WAVES;       // pieces of a block; per wave
+    constexpr int STAGE_BYTES = NLOAD * 1024, V_AT = 2 * KS * 1024;
+    constexpr int STAGES = HD == 256 ? 4 : 6;
+    static_assert(NLOAD % PW_WAVES == 0 && STAGES * STAGE_BYTES <= 160 * 1024, "every wave the same number of requests; LDS");
+    __shared__ __attribute__((aligned(16))) unsigned char stage[STAGES][STAGE_BYTES];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int c = lane & 15, g = lane >> 4;
+    const int KVH = D.p.n_kv_heads;
+    // KV heads in turn, so that with eight of them each stays on one die and its cache; a stream's last rows, which see most, first
+    const int kvh = blockIdx.x % KVH, rest = blockIdx.x / KVH;
+    const int split = rest % P.nsplit, tile = (int)(gridDim.x / (KVH * P.nsplit)) - 1 - rest / P.nsplit;
+    pa_tile T;
+    if (!pa_find_tile(D, A.G, P, tile, T)) return;
+    const int hd = D.p.head_dim, G = A.G;
+    const int n_rows = min(TR, T.QR - T.n0);
+    const int i_lo = T.n0 / G, i_hi = (T.n0 + n_rows - 1) / G;
+    const int n_lim = min(T.L + i_hi + 1, D.cap);              // tokens that the tile's last row sees
+    const int n_tok = min(T.L + T.rows, D.cap);                // tokens that are there
+    const int base = A.window ? max(0, T.L + i_lo - A.window + 1) & ~31 : 0;
+    const int w_begin = (int)min((int64_t)base + (int64_t)split * P.chunk, (int64_t)n_lim);
+    const int t_end = split == P.nsplit - 1 ? n_lim : (int)min((int64_t)w_begin + P.chunk, (int64_t)n_lim);
+    const int nblocks = (t_end - w_begin + 31) / 32;
+
+    // query fragments, once; they must have arrived before the first counted request
+    const int n0 = T.n0 + wave * WROWS + c;
+    bf16x8 qreg[NT][KS];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+        const int n = n0 + nt * 16, i = n / G;
+        const bf16_t* qp = (const bf16_t*)A.q + (T.row0 + i) * A.q_row + (kvh * G + n - i * G) * A.q_head + g * 8;
+#pragma unroll
+        for (int s = 0; s < KS; ++s)
+            qreg[nt][s] = n < T.QR && s * 32 + g * 8 < hd ? *reinterpret_cast<const bf16x8*>(qp + s * 32) : (bf16x8){0, 0, 0, 0, 0, 0, 0, 0};
+    }
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int s = 0; s < KS; ++s) asm volatile("" : "+v"(qreg[nt][s]));
+
+    // this wave's pieces: id = wave + 8u; below 2*KS keys (half id / KS, features 32 * (id % KS) ..), above values likewise.  Features that the
+    // head does not have are read at feature 0: their query elements are 0, their outputs are not stored.
+    const char* pool[LD];
+    int64_t page_bytes[LD];
+    unsigned voff[LD], ts[LD];
+    int half[LD];
+#pragma unroll
+    for (int u = 0; u < LD; ++u) {
+        const int id = wave + PW_WAVES * u, v = id >= 2 * KS, x = (id - v * 2 * KS) % KS;
+        half[u] = (id - v * 2 * KS) / KS;
+        pool[u] = v ? (const char*)((const bf16_t*)D.p.v + kvh * D.p.v_head) : (const char*)((const bf16_t*)D.p.k + kvh * D.p.k_head);
+        page_bytes[u] = (v ? D.p.v_page : D.p.k_page) * 2;
+        ts[u] = (unsigned)(v ? D.p.v_token : D.p.k_token) * 2;
+        const int token = v ? (lane & 31) >> 1 : c;
+        const int feature = x * 32 + (v ? (lane >> 5) * 16 + (lane & 1) * 8 : g * 8);
+        voff[u] = token * ts[u] + (feature < hd ? feature * 2 : 0);
+    }
+    const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)&stage[0][0];
+
+    // pages of 64 blocks, one per lane; a half whose page does not exist is read from page 0 and masked
+    const int32_t* tab = D.p.table + T.b * D.p.table_stride;
+    int page0 = 0, page1 = 0;
+    unsigned long long ok[2] = {0, 0}, ok_old[2] = {0, 0};
+    auto pages = [&](int blk0) {
+        const int64_t t = (int64_t)w_begin + 32 * ((int64_t)blk0 + lane);
+        int a = -1, b = -1;
+        if (t < t_end) {
+            a = tab[t >> D.page_log2];
+            const int e = (int)((t + 16) >> D.page_log2);
+            b = e < D.p.table_pages ? tab[e] : -1;
+        }
+        const bool oa = (unsigned)a < (unsigned)D.p.n_pages, ob = (unsigned)b < (unsigned)D.p.n_pages;
+        page0 = oa ? a : 0;
+        page1 = ob ? b : 0;
+        ok_old[0] = ok[0], ok_old[1] = ok[1];
+        ok[0] = __ballot(oa), ok[1] = __ballot(ob);
+    };
+    auto issue = [&](int blk, int st) {
+        const int t0 = w_begin + blk * 32;
+#pragma unroll
+        for (int u = 0; u < LD; ++u) {
+            const int page = __builtin_amdgcn_readlane(half[u] ? page1 : page0, blk & 63);
+            const int slot = (t0 + 16 * half[u]) & (D.p.page_size - 1);
+            cs_load_to_lds(voff[u], pool[u] + page * page_bytes[u] + (int64_t)slot * ts[u], lds0 + st * STAGE_BYTES + (wave + PW_WAVES * u) * 1024);
+        }
+    };
+    // at most `n` of this wave's requests still in flight, then meet the other waves
+#define PW_SYNC(n) asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(n) : "memory")
+
+    f32x4 oacc[MT][NT], lacc[NT];
+    float m_run[NT], thr[NT];
+    int q_last[NT];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+        const int i = (n0 + nt * 16) / G;
+        q_last[nt] = T.L + i;
+        m_run[nt] = thr[nt] = -INFINITY;
+        lacc[nt] = (f32x4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) oacc[mt][nt] = (f32x4){0.f, 0.f, 0.f, 0.f};
+    }
+    const float scale2 = A.scale2, inv_scale2 = 1.0f / A.scale2;
+    const bf16_t one = (bf16_t)1.0f;
+    const bf16x8 ones = (bf16x8){one, one, one, one, one, one, one, one};
+
+    auto scores = [&](const unsigned char* sp, f32x4 (&sacc)[2][NT]) {
+        auto k_frag = [&](int a, int s) { return *reinterpret_cast<const bf16x8*>(sp + ((a * KS + s) * 64 + lane) * 16); };
+        bf16x8 k0 = k_frag(0, 0), k1 = k_frag(1, 0);
+#pragma unroll
+        for (int s = 0; s < KS; ++s) {
+            bf16x8 m0 = k0, m1 = k1;
+            if (s + 1 < KS) {
+                m0 = k_frag(0, s + 1);
+                m1 = k_frag(1, s + 1);
+            }
+            const f32x4 zero4 = (f32x4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                sacc[0][nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k0, qreg[nt][s], s == 0 ? zero4 : sacc[0][nt], 0, 0, 0);
+                sacc[1][nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k1, qreg[nt][s], s == 0 ? zero4 : sacc[1][nt], 0, 0, 0);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            k0 = m0;
+            k1 = m1;
+        }
+    };
+    // the running maximum of the tile rows moves (and O is rescaled) only when it is left behind by 2^8
+    auto reference = [&](const f32x4 (&sacc)[2][NT], bool masked) {
+        if (!masked) {
+            bool over = false;
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                const float lm = fmaxf(fmaxf(fmaxf(sacc[0][nt][0], sacc[0][nt][1]), fmaxf(sacc[0][nt][2], sacc[0][nt][3])),
+                                       fmaxf(fmaxf(sacc[1][nt][0], sacc[1][nt][1]), fmaxf(sacc[1][nt][2], sacc[1][nt][3])));
+                over |= !(lm <= thr[nt]);
+            }
+            if (!__any(over)) return;
+        }
+        bool moved = false;
+        float alpha[NT];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            float mx = fmaxf(fmaxf(sacc[0][nt][0], sacc[0][nt][1]), sacc[0][nt][2]);
+            mx = fmaxf(fmaxf(mx, sacc[0][nt][3]), sacc[1][nt][0]);
+            mx = fmaxf(fmaxf(mx, sacc[1][nt][1]), fmaxf(sacc[1][nt][2], sacc[1][nt][3]));
+            mx = fa_row4_max(mx) * scale2;
+            const bool up = mx > m_run[nt] + FA_RESCALE_LOG2;
+            const float m_new = up ? mx : m_run[nt];
+            alpha[nt] = up ? __builtin_amdgcn_exp2f(m_run[nt] - (m_new == -INFINITY ? 0.f : m_new)) : 1.0f;
+            moved |= up;
+            m_run[nt] = m_new;
+            thr[nt] = m_new == -INFINITY ? -INFINITY : (m_new + FA_RESCALE_LOG2) * inv_scale2;
+        }
+        if (__any(moved)) {
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                lacc[nt] *= alpha[nt];
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt) oacc[mt][nt] *= alpha[nt];
+            }
+        }
+    };
+    typedef short s16x4 __attribute__((ext_vector_type(4)));
+    typedef short s16x8 __attribute__((ext_vector_type(8)));
+    auto finish = [&](f32x4 (&sacc)[2][NT], const unsigned char* sp, int t0, auto masked_tag, bool ok0, bool ok1) {
+        constexpr bool MASKED = decltype(masked_tag)::value;
+        if (MASKED) {
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int a = 0; a < 2; ++a)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const int t = t0 + 16 * a + 4 * g + j;
+                        const bool sees = t <= q_last[nt] && (A.window == 0 || t > q_last[nt] - A.window) && t < n_tok && (a ? ok1 : ok0);
+                        sacc[a][nt][j] = sees ? sacc[a][nt][j] : -INFINITY;
+                    }
+        }
+        reference(sacc, MASKED);
+        __builtin_amdgcn_sched_barrier(0);
+        bf16x8 pb[NT];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            const float m_safe = m_run[nt] == -INFINITY ? 0.f : m_run[nt];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) pb[nt][e] = (bf16_t)__builtin_amdgcn_exp2f(fmaf(sacc[e >> 2][nt][e & 3], scale2, -m_safe));
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        bf16x8 vf[4];
+        auto v_frag = [&](int mt) {
+            s16x4 h[2];
+#pragma unroll
+            for (int a = 0; a < 2; ++a) {
+                const unsigned char* p = sp + V_AT + (a * KS + (mt >> 1)) * 1024 + (mt & 1) * 512 + lane * 8;
+                h[a] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(__attribute__((address_space(3))) unsigned char*)p);
+                if (MASKED) {
+                    // what lies behind the last token or in place of a page may be anything, and 0 * anything must stay 0
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        if (t0 + 16 * a + 4 * g + j >= n_tok || !(a ? ok1 : ok0)) h[a][j] = 0;
+                }
+            }
+            return __builtin_bit_cast(bf16x8, (s16x8){h[0][0], h[0][1], h[0][2], h[0][3], h[1][0], h[1][1], h[1][2], h[1][3]});
+        };
+#pragma unroll
+        for (int mt = 0; mt < 3; ++mt) vf[mt] = v_frag(mt);
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
+            if (mt + 3 < MT) vf[(mt + 3) & 3] = v_frag(mt + 3);
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) oacc[mt][nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[mt & 3], pb[nt], oacc[mt][nt], 0, 0, 0);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) lacc[nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pb[nt], lacc[nt], 0, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);
+    };
+
+    // Blocks 0 .. STAGES-2 are requested up front; round i requests block i + STAGES - 1 into the stage that block i - 1 has left,
+    // works on block i, and ends when block i + 1 has landed in every wave's share.
+    constexpr int INFLIGHT = LD * (STAGES - 2);
+    pages(0);
+#pragma unroll
+    for (int j = 0; j < STAGES - 1; ++j) issue(j, j);         // (past the last block: page 0, into a stage that nobody reads)
+    PW_SYNC(INFLIGHT);
+    int st_cur = 0, st_req = STAGES - 1;
+    // The loop's bound and the position come from a vector register that the compiler cannot see through: around branches it
+    // takes for uniform it splits the live ranges of the accumulators, copies and spills them.
+    int vzero;
+    asm volatile("v_mov_b32 %0, 0" : "=v"(vzero));
+    const int nblocks_v = nblocks + vzero;
+    // positions that this wave's rows have: blocks outside what they see are not computed, blocks inside need no mask
+    const int p_lo = T.L + (T.n0 + wave * WROWS) / G + vzero;
+    const int p_hi = T.L + min(T.rows - 1, (T.n0 + wave * WROWS + WROWS - 1) / G) + vzero;
+    // tokens below w_lo are seen by no row of the wave, those from w_hi on by every one (as far as a window goes)
+    const int w_lo = A.window ? p_lo - A.window + 1 : 0, w_hi = A.window ? p_hi - A.window + 1 : 0;
+    const int p_end = T.n0 + wave * WROWS < T.QR ? p_hi : -1;      // a wave without rows multiplies nothing
+    const int p_open = min(p_lo, D.cap - 1);
+    const std::integral_constant<bool, false> plain_tag;
+    const std::integral_constant<bool, true> masked_tag;
+    f32x4 sa[2][NT];
+    for (int i = 0; i < nblocks_v; ++i) {
+        const int ahead = i + STAGES - 1;
+        if ((ahead & 63) == 0) pages(ahead);
+        issue(ahead, st_req);
+        st_req = st_req + 1 == STAGES ? 0 : st_req + 1;
+        const int t0 = w_begin + i * 32;
+        const bool newer = (ahead >> 6) == (i >> 6);
+        const int ok0 = (int)((newer ? ok[0] : ok_old[0]) >> (i & 63)) & 1, ok1 = (int)((newer ? ok[1] : ok_old[1]) >> (i & 63)) & 1;
+        const int gone = 1 - (ok0 & ok1) + vzero;
+        if ((t0 <= p_end) & (t0 + 31 >= w_lo)) {
+            scores(stage[st_cur], sa);
+            if ((t0 + 31 > p_open) | (t0 < w_hi) | (gone != 0)) finish(sa, stage[st_cur], t0, masked_tag, ok0, ok1);
+            else finish(sa, stage[st_cur], t0, plain_tag, true, true);
+        }
+        st_cur = st_cur + 1 == STAGES ? 0 : st_cur + 1;
+        PW_SYNC(INFLIGHT);
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");          // surplus requests, before the LDS is given up
+#undef PW_SYNC
+
+    // oacc[mt][nt][j]: query row nt*16 + c, feature mt*16 + 4g + j
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+        const int n = n0 + nt * 16;
+        if (n >= T.QR) continue;
+        const int i = n / G, h = kvh * G + n - i * G;
+        const int64_t r = T.row0 + i, rh = r * A.H + h;
+        const float l = lacc[nt][0];
+        if (P.nsplit == 1) {
+            const float inv = l > 0.f ? 1.0f / l : 0.f;
+            if (P.nsplit_all > 1 && g == 0) P.pml[rh] = make_float2(0.f, PA_DONE);
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) {
+                const int d = mt * 16 + 4 * g;
+                if (d < hd)
+                    *reinterpret_cast<bf16x4*>((bf16_t*)A.out + r * A.out_row + h * A.out_head + d) =
+                        (bf16x4){(bf16_t)(oacc[mt][nt][0] * inv), (bf16_t)(oacc[mt][nt][1] * inv), (bf16_t)(oacc[mt][nt][2] * inv), (bf16_t)(oacc[mt][nt][3] * inv)};
+            }
+            continue;
+        }
+        const int64_t at = (int64_t)split * D.R * A.H + rh;
+        if (g == 0) {
+            P.pml[at] = make_float2(m_run[nt], l);
+            if (split == 0)
+                for (int s = P.nsplit; s < P.nsplit_all; ++s) P.pml[(int64_t)s * D.R * A.H + rh] = make_float2(-INFINITY, 0.f);
+        }
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
+            const int d = mt * 16 + 4 * g;
+            if (d < hd) *reinterpret_cast<f32x4*>(P.po + at * hd + d) = oacc[mt][nt];
+        }
+    }
+}
+
 // ---- joining token ranges ---------------------------------------------------------------------
 // out[r][h] = sum_s 2^(m_s - M) O_s / sum_s 2^(m_s - M) l_s.  2^lanes_log2 lanes have a row's hd features, four each; a lane reads
 // the (max, sum) pairs of every lanes-th range, and the weights go round by shuffles.
@@ -519,31 +828,59 @@ static int check_shape(const char* who, const cs_pages* p, int32_t n_heads, int3
     return CS_OK;
 }
 
-// How a call is cut: the same for the workspace and the launch.
+// How a call is cut: the same for the workspace and the launches.
+struct pa_part {
+    int nt, TR, qr_lo, qr_hi, tiles, tiles_per, nsplit, chunk;      // tiles 0: no launch
+};
 struct pa_cut {
-    int hdt, nt, tiles, tiles_per, nsplit, chunk;
+    int hdt;
+    pa_part narrow, wide;
+    int room;                                                       // token ranges that the workspace holds
     int64_t part_floats, bytes;
 };
+#define PN_MOST 48                // query rows up to which a stream takes the kernel of few rows
+static void pa_ranges(pa_part& t, int64_t span, int64_t items, int64_t want, int64_t min_chunk) {
+    const int64_t n = std::max<int64_t>(1, std::min<int64_t>(cs_ceil_div(want, items), span / min_chunk));
+    t.chunk = (int)cs_round_up(cs_ceil_div(span, n), 128);
+    t.nsplit = (int)cs_ceil_div(span, t.chunk);
+}
 static pa_cut pa_make_cut(const cs_pages* p, int H, bool has_row0, int R, int max_rows, int64_t max_len, int window) {
-    pa_cut c;
+    pa_cut c = {};
     const int KVH = p->n_kv_heads, G = H / KVH, B = p->batch, cap = p->table_pages * p->page_size;
     const int rows = has_row0 ? (max_rows ? std::min(max_rows, R) : R) : R / B;
-    const int64_t qr = (int64_t)rows * G;
+    const int64_t qr = (int64_t)rows * G, all = (int64_t)R * G;
     c.hdt = p->head_dim <= 64 ? 64 : p->head_dim <= 128 ? 128 : 256;
-    c.nt = (int)std::min<int64_t>(c.hdt == 256 ? 1 : 3, cs_ceil_div(qr, 16));
-    const int TR = 16 * c.nt;
-    c.tiles_per = has_row0 ? 0 : (int)cs_ceil_div(qr, TR);
-    const int64_t tiles = has_row0 ? (int64_t)R * G / TR + std::min(B, R) : (int64_t)B * c.tiles_per;
-    c.tiles = (int)tiles;
     const int64_t len = max_len && max_len < cap ? max_len : cap;
     const int64_t span = window ? std::min<int64_t>(len, (int64_t)window + rows + 32) : len;
-    const int64_t items = tiles * KVH, want = 1024, min_chunk = 256;
-    auto ranges = [&](int64_t tokens) { return std::max<int64_t>(1, std::min<int64_t>(cs_ceil_div(want, items), tokens / min_chunk)); };
-    c.chunk = (int)cs_round_up(cs_ceil_div(span, ranges(span)), 128);
-    c.nsplit = (int)cs_ceil_div(span, c.chunk);
-    const int64_t rh = (int64_t)R * H, room = ranges(len);      // (a window only takes ranges away)
-    c.part_floats = room > 1 ? cs_round_up(room * rh * p->head_dim, 4) : 0;
-    c.bytes = room > 1 ? c.part_floats * 4 + room * rh * 8 : 0;
+    pa_part &N = c.narrow, &W = c.wide;
+    const int n_most = c.hdt == 256 ? 16 : PN_MOST;
+    if (has_row0 || qr <= n_most) {
+        N.nt = (int)std::min<int64_t>(n_most / 16, cs_ceil_div(qr, 16));
+        N.TR = 16 * N.nt;
+        N.qr_hi = qr <= n_most ? 0x7fffffff : n_most;
+        N.tiles_per = has_row0 ? 0 : 1;
+        N.tiles = !has_row0 ? B : qr <= n_most ? (int)std::min<int64_t>(all / N.TR + std::min(B, R), 0x7fffffff) : std::min(B, R);
+    }
+    if (qr > n_most) {
+        W.nt = c.hdt == 256 ? 1 : 2;
+        W.TR = PW_WAVES * 16 * W.nt;
+        W.qr_lo = has_row0 ? n_most : 0;
+        W.qr_hi = 0x7fffffff;
+        W.tiles_per = has_row0 ? 0 : (int)cs_ceil_div(qr, W.TR);
+        W.tiles = has_row0 ? (int)(all / W.TR + std::min<int64_t>(B, all / (n_most + 1))) : B * W.tiles_per;
+    }
+    if (N.tiles) pa_ranges(N, span, (int64_t)N.tiles * KVH, 1024, 256);
+    if (W.tiles) pa_ranges(W, span, (int64_t)W.tiles * KVH, 512, 512);
+    // (a window only takes ranges away)
+    pa_part n = N, w = W;
+    if (N.tiles) pa_ranges(n, len, (int64_t)N.tiles * KVH, 1024, 256);
+    if (W.tiles) pa_ranges(w, len, (int64_t)W.tiles * KVH, 512, 512);
+    c.room = std::max(std::max(n.nsplit, w.nsplit), std::max(N.nsplit, W.nsplit));
+    if (c.room > 1) {
+        const int64_t rh = (int64_t)R * H;
+        c.part_floats = cs_round_up(c.room * rh * p->head_dim, 4);
+        c.bytes = c.part_floats * 4 + c.room * rh * 8;
+    }
     return c;
 }
 
@@ -561,6 +898,14 @@ template <int HD, int NT>
 static int pn_launch(const cs_pages_dev& D, const pa_args& A, const pa_plan& P, unsigned grid, hipStream_t s) {
     k_paged_narrow<HD, NT><<<grid, 64 * PN_WAVES, 0, s>>>(D, A, P);
     return cs_launch_ok("k_paged_narrow");
+}
+template <int HD, int NT>
+static int pw_launch(const cs_pages_dev& D, const pa_args& A, const pa_plan& P, unsigned grid, hipStream_t s) {
+    k_paged_wide<HD, NT><<<grid, 64 * PW_WAVES, 0, s>>>(D, A, P);
+    return cs_launch_ok("k_paged_wide");
+}
+static pa_plan pa_plan_of(const pa_part& t, int nsplit_all, float* po, float2* pml) {
+    return {t.TR, t.qr_lo, t.qr_hi, t.nsplit, nsplit_all, t.chunk, t.tiles_per, po, pml};
 }
 
 extern "C" int cs_paged_attention(const cs_pages* p, const void* q, int64_t q_row, int64_t q_head, int32_t n_heads,
@@ -587,19 +932,30 @@ extern "C" int cs_paged_attention(const cs_pages* p, const void* q, int64_t q_ro
     CS_REQUIRE(c.bytes <= 0 || (workspace && workspace_bytes >= c.bytes), CS_E_CAPACITY, "%s: the workspace has %lld bytes, %lld are needed",
                who, (long long)(workspace ? workspace_bytes : 0), (long long)c.bytes);
     CS_REQUIRE(((uintptr_t)workspace & 15) == 0, CS_E_ARG, "%s: the workspace is not aligned to 16 bytes", who);
-    pa_plan P = {16 * c.nt, 0, 0x7fffffff, c.nsplit, c.nsplit, c.chunk, c.tiles_per, (float*)workspace, (float2*)((float*)workspace + c.part_floats)};
-    const int64_t grid = (int64_t)c.tiles * p->n_kv_heads * c.nsplit;
-    CS_REQUIRE(grid <= 0x7fffffff, CS_E_UNSUPPORTED, "%s: too many tiles", who);
-    int rc = CS_E_STATE;
-#define PN(HD_, NT_) if (c.hdt == HD_ && c.nt == NT_) rc = pn_launch<HD_, NT_>(D, A, P, (unsigned)grid, s)
-    PN(64, 1); PN(64, 2); PN(64, 3); PN(128, 1); PN(128, 2); PN(128, 3); PN(256, 1);
+    float* po = (float*)workspace;
+    float2* pml = (float2*)(po + c.part_floats);
+    const int nsplit = std::max(c.narrow.nsplit, c.wide.nsplit);
+    const int64_t grid_n = (int64_t)c.narrow.tiles * p->n_kv_heads * c.narrow.nsplit, grid_w = (int64_t)c.wide.tiles * p->n_kv_heads * c.wide.nsplit;
+    CS_REQUIRE(grid_n <= 0x7fffffff && grid_w <= 0x7fffffff, CS_E_UNSUPPORTED, "%s: too many tiles", who);
+    if (grid_w) {
+        const pa_plan P = pa_plan_of(c.wide, nsplit, po, pml);
+        if (c.hdt == 64) CS_TRY((pw_launch<64, 2>(D, A, P, (unsigned)grid_w, s)));
+        else if (c.hdt == 128) CS_TRY((pw_launch<128, 2>(D, A, P, (unsigned)grid_w, s)));
+        else CS_TRY((pw_launch<256, 1>(D, A, P, (unsigned)grid_w, s)));
+    }
+    if (grid_n) {
+        const pa_plan P = pa_plan_of(c.narrow, nsplit, po, pml);
+        int rc = CS_E_STATE;
+#define PN(HD_, NT_) if (c.hdt == HD_ && c.narrow.nt == NT_) rc = pn_launch<HD_, NT_>(D, A, P, (unsigned)grid_n, s)
+        PN(64, 1); PN(64, 2); PN(64, 3); PN(128, 1); PN(128, 2); PN(128, 3); PN(256, 1);
 #undef PN
-    CS_TRY(rc);
-    if (c.nsplit > 1) {
+        CS_TRY(rc);
+    }
+    if (nsplit > 1) {
         int lanes = 0;
         while (4 << lanes < p->head_dim) ++lanes;
         const int64_t rh = (int64_t)R * n_heads;
-        k_paged_merge<bf16_t><<<(unsigned)cs_ceil_div(rh, 256 >> lanes), 256, 0, s>>>(P.po, P.pml, c.nsplit, rh, n_heads, p->head_dim, lanes,
+        k_paged_merge<bf16_t><<<(unsigned)cs_ceil_div(rh, 256 >> lanes), 256, 0, s>>>(po, pml, nsplit, rh, n_heads, p->head_dim, lanes,
                                                                              d_row0 ? d_row0 + p->batch : nullptr, (bf16_t*)out, out_row, out_head);
         return cs_launch_ok("k_paged_merge");
     }
