@@ -19,68 +19,6 @@ struct pa_args {
     float scale2;             // scale * log2(e): scores in base-2 units
 };
 
-__device__ __forceinline__ float ld1(const float* p) { return *p; }
-__device__ __forceinline__ float ld1(const bf16_t* p) { return (float)*p; }
-
-// a wave per (row, query head): a token per lane for the scores, four features per lane for the output
-template <typename T>
-__global__ __launch_bounds__(256) void k_paged_plain(cs_pages_dev D, pa_args A) {
-    __shared__ float sq[4][256];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t task = (int64_t)blockIdx.x * 4 + wave;
-    const int hd = D.p.head_dim;
-    const int r = (int)(task / A.H), h = (int)(task % A.H), g = h / A.G;
-    int b = -1, i = 0;
-    if (r < D.R)
-        for (int s = 0; s < D.p.batch; ++s) {
-            const int2 sr = cs_stream_rows(D, s);
-            if (r >= sr.x && r < sr.x + sr.y) { b = s; i = r - sr.x; break; }
-        }
-    if (b >= 0)
-        for (int d = lane; d < hd; d += 64) sq[wave][d] = ld1((const T*)A.q + r * A.q_row + h * A.q_head + d);
-    __syncthreads();
-    if (b < 0) return;
-    const int L = cs_stream_len(D, b);
-    const int last = min(L + i, D.cap - 1), first = A.window ? max(0, L + i - A.window + 1) : 0;
-    float m = -INFINITY, l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int t0 = first & ~63; t0 <= last; t0 += 64) {
-        const int t = t0 + lane;
-        int page = -1;
-        float s = -INFINITY;
-        if (t >= first && t <= last) {
-            page = D.p.table[b * D.p.table_stride + (t >> D.page_log2)];
-            if (page >= D.p.n_pages) page = -1;
-        }
-        const int slot = t & (D.p.page_size - 1);
-        if (page >= 0) {
-            const T* kr = (const T*)D.p.k + page * D.p.k_page + g * D.p.k_head + slot * D.p.k_token;
-            s = 0.f;
-            for (int d = 0; d < hd; ++d) s += sq[wave][d] * ld1(kr + d);
-            s *= A.scale2;
-        }
-        const float mn = fmaxf(m, cs_wave_max(s));
-        if (mn == -INFINITY) continue;
-        const float alpha = exp2f(m - mn), p = page >= 0 ? exp2f(s - mn) : 0.f;
-        l = l * alpha + cs_wave_sum(p);
-        m = mn;
-#pragma unroll
-        for (int u = 0; u < 4; ++u) o[u] *= alpha;
-        for (int j = 0; j < 64; ++j) {
-            const int pj = __shfl(page, j, 64);
-            const float w = __shfl(p, j, 64);
-            if (pj < 0) continue;
-            const T* vr = (const T*)D.p.v + pj * D.p.v_page + g * D.p.v_head + ((t0 + j) & (D.p.page_size - 1)) * D.p.v_token;
-#pragma unroll
-            for (int u = 0; u < 4; ++u)
-                if (lane + 64 * u < hd) o[u] += w * ld1(vr + lane + 64 * u);
-        }
-    }
-    T* out = (T*)A.out + r * A.out_row + h * A.out_head;
-#pragma unroll
-    for (int u = 0; u < 4; ++u)
-        if (lane + 64 * u < hd) cs_st(out, lane + 64 * u, l > 0.f ? o[u] / l : 0.f);
-}
-
 // ---- which query rows a workgroup has ----------------------------------------------------
 // The G * rows query rows of a stream's KV head (row n: block row n / G, head n % G of the group) are cut into tiles of TR.
 // Streams with qr_lo < G * rows <= qr_hi take part in a launch.
@@ -141,9 +79,14 @@ __device__ __forceinline__ bool pa_find_tile(const cs_pages_dev& D, int G, const
     return o.n0 < o.QR;
 }
 
+__device__ __forceinline__ void pa_store4(float* p, f32x4 v) { *reinterpret_cast<f32x4*>(p) = v; }
+__device__ __forceinline__ void pa_store4(bf16_t* p, f32x4 v) {
+    *reinterpret_cast<bf16x4*>(p) = (bf16x4){(bf16_t)v[0], (bf16_t)v[1], (bf16_t)v[2], (bf16_t)v[3]};
+}
+
 // The (max, sum, O) triples of W waves side by side in LDS -> the tile's rows: the output itself where the tokens are in one
 // range, else this range's partial result.
-template <int W, int HD, int ROWS>
+template <int W, int HD, int ROWS, typename T_>
 __device__ __forceinline__ void pa_finish(const cs_pages_dev& D, const pa_args& A, const pa_plan& P, const pa_tile& T, int kvh, int split,
                                           int n_rows, const float* s_o, const float2* s_ml, int tid, int n_threads) {
     constexpr int OROW = HD + 4;
@@ -171,11 +114,7 @@ __device__ __forceinline__ void pa_finish(const cs_pages_dev& D, const pa_args& 
         const int64_t r = T.row0 + i, rh = r * A.H + h;
         if (P.nsplit == 1) {
             const float inv = l > 0.f ? 1.0f / l : 0.f;           // a row that sees nothing: 0
-            if (d < hd) {
-                typedef __bf16 bf16x4_t __attribute__((ext_vector_type(4)));
-                *reinterpret_cast<bf16x4_t*>((bf16_t*)A.out + r * A.out_row + h * A.out_head + d) =
-                    (bf16x4_t){(bf16_t)(o[0] * inv), (bf16_t)(o[1] * inv), (bf16_t)(o[2] * inv), (bf16_t)(o[3] * inv)};
-            }
+            if (d < hd) pa_store4((T_*)A.out + r * A.out_row + h * A.out_head + d, o * inv);
             if (P.nsplit_all > 1 && d == 0) P.pml[rh] = make_float2(0.f, PA_DONE);
             continue;
         }
@@ -467,7 +406,7 @@ __global__ __launch_bounds__(64 * PN_WAVES) void k_paged_narrow(cs_pages_dev D, 
                 }
     }
     __syncthreads();
-    pa_finish<PN_WAVES, HD, ROWS>(D, A, P, T, kvh, split, n_rows, s_o, s_ml, tid, 64 * PN_WAVES);
+    pa_finish<PN_WAVES, HD, ROWS, bf16_t>(D, A, P, T, kvh, split, n_rows, s_o, s_ml, tid, 64 * PN_WAVES);
 }
 
 // ---- many query rows: the matrix cores and the vector unit are the bound -----------------------------
@@ -758,9 +697,7 @@ __global__ __launch_bounds__(64 * PW_WAVES) void k_paged_wide(cs_pages_dev D, pa
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt) {
                 const int d = mt * 16 + 4 * g;
-                if (d < hd)
-                    *reinterpret_cast<bf16x4*>((bf16_t*)A.out + r * A.out_row + h * A.out_head + d) =
-                        (bf16x4){(bf16_t)(oacc[mt][nt][0] * inv), (bf16_t)(oacc[mt][nt][1] * inv), (bf16_t)(oacc[mt][nt][2] * inv), (bf16_t)(oacc[mt][nt][3] * inv)};
+                if (d < hd) pa_store4((bf16_t*)A.out + r * A.out_row + h * A.out_head + d, oacc[mt][nt] * inv);
             }
             continue;
         }
@@ -774,6 +711,250 @@ __global__ __launch_bounds__(64 * PW_WAVES) void k_paged_wide(cs_pages_dev D, pa
         for (int mt = 0; mt < MT; ++mt) {
             const int d = mt * 16 + 4 * g;
             if (d < hd) *reinterpret_cast<f32x4*>(P.po + at * hd + d) = oacc[mt][nt];
+        }
+    }
+}
+
+// ---- float32 caches: everything in float32, on the float32 matrix instruction -------------------------
+//   S^T[token][row] = K . Q^T, O^T[feature][row] += V^T . P^T over blocks of 16 tokens, four k per instruction.
+// Lane (c, g) loads 16 bytes of a key row, four steps of the first product; the rows of S^T that it gets are the k of the second
+// one, step j taking token 4g + j, and its 16 bytes of that token's value row are four features 4c + u, one for each
+// of four tiles.  So nothing is moved between lanes, and nothing goes through LDS but the query rows (and, with TOKENS, the
+// waves' results: few rows, where the waves share them and take the token blocks in turn; without it every wave has 16 * NT rows
+// of its own, and what bounds it is the instruction's rate, 157 TFLOP/s, the re-read blocks coming out of the caches).
+#define PF_WAVES 4
+template <int HD, int NT, bool TOKENS>
+__global__ __launch_bounds__(64 * PF_WAVES) void k_paged_f32(cs_pages_dev D, pa_args A, pa_plan P) {
+    constexpr int KL = HD / 16, VX = HD / 64, MT = HD / 16;
+    constexpr int WROWS = 16 * NT, TR = TOKENS ? WROWS : PF_WAVES * WROWS, OROW = HD + 4, QROW = HD + 4;
+    constexpr int MERGE_FLOATS = TOKENS ? PF_WAVES * WROWS * (OROW + 2) : 0, Q_FLOATS = TR * QROW;
+    __shared__ __attribute__((aligned(16))) float smem[MERGE_FLOATS > Q_FLOATS ? MERGE_FLOATS : Q_FLOATS];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int c = lane & 15, g = lane >> 4;
+    const int KVH = D.p.n_kv_heads, kvh = blockIdx.x % KVH, rest = blockIdx.x / KVH;
+    const int split = rest % P.nsplit, tile = (int)(gridDim.x / (KVH * P.nsplit)) - 1 - rest / P.nsplit;
+    pa_tile T;
+    if (!pa_find_tile(D, A.G, P, tile, T)) return;
+    const int hd = D.p.head_dim, G = A.G;
+    const int n_rows = min(TR, T.QR - T.n0);
+    const int i_hi = (T.n0 + n_rows - 1) / G;
+    const int n_lim = min(T.L + i_hi + 1, D.cap);
+    const int base = A.window ? max(0, T.L + T.n0 / G - A.window + 1) & ~31 : 0;
+    const int w_begin = (int)min((int64_t)base + (int64_t)split * P.chunk, (int64_t)n_lim);
+    const int t_end = split == P.nsplit - 1 ? n_lim : (int)min((int64_t)w_begin + P.chunk, (int64_t)n_lim);
+    for (int idx = tid; idx < TR * (HD / 4); idx += 64 * PF_WAVES) {
+        const int n = idx / (HD / 4), d = idx % (HD / 4) * 4;
+        f32x4 v = (f32x4){0.f, 0.f, 0.f, 0.f};
+        if (n < n_rows && d < hd) {
+            const int i = (T.n0 + n) / G, h = kvh * G + T.n0 + n - i * G;
+            v = *reinterpret_cast<const f32x4*>((const float*)A.q + (T.row0 + i) * A.q_row + h * A.q_head + d);
+        }
+        *reinterpret_cast<f32x4*>(&smem[n * QROW + d]) = v;
+    }
+    const int wrow = TOKENS ? 0 : wave * WROWS;         // the wave's first row in the tile
+    const int w_rows = max(0, min(WROWS, n_rows - wrow));
+    // positions of the wave's first and last row, tokens that it walks
+    const int p_lo = T.L + (T.n0 + wrow) / G, p_hi = T.L + (T.n0 + wrow + max(w_rows, 1) - 1) / G;
+    const int my_end = w_rows ? min(t_end, min(p_hi + 1, D.cap)) : w_begin;
+    const int open_lo = A.window ? p_hi - A.window + 1 : 0, open_hi = min(p_lo + 1, D.cap);
+    int q_last[NT];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+        const int n = wrow + nt * 16 + c;
+        q_last[nt] = n < n_rows ? T.L + (T.n0 + n) / G : -1;
+    }
+    const float* Kh = (const float*)D.p.k + kvh * D.p.k_head;
+    const float* Vh = (const float*)D.p.v + kvh * D.p.v_head;
+    const int32_t* tab = D.p.table + T.b * D.p.table_stride;
+    constexpr unsigned NOWHERE = 0x80000000u;
+    const unsigned kts = (unsigned)D.p.k_token * 4, vts = (unsigned)D.p.v_token * 4;
+    unsigned koff[KL], voff[4][VX];
+#pragma unroll
+    for (int s = 0; s < KL; ++s) koff[s] = s * 16 + g * 4 < hd ? c * kts + s * 64 + g * 16 : NOWHERE;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int x = 0; x < VX; ++x) voff[j][x] = x * 64 + c * 4 < hd ? (4 * g + j) * vts + x * 256 + c * 16 : NOWHERE;
+
+    f32x4 oacc[MT][NT];
+    float m_run[NT], l_run[NT];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+        m_run[nt] = -INFINITY;
+        l_run[nt] = 0.f;
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) oacc[mt][nt] = (f32x4){0.f, 0.f, 0.f, 0.f};
+    }
+    const float scale2 = A.scale2;
+    __syncthreads();
+
+    constexpr int STEP = TOKENS ? 16 * PF_WAVES : 16;
+    for (int seg0 = w_begin; seg0 < t_end; seg0 += 64 * STEP) {
+        const int t_begin = seg0 + (TOKENS ? 16 * wave : 0);
+        const int n_all = t_begin < my_end ? min(64, (my_end - t_begin + STEP - 1) / STEP) : 0;
+        int page_l = -1;
+        {
+            const int64_t tb = (int64_t)t_begin + (int64_t)lane * STEP;
+            if (tb < my_end) page_l = tab[tb >> D.page_log2];
+            page_l = (unsigned)page_l < (unsigned)D.p.n_pages ? page_l : -1;
+        }
+        auto at = [&](int i) { return t_begin + i * STEP; };
+        auto page_of = [&](int i) { return __builtin_amdgcn_readlane(page_l, i); };
+        auto buffer = [&](const float* head, int64_t page_stride, unsigned ts, int i) {
+            const int t = at(i), page = i < n_all ? page_of(i) : -1, live = min(16, n_lim - t);
+            const unsigned bytes = page >= 0 && live > 0 ? (live - 1) * ts + hd * 4 : 0;
+            const char* p = (const char*)(head + (page >= 0 ? page : 0) * page_stride) + (int64_t)(t & (D.p.page_size - 1)) * ts;
+            return __builtin_amdgcn_make_buffer_rsrc((void*)p, 0, (int)bytes, CS_BUFFER_WORD3);
+        };
+        auto ldk = [&](f32x4 (&buf)[KL], int i) {
+            const auto rs = buffer(Kh, D.p.k_page, kts, i);
+#pragma unroll
+            for (int s = 0; s < KL; ++s) buf[s] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(rs, koff[s], 0, 0));
+        };
+        auto ldv = [&](f32x4 (&buf)[4][VX], int i) {
+            const auto rs = buffer(Vh, D.p.v_page, vts, i);
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int x = 0; x < VX; ++x) buf[j][x] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(rs, voff[j][x], 0, 0));
+        };
+        auto block = [&](f32x4 (&kb)[KL], f32x4 (&vb)[4][VX], int i) {
+            f32x4 sacc[NT];
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) sacc[nt] = (f32x4){0.f, 0.f, 0.f, 0.f};
+            f32x4 odd[NT];                              // a second chain, where one would wait for itself
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) odd[nt] = (f32x4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int s = 0; s < KL; ++s) {
+                f32x4 qb[NT];
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) qb[nt] = *reinterpret_cast<const f32x4*>(&smem[(wrow + nt * 16 + c) * QROW + s * 16 + g * 4]);
+#pragma unroll
+                for (int u = 0; u < 4; ++u)
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) {
+                        f32x4& z = u & 1 ? odd[nt] : sacc[nt];
+                        z = __builtin_amdgcn_mfma_f32_16x16x4f32(kb[s][u], qb[nt][u], z, 0, 0, 0);
+                    }
+            }
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) sacc[nt] += odd[nt];
+            __builtin_amdgcn_sched_barrier(0);
+            ldk(kb, i + 2);
+            __builtin_amdgcn_sched_barrier(0);
+            const int t0 = at(i), page = page_of(i);
+            if (t0 < open_lo || t0 + 16 > open_hi || page < 0) {
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const int t = t0 + 4 * g + j;
+                        const bool sees = t <= q_last[nt] && (A.window == 0 || t > q_last[nt] - A.window) && t < D.cap && page >= 0;
+                        sacc[nt][j] = sees ? sacc[nt][j] : -INFINITY;
+                    }
+            }
+            bool moved = false;
+            float alpha[NT];
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                const float mx = fa_row4_max(fmaxf(fmaxf(sacc[nt][0], sacc[nt][1]), fmaxf(sacc[nt][2], sacc[nt][3]))) * scale2;
+                const bool up = mx > m_run[nt] + FA_RESCALE_LOG2;
+                const float m_new = up ? mx : m_run[nt];
+                const float m_safe = m_new == -INFINITY ? 0.f : m_new;
+                alpha[nt] = up ? __builtin_amdgcn_exp2f(m_run[nt] - m_safe) : 1.0f;
+                moved |= up;
+                m_run[nt] = m_new;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) sacc[nt][j] = __builtin_amdgcn_exp2f(fmaf(sacc[nt][j], scale2, -m_safe));
+            }
+            if (__any(moved)) {
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+                    l_run[nt] *= alpha[nt];
+#pragma unroll
+                    for (int mt = 0; mt < MT; ++mt) oacc[mt][nt] *= alpha[nt];
+                }
+            }
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) l_run[nt] += (sacc[nt][0] + sacc[nt][1]) + (sacc[nt][2] + sacc[nt][3]);
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int x = 0; x < VX; ++x)
+#pragma unroll
+                    for (int u = 0; u < 4; ++u)
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt)
+                            oacc[x * 4 + u][nt] = __builtin_amdgcn_mfma_f32_16x16x4f32(vb[j][x][u], sacc[nt][j], oacc[x * 4 + u][nt], 0, 0, 0);
+        };
+        f32x4 k0[KL], k1[KL], v0[4][VX], v1[4][VX];
+        __builtin_amdgcn_sched_barrier(0);
+        ldk(k0, 0);
+        __builtin_amdgcn_sched_barrier(0);
+        ldv(v0, 0);
+        __builtin_amdgcn_sched_barrier(0);
+        ldk(k1, 1);
+        __builtin_amdgcn_sched_barrier(0);
+        int i = 0;
+        for (; i + 1 < n_all; i += 2) {
+            ldv(v1, i + 1);
+            __builtin_amdgcn_sched_barrier(0);
+            block(k0, v0, i);
+            ldv(v0, i + 2);
+            __builtin_amdgcn_sched_barrier(0);
+            block(k1, v1, i + 1);
+        }
+        if (i < n_all) block(k0, v0, i);
+    }
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {                   // a row's sum is spread over its four lanes
+        l_run[nt] += __shfl_xor(l_run[nt], 16, 64);
+        l_run[nt] += __shfl_xor(l_run[nt], 32, 64);
+    }
+    // oacc[x*4 + u][nt][j]: query row nt*16 + c, feature x*64 + 16g + 4j + u
+    if constexpr (TOKENS) {
+        __syncthreads();
+        float* s_o = smem;
+        float2* s_ml = reinterpret_cast<float2*>(s_o + PF_WAVES * WROWS * OROW);
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            const int n = wave * WROWS + nt * 16 + c;
+            if (g == 0) s_ml[n] = make_float2(m_run[nt], l_run[nt]);
+#pragma unroll
+            for (int x = 0; x < VX; ++x)
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    *reinterpret_cast<f32x4*>(&s_o[n * OROW + x * 64 + 16 * g + 4 * j]) =
+                        (f32x4){oacc[x * 4][nt][j], oacc[x * 4 + 1][nt][j], oacc[x * 4 + 2][nt][j], oacc[x * 4 + 3][nt][j]};
+        }
+        __syncthreads();
+        pa_finish<PF_WAVES, HD, WROWS, float>(D, A, P, T, kvh, split, n_rows, s_o, s_ml, tid, 64 * PF_WAVES);
+    } else {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            const int n = wrow + nt * 16 + c;
+            if (n >= n_rows) continue;
+            const int i = (T.n0 + n) / G, h = kvh * G + T.n0 + n - i * G;
+            const int64_t r = T.row0 + i, rh = r * A.H + h, at = (int64_t)split * D.R * A.H + rh;
+            const bool whole = P.nsplit == 1;
+            const float inv = l_run[nt] > 0.f ? 1.0f / l_run[nt] : 0.f;
+            if (g == 0) {
+                if (!whole) P.pml[at] = make_float2(m_run[nt], l_run[nt]);
+                else if (P.nsplit_all > 1) P.pml[rh] = make_float2(0.f, PA_DONE);
+                if (!whole && split == 0)
+                    for (int s = P.nsplit; s < P.nsplit_all; ++s) P.pml[(int64_t)s * D.R * A.H + rh] = make_float2(-INFINITY, 0.f);
+            }
+#pragma unroll
+            for (int x = 0; x < VX; ++x)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int d = x * 64 + 16 * g + 4 * j;
+                    const f32x4 o = (f32x4){oacc[x * 4][nt][j], oacc[x * 4 + 1][nt][j], oacc[x * 4 + 2][nt][j], oacc[x * 4 + 3][nt][j]};
+                    if (d >= hd) continue;
+                    if (whole) pa_store4((float*)A.out + r * A.out_row + h * A.out_head + d, o * inv);
+                    else pa_store4(P.po + at * hd + d, o);
+                }
         }
     }
 }
@@ -853,6 +1034,7 @@ static pa_cut pa_make_cut(const cs_pages* p, int H, bool has_row0, int R, int ma
     const int64_t len = max_len && max_len < cap ? max_len : cap;
     const int64_t span = window ? std::min<int64_t>(len, (int64_t)window + rows + 32) : len;
     pa_part &N = c.narrow, &W = c.wide;
+    const bool f32 = p->dtype == CS_F32;
     const int n_most = c.hdt == 256 ? 16 : PN_MOST;
     if (has_row0 || qr <= n_most) {
         N.nt = (int)std::min<int64_t>(n_most / 16, cs_ceil_div(qr, 16));
@@ -863,7 +1045,7 @@ static pa_cut pa_make_cut(const cs_pages* p, int H, bool has_row0, int R, int ma
     }
     if (qr > n_most) {
         W.nt = c.hdt == 256 ? 1 : 2;
-        W.TR = PW_WAVES * 16 * W.nt;
+        W.TR = (f32 ? PF_WAVES : PW_WAVES) * 16 * W.nt;
         W.qr_lo = has_row0 ? n_most : 0;
         W.qr_hi = 0x7fffffff;
         W.tiles_per = has_row0 ? 0 : (int)cs_ceil_div(qr, W.TR);
@@ -890,7 +1072,7 @@ extern "C" int64_t cs_paged_attention_workspace(const cs_pages* p, int32_t n_hea
     CS_TRY(check_shape(who, p, n_heads, R, max_rows, max_len));
     CS_REQUIRE(has_row0 || p->batch == 0 || R % p->batch == 0, CS_E_ARG, "%s: R rows cannot be shared out among %d streams without d_row0",
                who, p->batch);
-    if (R == 0 || p->batch == 0 || p->dtype != CS_BF16) return 0;
+    if (R == 0 || p->batch == 0) return 0;
     return pa_make_cut(p, n_heads, has_row0 != 0, R, max_rows, max_len, 0).bytes;
 }
 
@@ -898,6 +1080,11 @@ template <int HD, int NT>
 static int pn_launch(const cs_pages_dev& D, const pa_args& A, const pa_plan& P, unsigned grid, hipStream_t s) {
     k_paged_narrow<HD, NT><<<grid, 64 * PN_WAVES, 0, s>>>(D, A, P);
     return cs_launch_ok("k_paged_narrow");
+}
+template <int HD, int NT, bool TOKENS>
+static int pf_launch(const cs_pages_dev& D, const pa_args& A, const pa_plan& P, unsigned grid, hipStream_t s) {
+    k_paged_f32<HD, NT, TOKENS><<<grid, 64 * PF_WAVES, 0, s>>>(D, A, P);
+    return cs_launch_ok("k_paged_f32");
 }
 template <int HD, int NT>
 static int pw_launch(const cs_pages_dev& D, const pa_args& A, const pa_plan& P, unsigned grid, hipStream_t s) {
@@ -924,10 +1111,6 @@ extern "C" int cs_paged_attention(const cs_pages* p, const void* q, int64_t q_ro
     CS_TRY(cs_check_rows(who, "out", out, out_row, out_head, esz));
     pa_args A = {q, q_row, q_head, out, out_row, out_head, n_heads, n_heads / p->n_kv_heads, window, scale * 1.4426950408889634f};
     hipStream_t s = (hipStream_t)stream;
-    if (p->dtype == CS_F32) {
-        k_paged_plain<float><<<(unsigned)cs_ceil_div((int64_t)R * n_heads, 4), 256, 0, s>>>(D, A);
-        return cs_launch_ok("k_paged_plain");
-    }
     pa_cut c = pa_make_cut(p, n_heads, d_row0 != nullptr, R, max_rows, max_len, window);
     CS_REQUIRE(c.bytes <= 0 || (workspace && workspace_bytes >= c.bytes), CS_E_CAPACITY, "%s: the workspace has %lld bytes, %lld are needed",
                who, (long long)(workspace ? workspace_bytes : 0), (long long)c.bytes);
@@ -937,16 +1120,19 @@ extern "C" int cs_paged_attention(const cs_pages* p, const void* q, int64_t q_ro
     const int nsplit = std::max(c.narrow.nsplit, c.wide.nsplit);
     const int64_t grid_n = (int64_t)c.narrow.tiles * p->n_kv_heads * c.narrow.nsplit, grid_w = (int64_t)c.wide.tiles * p->n_kv_heads * c.wide.nsplit;
     CS_REQUIRE(grid_n <= 0x7fffffff && grid_w <= 0x7fffffff, CS_E_UNSUPPORTED, "%s: too many tiles", who);
+    const bool f32 = p->dtype == CS_F32;
+    int rc = CS_OK;
     if (grid_w) {
         const pa_plan P = pa_plan_of(c.wide, nsplit, po, pml);
-        if (c.hdt == 64) CS_TRY((pw_launch<64, 2>(D, A, P, (unsigned)grid_w, s)));
-        else if (c.hdt == 128) CS_TRY((pw_launch<128, 2>(D, A, P, (unsigned)grid_w, s)));
-        else CS_TRY((pw_launch<256, 1>(D, A, P, (unsigned)grid_w, s)));
+        const unsigned n = (unsigned)grid_w;
+        if (f32) rc = c.hdt == 64 ? pf_launch<64, 2, false>(D, A, P, n, s) : c.hdt == 128 ? pf_launch<128, 2, false>(D, A, P, n, s) : pf_launch<256, 1, false>(D, A, P, n, s);
+        else rc = c.hdt == 64 ? pw_launch<64, 2>(D, A, P, n, s) : c.hdt == 128 ? pw_launch<128, 2>(D, A, P, n, s) : pw_launch<256, 1>(D, A, P, n, s);
+        CS_TRY(rc);
     }
     if (grid_n) {
         const pa_plan P = pa_plan_of(c.narrow, nsplit, po, pml);
-        int rc = CS_E_STATE;
-#define PN(HD_, NT_) if (c.hdt == HD_ && c.narrow.nt == NT_) rc = pn_launch<HD_, NT_>(D, A, P, (unsigned)grid_n, s)
+        const unsigned n = (unsigned)grid_n;
+#define PN(HD_, NT_) if (c.hdt == HD_ && c.narrow.nt == NT_) rc = f32 ? pf_launch<HD_, NT_, true>(D, A, P, n, s) : pn_launch<HD_, NT_>(D, A, P, n, s)
         PN(64, 1); PN(64, 2); PN(64, 3); PN(128, 1); PN(128, 2); PN(128, 3); PN(256, 1);
 #undef PN
         CS_TRY(rc);
@@ -955,8 +1141,10 @@ extern "C" int cs_paged_attention(const cs_pages* p, const void* q, int64_t q_ro
         int lanes = 0;
         while (4 << lanes < p->head_dim) ++lanes;
         const int64_t rh = (int64_t)R * n_heads;
-        k_paged_merge<bf16_t><<<(unsigned)cs_ceil_div(rh, 256 >> lanes), 256, 0, s>>>(po, pml, nsplit, rh, n_heads, p->head_dim, lanes,
-                                                                             d_row0 ? d_row0 + p->batch : nullptr, (bf16_t*)out, out_row, out_head);
+        const unsigned n = (unsigned)cs_ceil_div(rh, 256 >> lanes);
+        const int32_t* end = d_row0 ? d_row0 + p->batch : nullptr;
+        if (f32) k_paged_merge<float><<<n, 256, 0, s>>>(po, pml, nsplit, rh, n_heads, p->head_dim, lanes, end, (float*)out, out_row, out_head);
+        else k_paged_merge<bf16_t><<<n, 256, 0, s>>>(po, pml, nsplit, rh, n_heads, p->head_dim, lanes, end, (bf16_t*)out, out_row, out_head);
         return cs_launch_ok("k_paged_merge");
     }
     return CS_OK;
