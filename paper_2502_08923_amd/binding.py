@@ -638,34 +638,60 @@ def cs_op_argmax_accept(model: Model, logits: torch.Tensor, draft: torch.Tensor,
 _DTYPES = {torch.float32: CS_F32, torch.bfloat16: CS_BF16}
 
 
-def _place(tensors, stream):
-    """(context, raw stream, torch stream or None) for a call on these tensors: the device is theirs, whatever the current
-    one is, and the default stream is that device's current one."""
+# (torch's own accessor, where it is there, costs a tenth of the public one)
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+
+
+def _device_of(tensors) -> int:
+    """Index of the one device that holds all of them (None: left out)."""
     dev = None
-    for name, t in tensors:
-        if t is None:
-            continue
-        if not t.is_cuda:
-            raise TypeError(f"{name} must be a CUDA tensor")
-        if dev is None:
-            dev = t.device
-        elif t.device != dev:
-            raise ValueError(f"{name} is on {t.device}, the other tensors on {dev}")
-    if stream is not None and not hasattr(stream, "cuda_stream"):
-        stream = torch.cuda.ExternalStream(int(stream), device=dev)
-    if stream is not None and stream.device != dev:
-        raise ValueError(f"the stream belongs to {stream.device}, the tensors are on {dev}")
-    here = contextlib.nullcontext() if torch.cuda.current_device() == dev.index else torch.cuda.device(dev)
-    return here, stream
+    for t in tensors:
+        if t is not None:
+            d = t.get_device()
+            if d != dev:
+                if d < 0 or dev is not None:
+                    raise TypeError("all tensors must be on one CUDA device, not on "
+                                    + ", ".join(sorted({str(x.device) for x in tensors if x is not None})))
+                dev = d
+    return dev
 
 
-def _rows3(t: torch.Tensor, name: str):
+@contextlib.contextmanager
+def _on(dev: int, stream):
+    """The tensors' device is the current one, and `stream` its current stream (also what new tensors belong to)."""
+    with torch.cuda.device(dev):
+        if stream is None:
+            yield
+            return
+        if not hasattr(stream, "cuda_stream"):
+            stream = torch.cuda.ExternalStream(int(stream), device=dev)
+        if stream.device.index != dev:
+            raise ValueError(f"the stream belongs to {stream.device}, the tensors are on device {dev}")
+        with torch.cuda.stream(stream):
+            yield
+
+
+def _elsewhere(dev: int, stream) -> bool:
+    return stream is not None or _current_device() != dev
+
+
+def _stream_of(dev: int) -> int:
+    return _raw_stream(dev) if _raw_stream else torch.cuda.current_stream(dev).cuda_stream
+
+
+def _rows3(t: torch.Tensor, name: str, shape):
     """Pointer and strides of a tensor of rows of heads (a stride that is never taken counts as 0)."""
-    if t.dim() != 3 or (t.shape[2] > 1 and t.stride(2) != 1):
-        raise TypeError(f"{name} must be [rows][heads][head_dim] with contiguous head rows")
-    if t.dtype not in _DTYPES:
+    st = t.stride()
+    if len(st) != 3 or t.shape != shape or (st[2] != 1 and shape[2] > 1):
+        raise ValueError(f"{name} must be {list(shape)} ([rows][heads][head_dim]) with contiguous head rows")
+    return t.data_ptr(), st[0] if shape[0] > 1 else 0, st[1] if shape[1] > 1 else 0
+
+
+def _dtype(t: torch.Tensor, name: str) -> int:
+    d = _DTYPES.get(t.dtype)
+    if d is None:
         raise TypeError(f"{name} must be float32 or bfloat16")
-    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else 0, t.stride(1) if t.shape[1] > 1 else 0
+    return d
 
 
 def _vec(t: Optional[torch.Tensor], name: str, dtype, n: int):
@@ -683,7 +709,7 @@ class Pages:
     may be changed in place between calls."""
 
     def __init__(self, k: torch.Tensor, v: torch.Tensor, table: torch.Tensor, length: torch.Tensor):
-        _place((("k", k), ("v", v), ("table", table), ("length", length)), None)
+        self.device = _device_of((k, v, table, length))
         if k.dim() != 4 or k.shape != v.shape or k.dtype != v.dtype or k.dtype not in _DTYPES:
             raise TypeError("k and v must be [n_pages][n_kv_heads][page_size][head_dim] of one type, float32 or bfloat16")
         if k.stride(3) != 1 or v.stride(3) != 1:
@@ -697,6 +723,7 @@ class Pages:
         self.c = cs_pages(k.data_ptr(), v.data_ptr(), *st[0], *st[1], table.data_ptr(),
                           table.stride(0) if table.shape[0] > 1 else table.shape[1], length.data_ptr(), table.shape[0],
                           table.shape[1], k.shape[0], k.shape[2], k.shape[1], k.shape[3], _DTYPES[k.dtype], 0)
+        self.ref = C.byref(self.c)
 
     def _row0(self, row0: Optional[torch.Tensor]):
         return _vec(row0, "row0", torch.int32, self.table.shape[0] + 1)
@@ -709,47 +736,66 @@ def cs_op_qk_norm_rope(q: torch.Tensor, k: Optional[torch.Tensor] = None, pos: O
     """q [R][H][hd], k [R][KVH][hd] or None: RMSNorm of every head (a gain of None: no norm) and rotation by
     pos[r] * inv_freq[j] (float64 [rot/2]; None: no rotation).  Returns (q, k) rows in new tensors, or in
     out = (q_out, k_out), which may be the inputs."""
-    here, st = _place((("q", q), ("k", k), ("pos", pos), ("inv_freq", inv_freq), ("q_gain", q_gain), ("k_gain", k_gain))
-                      + (() if out is None else (("out[0]", out[0]), ("out[1]", out[1]))), stream)
-    qp = _rows3(q, "q")
-    R, H, hd = q.shape
-    kp, KVH = (None, 0, 0), 0
-    if k is not None:
-        kp, KVH = _rows3(k, "k"), k.shape[1]
-        if k.shape[0] != R or k.shape[2] != hd or k.dtype != q.dtype:
-            raise ValueError("q and k must have the same rows, head_dim and type")
+    qo, ko = out if out is not None else (None, None)
+    dev = _device_of((q, k, pos, inv_freq, q_gain, k_gain, qo, ko))
+    if _elsewhere(dev, stream):
+        with _on(dev, stream):
+            return cs_op_qk_norm_rope(q, k, pos, inv_freq, q_gain, k_gain, eps, out_dtype, out)
+    qs = q.shape
+    dt, qp = _dtype(q, "q"), _rows3(q, "q", qs)
+    R, H, hd = qs
     rot = 0 if inv_freq is None else 2 * inv_freq.numel()
     if rot and pos is None:
         raise ValueError("a rotation needs positions")
-    with here, (torch.cuda.stream(st) if st is not None else contextlib.nullcontext()):
-        if out is None:
-            dt = out_dtype or q.dtype
-            out = (torch.empty((R, H, hd), dtype=dt, device=q.device),
-                   None if k is None else torch.empty((R, KVH, hd), dtype=dt, device=q.device))
-        qo, ko = out
-        if qo.shape != q.shape or (k is not None and (ko is None or ko.shape != k.shape or ko.dtype != qo.dtype)) \
-                or (out_dtype is not None and qo.dtype != out_dtype):
-            raise ValueError("out must be (q_out, k_out) in the shapes of q and k and of one type")
-        qop, kop = _rows3(qo, "out[0]"), (None, 0, 0) if k is None else _rows3(ko, "out[1]")
-        _check(load_library().cs_op_qk_norm_rope(
-            _DTYPES[q.dtype], _DTYPES[qo.dtype], *qp, *kp, R, H, KVH, hd, _vec(q_gain, "q_gain", torch.float32, hd),
-            _vec(k_gain, "k_gain", torch.float32, hd), eps, _vec(pos, "pos", torch.int32, R),
-            _vec(inv_freq, "inv_freq", torch.float64, rot // 2), rot, *qop, *kop, _stream(None)))
-    return out
+    odt = out_dtype or (q.dtype if qo is None else qo.dtype)
+    if qo is None:
+        qo = q.new_empty(qs, dtype=odt)
+    kp, kop, KVH = (None, 0, 0), (None, 0, 0), 0
+    if k is not None:
+        ks = k.shape
+        if len(ks) != 3 or ks[0] != R or ks[2] != hd or k.dtype != q.dtype:
+            raise ValueError("q and k must have the same rows, head_dim and type")
+        KVH = ks[1]
+        if ko is None:
+            if out is not None:
+                raise ValueError("out must be (q_out, k_out)")
+            ko = q.new_empty(ks, dtype=odt)
+        kp, kop = _rows3(k, "k", ks), _rows3(ko, "k_out", ks)
+        if ko.dtype != odt:
+            raise TypeError("q_out and k_out must be of one type, out_dtype if that is given")
+    if qo.dtype != odt:
+        raise TypeError("q_out and k_out must be of one type, out_dtype if that is given")
+    _check(load_library().cs_op_qk_norm_rope(
+        dt, _dtype(qo, "q_out"), *qp, *kp, R, H, KVH, hd, _vec(q_gain, "q_gain", torch.float32, hd),
+        _vec(k_gain, "k_gain", torch.float32, hd), eps, _vec(pos, "pos", torch.int32, R),
+        _vec(inv_freq, "inv_freq", torch.float64, rot // 2), rot, *_rows3(qo, "q_out", qs), *kop, _stream_of(dev)))
+    return qo, ko
 
 
 def cs_paged_append(pages: Pages, k: torch.Tensor, v: torch.Tensor, row0: Optional[torch.Tensor] = None,
                     inv_freq: Optional[torch.Tensor] = None, stream=None):
     """New rows k, v [R][KVH][hd] into the pages of their streams, at positions length[b] + i; keys are rotated on the way
     if inv_freq (float64 [rot/2]) is given.  row0: int32 [batch + 1] offsets of the streams' rows, None: equal shares."""
-    here, st = _place((("pages", pages.k), ("k", k), ("v", v), ("row0", row0), ("inv_freq", inv_freq)), stream)
-    if k.shape != v.shape or k.dtype != v.dtype or k.dim() != 3 or tuple(k.shape[1:]) != (pages.c.n_kv_heads, pages.c.head_dim):
-        raise ValueError("k and v must be [rows][n_kv_heads][head_dim] of one type")
+    dev = _device_of((pages.k, k, v, row0, inv_freq))
+    if _elsewhere(dev, stream):
+        with _on(dev, stream):
+            return cs_paged_append(pages, k, v, row0, inv_freq)
+    R, c = k.shape[0], pages.c
+    want = (R, c.n_kv_heads, c.head_dim)
+    dt = _dtype(k, "k")
+    if v.dtype != k.dtype:
+        raise TypeError("k and v must be of one type")
     rot = 0 if inv_freq is None else 2 * inv_freq.numel()
-    with here, (torch.cuda.stream(st) if st is not None else contextlib.nullcontext()):
-        _check(load_library().cs_paged_append(C.byref(pages.c), _DTYPES.get(k.dtype, -1), *_rows3(k, "k"), *_rows3(v, "v"),
-                                              pages._row0(row0), k.shape[0], _vec(inv_freq, "inv_freq", torch.float64, rot // 2),
-                                              rot, _stream(None)))
+    _check(load_library().cs_paged_append(pages.ref, dt, *_rows3(k, "k", want), *_rows3(v, "v", want), pages._row0(row0), R,
+                                          _vec(inv_freq, "inv_freq", torch.float64, rot // 2), rot, _stream_of(dev)))
+
+
+def cs_paged_attention_workspace(pages: Pages, n_heads: int, R: int, row0: bool = False, max_rows: int = 0, max_len: int = 0) -> int:
+    """Bytes that cs_paged_attention needs for these arguments (row0: whether it is given offsets)."""
+    need = load_library().cs_paged_attention_workspace(pages.ref, n_heads, 1 if row0 else 0, R, max_rows, max_len)
+    if need < 0:
+        _check(need)
+    return need
 
 
 def cs_paged_attention(pages: Pages, q: torch.Tensor, row0: Optional[torch.Tensor] = None, scale: Optional[float] = None,
@@ -757,29 +803,31 @@ def cs_paged_attention(pages: Pages, q: torch.Tensor, row0: Optional[torch.Tenso
                        workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """q [R][H][hd] of the cache's type, rotated.  Returns [R][H][hd] (in `out` if given, which may be q; rows behind the last
     stream are left as they were).  scale: 1/sqrt(head_dim) by default.  max_rows, max_len: hints, see copyspec.h.
-    workspace: uint8 tensor of at least the size that cs_paged_attention_workspace asks for; by default one is allocated
+    workspace: a contiguous tensor of at least the size that cs_paged_attention_workspace gives; by default one is allocated
     for the call."""
-    here, st = _place((("pages", pages.k), ("q", q), ("row0", row0), ("out", out), ("workspace", workspace)), stream)
-    if q.dtype != pages.dtype:
-        raise TypeError(f"q must have the cache's type, {pages.dtype}")
-    qp = _rows3(q, "q")
-    R, H, hd = q.shape
-    if hd != pages.c.head_dim:
-        raise ValueError("q must have the cache's head_dim")
+    dev = _device_of((pages.k, q, row0, out, workspace))
+    if _elsewhere(dev, stream):
+        with _on(dev, stream):
+            return cs_paged_attention(pages, q, row0, scale, window, max_rows, max_len, out, workspace)
+    qs, c = q.shape, pages.c
+    qp = _rows3(q, "q", qs)
+    R, H, hd = qs
+    if q.dtype != pages.dtype or hd != c.head_dim:
+        raise TypeError(f"q must have the cache's type and head_dim, {pages.dtype} and {c.head_dim}")
+    if out is None:
+        out = q.new_empty(qs)
+    elif out.dtype != q.dtype:
+        raise TypeError("out must have the type of q")
     lib, r0 = load_library(), pages._row0(row0)
-    with here, (torch.cuda.stream(st) if st is not None else contextlib.nullcontext()):
-        if out is None:
-            out = torch.empty((R, H, hd), dtype=q.dtype, device=q.device)
-        elif out.shape != q.shape or out.dtype != q.dtype:
-            raise ValueError("out must have the shape and type of q")
-        need = lib.cs_paged_attention_workspace(C.byref(pages.c), H, 1 if r0 else 0, R, max_rows, max_len)
-        if need < 0:
-            _check(need)
-        if workspace is None and need > 0:
+    if workspace is None:
+        need = cs_paged_attention_workspace(pages, H, R, r0 is not None, max_rows, max_len)
+        if need > 0:
             workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
-        _check(lib.cs_paged_attention(C.byref(pages.c), *qp, H, r0, R, 1.0 / math.sqrt(hd) if scale is None else scale, window,
-                                      max_rows, max_len, *_rows3(out, "out"), _ptr(workspace),
-                                      0 if workspace is None else workspace.numel() * workspace.element_size(), _stream(None)))
+    elif not workspace.is_contiguous():
+        raise ValueError("workspace must be contiguous")
+    _check(lib.cs_paged_attention(pages.ref, *qp, H, r0, R, 1.0 / math.sqrt(hd) if scale is None else scale, window,
+                                  max_rows, max_len, *_rows3(out, "out", qs), _ptr(workspace),
+                                  0 if workspace is None else workspace.numel() * workspace.element_size(), _stream_of(dev)))
     return out
 
 

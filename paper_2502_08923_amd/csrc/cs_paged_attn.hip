@@ -28,13 +28,12 @@ struct pa_tile {
 };
 struct pa_plan {
     int TR, qr_lo, qr_hi;
-    int nsplit, nsplit_all;   // token ranges of this launch, and of the workspace
+    int nsplit;               // token ranges
     int chunk;                // tokens of a range; the last one takes what is left
     int tiles_per;            // tiles of a stream where all have the same rows, else 0
-    float* po;                // [nsplit_all][R][H][hd] partial outputs
-    float2* pml;              // [nsplit_all][R][H] (maximum, sum); sum < 0 in range 0: the output is there already
+    float* po;                // [nsplit][R][H][hd] partial outputs
+    float2* pml;              // [nsplit][R][H] their (maximum, sum)
 };
-#define PA_DONE (-1.0f)
 
 __device__ __forceinline__ bool pa_find_tile(const cs_pages_dev& D, int G, const pa_plan& P, int tile, pa_tile& o) {
     int b = -1, k = 0;
@@ -115,16 +114,11 @@ __device__ __forceinline__ void pa_finish(const cs_pages_dev& D, const pa_args& 
         if (P.nsplit == 1) {
             const float inv = l > 0.f ? 1.0f / l : 0.f;           // a row that sees nothing: 0
             if (d < hd) pa_store4((T_*)A.out + r * A.out_row + h * A.out_head + d, o * inv);
-            if (P.nsplit_all > 1 && d == 0) P.pml[rh] = make_float2(0.f, PA_DONE);
             continue;
         }
         const int64_t at = (int64_t)split * D.R * A.H + rh;
         if (d < hd) *reinterpret_cast<f32x4*>(P.po + at * hd + d) = o;
-        if (d == 0) {
-            P.pml[at] = make_float2(M, l);
-            if (split == 0)
-                for (int s = P.nsplit; s < P.nsplit_all; ++s) P.pml[(int64_t)s * D.R * A.H + rh] = make_float2(-INFINITY, 0.f);
-        }
+        if (d == 0) P.pml[at] = make_float2(M, l);
     }
 }
 
@@ -156,10 +150,9 @@ __global__ __launch_bounds__(64 * PN_WAVES) void k_paged_narrow(cs_pages_dev D, 
     __shared__ __attribute__((aligned(16))) unsigned char smem[MERGE_BYTES > Q_BYTES ? MERGE_BYTES : Q_BYTES];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int c = lane & 15, g = lane >> 4;
-    const int split = blockIdx.x % P.nsplit, item = blockIdx.x / P.nsplit;
-    const int KVH = D.p.n_kv_heads, kvh = item % KVH;
+    const int KVH = D.p.n_kv_heads, kvh = blockIdx.x % KVH, rest = blockIdx.x / KVH, split = rest % P.nsplit;
     pa_tile T;
-    if (!pa_find_tile(D, A.G, P, item / KVH, T)) return;
+    if (!pa_find_tile(D, A.G, P, rest / P.nsplit, T)) return;
     const int hd = D.p.head_dim;
     const int n_rows = min(ROWS, T.QR - T.n0);          // live query rows of the tile
     const int i_lo = T.n0 / A.G, i_hi = (T.n0 + n_rows - 1) / A.G;
@@ -409,6 +402,15 @@ __global__ __launch_bounds__(64 * PN_WAVES) void k_paged_narrow(cs_pages_dev D, 
     pa_finish<PN_WAVES, HD, ROWS, bf16_t>(D, A, P, T, kvh, split, n_rows, s_o, s_ml, tid, 64 * PN_WAVES);
 }
 
+// As cs_load_to_lds, where the base comes straight from a lane: five wait states lie between a v_readlane and the load that takes
+// its address from the result.
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+__device__ __forceinline__ void cs_load_to_lds_lane(unsigned voff, const void* sbase, unsigned lds_addr) {
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(voff), "s"(sbase), "s"(lds_addr) : "m0");
+}
+#pragma clang diagnostic pop
+
 // ---- many query rows: the matrix cores and the vector unit are the bound -----------------------------
 // Eight waves have 16 * NT query rows each and walk the tokens together: every 32-token block goes once from its pages to LDS and
 // serves all of them.  Each wave requests its share of a block (1 KB pieces, direct to LDS) into a ring of stages, so several
@@ -425,7 +427,7 @@ __global__ __launch_bounds__(64 * PW_WAVES) void k_paged_wide(cs_pages_dev D, pa
     constexpr int WROWS = 16 * NT, TR = PW_WAVES * WROWS;
     constexpr int NLOAD = 4 * KS, LD = NLOAD / PW_WAVES;       // pieces of a block; per wave
     constexpr int STAGE_BYTES = NLOAD * 1024, V_AT = 2 * KS * 1024;
-    constexpr int STAGES = HD == 256 ? 4 : 6;
+    constexpr int STAGES = HD == 256 ? 5 : 8;
     static_assert(NLOAD % PW_WAVES == 0 && STAGES * STAGE_BYTES <= 160 * 1024, "every wave the same number of requests; LDS");
     __shared__ __attribute__((aligned(16))) unsigned char stage[STAGES][STAGE_BYTES];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -464,52 +466,56 @@ __global__ __launch_bounds__(64 * PW_WAVES) void k_paged_wide(cs_pages_dev D, pa
 
     // this wave's pieces: id = wave + 8u; below 2*KS keys (half id / KS, features 32 * (id % KS) ..), above values likewise.  Features that the
     // head does not have are read at feature 0: their query elements are 0, their outputs are not stored.
-    const char* pool[LD];
-    int64_t page_bytes[LD];
-    unsigned voff[LD], ts[LD];
-    int half[LD];
+    unsigned voff[LD];
 #pragma unroll
     for (int u = 0; u < LD; ++u) {
-        const int id = wave + PW_WAVES * u, v = id >= 2 * KS, x = (id - v * 2 * KS) % KS;
-        half[u] = (id - v * 2 * KS) / KS;
-        pool[u] = v ? (const char*)((const bf16_t*)D.p.v + kvh * D.p.v_head) : (const char*)((const bf16_t*)D.p.k + kvh * D.p.k_head);
-        page_bytes[u] = (v ? D.p.v_page : D.p.k_page) * 2;
-        ts[u] = (unsigned)(v ? D.p.v_token : D.p.k_token) * 2;
+        const int id = wave + PW_WAVES * u, v = id >= 2 * KS, x = id % KS;
         const int token = v ? (lane & 31) >> 1 : c;
         const int feature = x * 32 + (v ? (lane >> 5) * 16 + (lane & 1) * 8 : g * 8);
-        voff[u] = token * ts[u] + (feature < hd ? feature * 2 : 0);
+        voff[u] = token * (unsigned)(v ? D.p.v_token : D.p.k_token) * 2 + (feature < hd ? feature * 2 : 0);
     }
     const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)&stage[0][0];
 
-    // pages of 64 blocks, one per lane; a half whose page does not exist is read from page 0 and masked
+    // A lane has one of the next 64 blocks: where in the pool each of the wave's pieces of it starts, so that a request costs the scalar
+    // unit no multiplication.  A half whose page does not exist is read from page 0 and masked.
     const int32_t* tab = D.p.table + T.b * D.p.table_stride;
-    int page0 = 0, page1 = 0;
-    unsigned long long ok[2] = {0, 0}, ok_old[2] = {0, 0};
+    unsigned from_lo[LD], from_hi[LD];
+    unsigned long long okay0 = 0, okay1 = 0, old0 = 0, old1 = 0;     // halves that exist, of these and of the 64 blocks before
     auto pages = [&](int blk0) {
         const int64_t t = (int64_t)w_begin + 32 * ((int64_t)blk0 + lane);
-        int a = -1, b = -1;
+        int page0 = -1, page1 = -1;
         if (t < t_end) {
-            a = tab[t >> D.page_log2];
+            page0 = tab[t >> D.page_log2];
             const int e = (int)((t + 16) >> D.page_log2);
-            b = e < D.p.table_pages ? tab[e] : -1;
+            page1 = e < D.p.table_pages ? tab[e] : -1;
         }
-        const bool oa = (unsigned)a < (unsigned)D.p.n_pages, ob = (unsigned)b < (unsigned)D.p.n_pages;
-        page0 = oa ? a : 0;
-        page1 = ob ? b : 0;
-        ok_old[0] = ok[0], ok_old[1] = ok[1];
-        ok[0] = __ballot(oa), ok[1] = __ballot(ob);
-    };
-    auto issue = [&](int blk, int st) {
-        const int t0 = w_begin + blk * 32;
+        const bool ok0 = (unsigned)page0 < (unsigned)D.p.n_pages, ok1 = (unsigned)page1 < (unsigned)D.p.n_pages;
+        old0 = okay0, old1 = okay1;
+        okay0 = __ballot(ok0), okay1 = __ballot(ok1);
 #pragma unroll
         for (int u = 0; u < LD; ++u) {
-            const int page = __builtin_amdgcn_readlane(half[u] ? page1 : page0, blk & 63);
-            const int slot = (t0 + 16 * half[u]) & (D.p.page_size - 1);
-            cs_load_to_lds(voff[u], pool[u] + page * page_bytes[u] + (int64_t)slot * ts[u], lds0 + st * STAGE_BYTES + (wave + PW_WAVES * u) * 1024);
+            const int id = wave + PW_WAVES * u, v = id >= 2 * KS, half = id / KS & 1;
+            const int page = half ? (ok1 ? page1 : 0) : (ok0 ? page0 : 0), slot = (int)(t + 16 * half) & (D.p.page_size - 1);
+            const int64_t at = v ? page * D.p.v_page + kvh * D.p.v_head + slot * D.p.v_token : page * D.p.k_page + kvh * D.p.k_head + slot * D.p.k_token;
+            const uint64_t from = (uint64_t)(v ? D.p.v : D.p.k) + 2 * at;
+            from_lo[u] = (unsigned)from;
+            from_hi[u] = (unsigned)(from >> 32);
         }
     };
-    // at most `n` of this wave's requests still in flight, then meet the other waves
-#define PW_SYNC(n) asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(n) : "memory")
+    auto issue = [&](int blk, int st) {
+#pragma unroll
+        for (int u = 0; u < LD; ++u) {
+            const uint64_t from = (uint64_t)(unsigned)__builtin_amdgcn_readlane((int)from_hi[u], blk & 63) << 32 | (unsigned)__builtin_amdgcn_readlane((int)from_lo[u], blk & 63);
+            cs_load_to_lds_lane(voff[u], (const void*)from, lds0 + st * STAGE_BYTES + (wave + PW_WAVES * u) * 1024);
+        }
+    };
+    // At most INFLIGHT of this wave's requests still in flight, then meet the other waves.  The two waves of a SIMD meet them at different
+    // points of a block: the first four behind it, the others between scores and softmax, so that one wave of every SIMD has the
+    // matrix unit while the other has the vector unit.  (One statement: see cs_load_to_lds_if.)
+    constexpr int INFLIGHT = LD * (STAGES - 3);
+    const int team = wave / (PW_WAVES / 2);
+#define PW_SYNC(on) \
+    asm volatile("s_cmp_eq_u32 %1, 0\n\ts_cbranch_scc1 .Lno%=\n\ts_waitcnt vmcnt(%0)\n\ts_barrier\n.Lno%=:" ::"n"(INFLIGHT), "s"(on) : "memory", "scc")
 
     f32x4 oacc[MT][NT], lacc[NT];
     float m_run[NT], thr[NT];
@@ -530,6 +536,7 @@ __global__ __launch_bounds__(64 * PW_WAVES) void k_paged_wide(cs_pages_dev D, pa
     auto scores = [&](const unsigned char* sp, f32x4 (&sacc)[2][NT]) {
         auto k_frag = [&](int a, int s) { return *reinterpret_cast<const bf16x8*>(sp + ((a * KS + s) * 64 + lane) * 16); };
         bf16x8 k0 = k_frag(0, 0), k1 = k_frag(1, 0);
+        __builtin_amdgcn_s_setprio(1);
 #pragma unroll
         for (int s = 0; s < KS; ++s) {
             bf16x8 m0 = k0, m1 = k1;
@@ -547,6 +554,7 @@ __global__ __launch_bounds__(64 * PW_WAVES) void k_paged_wide(cs_pages_dev D, pa
             k0 = m0;
             k1 = m1;
         }
+        __builtin_amdgcn_s_setprio(0);
     };
     // the running maximum of the tile rows moves (and O is rescaled) only when it is left behind by 2^8
     auto reference = [&](const f32x4 (&sacc)[2][NT], bool masked) {
@@ -626,6 +634,7 @@ __global__ __launch_bounds__(64 * PW_WAVES) void k_paged_wide(cs_pages_dev D, pa
             }
             return __builtin_bit_cast(bf16x8, (s16x8){h[0][0], h[0][1], h[0][2], h[0][3], h[1][0], h[1][1], h[1][2], h[1][3]});
         };
+        __builtin_amdgcn_s_setprio(1);
 #pragma unroll
         for (int mt = 0; mt < 3; ++mt) vf[mt] = v_frag(mt);
 #pragma unroll
@@ -638,16 +647,16 @@ __global__ __launch_bounds__(64 * PW_WAVES) void k_paged_wide(cs_pages_dev D, pa
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) lacc[nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pb[nt], lacc[nt], 0, 0, 0);
         __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_setprio(0);
     };
 
-    // Blocks 0 .. STAGES-2 are requested up front; round i requests block i + STAGES - 1 into the stage that block i - 1 has left,
-    // works on block i, and ends when block i + 1 has landed in every wave's share.
-    constexpr int INFLIGHT = LD * (STAGES - 2);
+    // Blocks 0 .. STAGES-3 are requested up front; round i requests block i + STAGES - 2 into the stage of block i - 2, whose values the second
+    // team has read before the meeting behind its scores of block i - 1.  Behind round i's meeting block i + 1 is there.
     pages(0);
 #pragma unroll
-    for (int j = 0; j < STAGES - 1; ++j) issue(j, j);         // (past the last block: page 0, into a stage that nobody reads)
-    PW_SYNC(INFLIGHT);
-    int st_cur = 0, st_req = STAGES - 1;
+    for (int j = 0; j < STAGES - 2; ++j) issue(j, j);         // (past the last block: page 0, into a stage that nobody reads)
+    PW_SYNC(1);
+    int st_cur = 0, st_req = STAGES - 2;
     // The loop's bound and the position come from a vector register that the compiler cannot see through: around branches it
     // takes for uniform it splits the live ranges of the accumulators, copies and spills them.
     int vzero;
@@ -664,21 +673,24 @@ __global__ __launch_bounds__(64 * PW_WAVES) void k_paged_wide(cs_pages_dev D, pa
     const std::integral_constant<bool, true> masked_tag;
     f32x4 sa[2][NT];
     for (int i = 0; i < nblocks_v; ++i) {
-        const int ahead = i + STAGES - 1;
+        const int ahead = i + STAGES - 2;
         if ((ahead & 63) == 0) pages(ahead);
         issue(ahead, st_req);
         st_req = st_req + 1 == STAGES ? 0 : st_req + 1;
         const int t0 = w_begin + i * 32;
-        const bool newer = (ahead >> 6) == (i >> 6);
-        const int ok0 = (int)((newer ? ok[0] : ok_old[0]) >> (i & 63)) & 1, ok1 = (int)((newer ? ok[1] : ok_old[1]) >> (i & 63)) & 1;
-        const int gone = 1 - (ok0 & ok1) + vzero;
-        if ((t0 <= p_end) & (t0 + 31 >= w_lo)) {
-            scores(stage[st_cur], sa);
-            if ((t0 + 31 > p_open) | (t0 < w_hi) | (gone != 0)) finish(sa, stage[st_cur], t0, masked_tag, ok0, ok1);
-            else finish(sa, stage[st_cur], t0, plain_tag, true, true);
+        const unsigned long long whole = (ahead >> 6) == (i >> 6) ? okay0 & okay1 : old0 & old1;
+        const int gone = 1 - ((int)(whole >> (i & 63)) & 1) + vzero;
+        const bool mine = (t0 <= p_end) & (t0 + 31 >= w_lo);
+        if (mine) scores(stage[st_cur], sa);
+        PW_SYNC(team);
+        if (mine) {
+            if ((t0 + 31 > p_open) | (t0 < w_hi) | (gone != 0)) {
+                const unsigned long long h0 = (ahead >> 6) == (i >> 6) ? okay0 : old0, h1 = (ahead >> 6) == (i >> 6) ? okay1 : old1;
+                finish(sa, stage[st_cur], t0, masked_tag, (int)(h0 >> (i & 63)) & 1, (int)(h1 >> (i & 63)) & 1);
+            } else finish(sa, stage[st_cur], t0, plain_tag, true, true);
         }
         st_cur = st_cur + 1 == STAGES ? 0 : st_cur + 1;
-        PW_SYNC(INFLIGHT);
+        PW_SYNC(1 - team);
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");          // surplus requests, before the LDS is given up
 #undef PW_SYNC
@@ -693,7 +705,6 @@ __global__ __launch_bounds__(64 * PW_WAVES) void k_paged_wide(cs_pages_dev D, pa
         const float l = lacc[nt][0];
         if (P.nsplit == 1) {
             const float inv = l > 0.f ? 1.0f / l : 0.f;
-            if (P.nsplit_all > 1 && g == 0) P.pml[rh] = make_float2(0.f, PA_DONE);
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt) {
                 const int d = mt * 16 + 4 * g;
@@ -702,11 +713,7 @@ __global__ __launch_bounds__(64 * PW_WAVES) void k_paged_wide(cs_pages_dev D, pa
             continue;
         }
         const int64_t at = (int64_t)split * D.R * A.H + rh;
-        if (g == 0) {
-            P.pml[at] = make_float2(m_run[nt], l);
-            if (split == 0)
-                for (int s = P.nsplit; s < P.nsplit_all; ++s) P.pml[(int64_t)s * D.R * A.H + rh] = make_float2(-INFINITY, 0.f);
-        }
+        if (g == 0) P.pml[at] = make_float2(m_run[nt], l);
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
             const int d = mt * 16 + 4 * g;
@@ -724,7 +731,7 @@ __global__ __launch_bounds__(64 * PW_WAVES) void k_paged_wide(cs_pages_dev D, pa
 // of its own, and what bounds it is the instruction's rate, 157 TFLOP/s, the re-read blocks coming out of the caches).
 #define PF_WAVES 4
 template <int HD, int NT, bool TOKENS>
-__global__ __launch_bounds__(64 * PF_WAVES) void k_paged_f32(cs_pages_dev D, pa_args A, pa_plan P) {
+__global__ __launch_bounds__(64 * PF_WAVES, !TOKENS && HD <= 128 ? 2 : 1) void k_paged_f32(cs_pages_dev D, pa_args A, pa_plan P) {
     constexpr int KL = HD / 16, VX = HD / 64, MT = HD / 16;
     constexpr int WROWS = 16 * NT, TR = TOKENS ? WROWS : PF_WAVES * WROWS, OROW = HD + 4, QROW = HD + 4;
     constexpr int MERGE_FLOATS = TOKENS ? PF_WAVES * WROWS * (OROW + 2) : 0, Q_FLOATS = TR * QROW;
@@ -841,7 +848,7 @@ __global__ __launch_bounds__(64 * PF_WAVES) void k_paged_f32(cs_pages_dev D, pa_
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) sacc[nt] += odd[nt];
             __builtin_amdgcn_sched_barrier(0);
-            ldk(kb, i + 2);
+            ldk(kb, i + (TOKENS ? 2 : 1));
             __builtin_amdgcn_sched_barrier(0);
             const int t0 = at(i), page = page_of(i);
             if (t0 < open_lo || t0 + 16 > open_hi || page < 0) {
@@ -887,13 +894,23 @@ __global__ __launch_bounds__(64 * PF_WAVES) void k_paged_f32(cs_pages_dev D, pa_
 #pragma unroll
                         for (int nt = 0; nt < NT; ++nt)
                             oacc[x * 4 + u][nt] = __builtin_amdgcn_mfma_f32_16x16x4f32(vb[j][x][u], sacc[nt][j], oacc[x * 4 + u][nt], 0, 0, 0);
+            if constexpr (!TOKENS) {
+                __builtin_amdgcn_sched_barrier(0);
+                ldv(vb, i + 1);
+                __builtin_amdgcn_sched_barrier(0);
+            }
         };
-        f32x4 k0[KL], k1[KL], v0[4][VX], v1[4][VX];
+        f32x4 k0[KL], v0[4][VX];
         __builtin_amdgcn_sched_barrier(0);
         ldk(k0, 0);
         __builtin_amdgcn_sched_barrier(0);
         ldv(v0, 0);
         __builtin_amdgcn_sched_barrier(0);
+        if constexpr (!TOKENS) {                        // either product covers the loads for the other: one buffer each
+            for (int i = 0; i < n_all; ++i) block(k0, v0, i);
+            continue;
+        }
+        f32x4 k1[KL], v1[4][VX];
         ldk(k1, 1);
         __builtin_amdgcn_sched_barrier(0);
         int i = 0;
@@ -939,12 +956,7 @@ __global__ __launch_bounds__(64 * PF_WAVES) void k_paged_f32(cs_pages_dev D, pa_
             const int64_t r = T.row0 + i, rh = r * A.H + h, at = (int64_t)split * D.R * A.H + rh;
             const bool whole = P.nsplit == 1;
             const float inv = l_run[nt] > 0.f ? 1.0f / l_run[nt] : 0.f;
-            if (g == 0) {
-                if (!whole) P.pml[at] = make_float2(m_run[nt], l_run[nt]);
-                else if (P.nsplit_all > 1) P.pml[rh] = make_float2(0.f, PA_DONE);
-                if (!whole && split == 0)
-                    for (int s = P.nsplit; s < P.nsplit_all; ++s) P.pml[(int64_t)s * D.R * A.H + rh] = make_float2(-INFINITY, 0.f);
-            }
+            if (g == 0 && !whole) P.pml[at] = make_float2(m_run[nt], l_run[nt]);
 #pragma unroll
             for (int x = 0; x < VX; ++x)
 #pragma unroll
@@ -960,42 +972,44 @@ __global__ __launch_bounds__(64 * PF_WAVES) void k_paged_f32(cs_pages_dev D, pa_
 }
 
 // ---- joining token ranges ---------------------------------------------------------------------
-// out[r][h] = sum_s 2^(m_s - M) O_s / sum_s 2^(m_s - M) l_s.  2^lanes_log2 lanes have a row's hd features, four each; a lane reads
-// the (max, sum) pairs of every lanes-th range, and the weights go round by shuffles.
-template <typename T>
-__global__ __launch_bounds__(256) void k_paged_merge(const float* __restrict__ po, const float2* __restrict__ pml, int nsplit, int64_t n_rh, int H,
-                                                     int hd, int lanes_log2, const int32_t* __restrict__ row0_end, T* __restrict__ out,
-                                                     int64_t out_row, int64_t out_head) {
+// out[r][h] = sum_s 2^(m_s - M) O_s / sum_s 2^(m_s - M) l_s.  2^lanes_log2 lanes have a query row's hd features, four each; a lane
+// reads the (max, sum) pairs of every lanes-th range, and the weights go round by shuffles.  A workgroup has 256 >> lanes_log2 query
+// rows of a tile, the same tiles as the kernel before it: rows that had no launch, or went without ranges, are not touched.
+#define PM_THREADS 256
+template <typename T_>
+__global__ __launch_bounds__(PM_THREADS) void k_paged_merge(cs_pages_dev D, pa_args A, pa_plan P, int lanes_log2, int groups) {
+    const int KVH = D.p.n_kv_heads, group = blockIdx.x % groups, item = blockIdx.x / groups, kvh = item % KVH;
     const int lanes = 1 << lanes_log2, sub = threadIdx.x & (lanes - 1), d = sub * 4;
-    const int64_t rh = (int64_t)blockIdx.x * (256 >> lanes_log2) + (threadIdx.x >> lanes_log2);
-    if (rh >= n_rh) return;
-    const int r = (int)(rh / H), h = (int)(rh % H);
-    if (row0_end && r >= *row0_end) return;                       // behind the last stream
-    if (pml[rh].y < 0.f) return;                                  // written by the kernel itself
+    const int n = group * (PM_THREADS >> lanes_log2) + (threadIdx.x >> lanes_log2);
+    pa_tile T;
+    if (!pa_find_tile(D, A.G, P, item / KVH, T)) return;
+    if (n >= P.TR || T.n0 + n >= T.QR) return;
+    const int i = (T.n0 + n) / A.G, h = kvh * A.G + T.n0 + n - i * A.G, hd = D.p.head_dim;
+    const int64_t r = T.row0 + i, rh = r * A.H + h, n_rh = (int64_t)D.R * A.H;
     float M = -INFINITY;
-    for (int s = sub; s < nsplit; s += lanes) M = fmaxf(M, pml[s * n_rh + rh].x);
+    for (int s = sub; s < P.nsplit; s += lanes) M = fmaxf(M, P.pml[s * n_rh + rh].x);
     for (int o = lanes >> 1; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor(M, o, 64));
     const float Ms = M == -INFINITY ? 0.f : M;
     f32x4 acc = (f32x4){0.f, 0.f, 0.f, 0.f};
     float l = 0.f;
-    for (int s0 = 0; s0 < nsplit; s0 += lanes) {
+    for (int s0 = 0; s0 < P.nsplit; s0 += lanes) {
         float2 ml = make_float2(-INFINITY, 0.f);
-        if (s0 + sub < nsplit) ml = pml[(s0 + sub) * n_rh + rh];
-        const float w = __builtin_amdgcn_exp2f(ml.x - Ms);
-        const float wl = w * ml.y;
-        const int n = min(lanes, nsplit - s0);
-        for (int s = 0; s < n; ++s) {
-            const int src = (threadIdx.x & 63 & ~(lanes - 1)) + s;
-            const float ws = __shfl(w, src, 64);
-            l += __shfl(wl, src, 64);
-            if (ws != 0.f && d < hd) acc += ws * *reinterpret_cast<const f32x4*>(po + ((s0 + s) * n_rh + rh) * hd + d);
-        }
+        if (s0 + sub < P.nsplit) ml = P.pml[(s0 + sub) * n_rh + rh];
+        const float w = __builtin_amdgcn_exp2f(ml.x - Ms), wl = w * ml.y;
+        const int ns = min(lanes, P.nsplit - s0);
+        const float* __restrict__ src = P.po + ((int64_t)s0 * n_rh + rh) * hd + min(d, hd - 4);
+        for (int s = 0; s < ns; s += 4)
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                // (past the last range: weight 0, its row once more; a range that saw nothing has stored zeros)
+                const int from = (threadIdx.x & 63 & ~(lanes - 1)) + min(s + u, ns - 1);
+                const float keep = s + u < ns ? 1.f : 0.f;
+                l += keep * __shfl(wl, from, 64);
+                acc += keep * __shfl(w, from, 64) * *reinterpret_cast<const f32x4*>(src + (int64_t)min(s + u, ns - 1) * n_rh * hd);
+            }
     }
     if (d >= hd) return;
-    const float inv = l > 0.f ? 1.0f / l : 0.f;
-    T* o = out + r * out_row + h * out_head + d;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) cs_st(o, j, acc[j] * inv);
+    pa_store4((T_*)A.out + r * A.out_row + h * A.out_head + d, acc * (l > 0.f ? 1.0f / l : 0.f));
 }
 
 // ---- entry points --------------------------------------------------------------------------
@@ -1016,14 +1030,27 @@ struct pa_part {
 struct pa_cut {
     int hdt;
     pa_part narrow, wide;
-    int room;                                                       // token ranges that the workspace holds
-    int64_t part_floats, bytes;
+    int64_t at_w, bytes;              // where the second launch's partial results start; bytes in all
 };
+static int64_t pa_part_bytes(int64_t nsplit, int64_t rh, int hd) { return nsplit > 1 ? cs_round_up(nsplit * rh * (hd * 4 + 8), 16) : 0; }
+#define PA_MOST_RANGES 256
 #define PN_MOST 48                // query rows up to which a stream takes the kernel of few rows
-static void pa_ranges(pa_part& t, int64_t span, int64_t items, int64_t want, int64_t min_chunk) {
-    const int64_t n = std::max<int64_t>(1, std::min<int64_t>(cs_ceil_div(want, items), span / min_chunk));
-    t.chunk = (int)cs_round_up(cs_ceil_div(span, n), 128);
-    t.nsplit = (int)cs_ceil_div(span, t.chunk);
+// Token ranges: as many as make the launch's rounds of the chip cheapest, a round costing what a range's tokens cost and, in the same unit,
+// what a workgroup's start and end cost; joining ranges costs a launch more.
+struct pa_cost {
+    int slots, start, join;           // workgroups that run at once; tokens' worth of a workgroup's ends, and of the merge
+};
+static void pa_ranges(pa_part& t, int64_t span, int64_t items, const pa_cost& k, int most) {
+    int64_t best = 0;
+    for (int n = 1; n <= most && (n == 1 || n * 64 <= span); ++n) {
+        const int64_t chunk = cs_round_up(cs_ceil_div(span, n), 32);
+        const int64_t cost = cs_ceil_div(items * n, k.slots) * (chunk + k.start) + (n > 1 ? k.join + n : 0);
+        if (n == 1 || cost < best) {
+            best = cost;
+            t.chunk = (int)chunk;
+            t.nsplit = (int)cs_ceil_div(span, chunk);
+        }
+    }
 }
 static pa_cut pa_make_cut(const cs_pages* p, int H, bool has_row0, int R, int max_rows, int64_t max_len, int window) {
     pa_cut c = {};
@@ -1035,7 +1062,9 @@ static pa_cut pa_make_cut(const cs_pages* p, int H, bool has_row0, int R, int ma
     const int64_t span = window ? std::min<int64_t>(len, (int64_t)window + rows + 32) : len;
     pa_part &N = c.narrow, &W = c.wide;
     const bool f32 = p->dtype == CS_F32;
-    const int n_most = c.hdt == 256 ? 16 : PN_MOST;
+    // Streams of up to n_most query rows per KV head go to the kernel of few rows.  Where a batch has longer ones too, that kernel is
+    // made for single tokens: a tile of 48 rows would cost every one of them three tiles' products.
+    const int n_most = c.hdt == 256 || qr > PN_MOST ? 16 : PN_MOST;
     if (has_row0 || qr <= n_most) {
         N.nt = (int)std::min<int64_t>(n_most / 16, cs_ceil_div(qr, 16));
         N.TR = 16 * N.nt;
@@ -1051,18 +1080,17 @@ static pa_cut pa_make_cut(const cs_pages* p, int H, bool has_row0, int R, int ma
         W.tiles_per = has_row0 ? 0 : (int)cs_ceil_div(qr, W.TR);
         W.tiles = has_row0 ? (int)(all / W.TR + std::min<int64_t>(B, all / (n_most + 1))) : B * W.tiles_per;
     }
-    if (N.tiles) pa_ranges(N, span, (int64_t)N.tiles * KVH, 1024, 256);
-    if (W.tiles) pa_ranges(W, span, (int64_t)W.tiles * KVH, 512, 512);
-    // (a window only takes ranges away)
-    pa_part n = N, w = W;
-    if (N.tiles) pa_ranges(n, len, (int64_t)N.tiles * KVH, 1024, 256);
-    if (W.tiles) pa_ranges(w, len, (int64_t)W.tiles * KVH, 512, 512);
-    c.room = std::max(std::max(n.nsplit, w.nsplit), std::max(N.nsplit, W.nsplit));
-    if (c.room > 1) {
-        const int64_t rh = (int64_t)R * H;
-        c.part_floats = cs_round_up(c.room * rh * p->head_dim, 4);
-        c.bytes = c.part_floats * 4 + c.room * rh * 8;
-    }
+    // the workspace is sized without a window, which is not given more ranges
+    const int64_t rh = (int64_t)R * H;
+    auto ranges = [&](pa_part& t, const pa_cost& k) -> int64_t {
+        if (!t.tiles) return 0;
+        pa_ranges(t, len, (int64_t)t.tiles * KVH, k, PA_MOST_RANGES);
+        const int64_t bytes = pa_part_bytes(t.nsplit, rh, p->head_dim);
+        if (span < len) pa_ranges(t, span, (int64_t)t.tiles * KVH, k, t.nsplit);
+        return bytes;
+    };
+    c.at_w = ranges(N, f32 ? pa_cost{256, 128, 384} : pa_cost{256, 256, 768});
+    c.bytes = c.at_w + ranges(W, f32 ? pa_cost{512, 16, 128} : pa_cost{256, 128, 192});
     return c;
 }
 
@@ -1091,8 +1119,20 @@ static int pw_launch(const cs_pages_dev& D, const pa_args& A, const pa_plan& P, 
     k_paged_wide<HD, NT><<<grid, 64 * PW_WAVES, 0, s>>>(D, A, P);
     return cs_launch_ok("k_paged_wide");
 }
-static pa_plan pa_plan_of(const pa_part& t, int nsplit_all, float* po, float2* pml) {
-    return {t.TR, t.qr_lo, t.qr_hi, t.nsplit, nsplit_all, t.chunk, t.tiles_per, po, pml};
+static pa_plan pa_plan_of(const pa_part& t, char* ws, int64_t rh, int hd) {
+    float* po = (float*)ws;
+    return {t.TR, t.qr_lo, t.qr_hi, t.nsplit, t.chunk, t.tiles_per, po, (float2*)(po + t.nsplit * rh * hd)};
+}
+static int pm_launch(const cs_pages_dev& D, const pa_args& A, const pa_plan& P, const pa_part& t, hipStream_t s) {
+    if (t.nsplit <= 1) return CS_OK;
+    int lanes = 0;
+    while (4 << lanes < D.p.head_dim) ++lanes;
+    const int groups = (int)cs_ceil_div(t.TR, PM_THREADS >> lanes);
+    const int64_t grid = (int64_t)t.tiles * D.p.n_kv_heads * groups;
+    CS_REQUIRE(grid <= 0x7fffffff, CS_E_UNSUPPORTED, "cs_paged_attention: too many tiles");
+    if (D.p.dtype == CS_F32) k_paged_merge<float><<<(unsigned)grid, PM_THREADS, 0, s>>>(D, A, P, lanes, groups);
+    else k_paged_merge<bf16_t><<<(unsigned)grid, PM_THREADS, 0, s>>>(D, A, P, lanes, groups);
+    return cs_launch_ok("k_paged_merge");
 }
 
 extern "C" int cs_paged_attention(const cs_pages* p, const void* q, int64_t q_row, int64_t q_head, int32_t n_heads,
@@ -1115,37 +1155,27 @@ extern "C" int cs_paged_attention(const cs_pages* p, const void* q, int64_t q_ro
     CS_REQUIRE(c.bytes <= 0 || (workspace && workspace_bytes >= c.bytes), CS_E_CAPACITY, "%s: the workspace has %lld bytes, %lld are needed",
                who, (long long)(workspace ? workspace_bytes : 0), (long long)c.bytes);
     CS_REQUIRE(((uintptr_t)workspace & 15) == 0, CS_E_ARG, "%s: the workspace is not aligned to 16 bytes", who);
-    float* po = (float*)workspace;
-    float2* pml = (float2*)(po + c.part_floats);
-    const int nsplit = std::max(c.narrow.nsplit, c.wide.nsplit);
+    const int64_t rh = (int64_t)R * n_heads;
     const int64_t grid_n = (int64_t)c.narrow.tiles * p->n_kv_heads * c.narrow.nsplit, grid_w = (int64_t)c.wide.tiles * p->n_kv_heads * c.wide.nsplit;
     CS_REQUIRE(grid_n <= 0x7fffffff && grid_w <= 0x7fffffff, CS_E_UNSUPPORTED, "%s: too many tiles", who);
     const bool f32 = p->dtype == CS_F32;
     int rc = CS_OK;
     if (grid_w) {
-        const pa_plan P = pa_plan_of(c.wide, nsplit, po, pml);
+        const pa_plan P = pa_plan_of(c.wide, (char*)workspace + c.at_w, rh, p->head_dim);
         const unsigned n = (unsigned)grid_w;
         if (f32) rc = c.hdt == 64 ? pf_launch<64, 2, false>(D, A, P, n, s) : c.hdt == 128 ? pf_launch<128, 2, false>(D, A, P, n, s) : pf_launch<256, 1, false>(D, A, P, n, s);
         else rc = c.hdt == 64 ? pw_launch<64, 2>(D, A, P, n, s) : c.hdt == 128 ? pw_launch<128, 2>(D, A, P, n, s) : pw_launch<256, 1>(D, A, P, n, s);
         CS_TRY(rc);
+        CS_TRY(pm_launch(D, A, P, c.wide, s));
     }
     if (grid_n) {
-        const pa_plan P = pa_plan_of(c.narrow, nsplit, po, pml);
+        const pa_plan P = pa_plan_of(c.narrow, (char*)workspace, rh, p->head_dim);
         const unsigned n = (unsigned)grid_n;
 #define PN(HD_, NT_) if (c.hdt == HD_ && c.narrow.nt == NT_) rc = f32 ? pf_launch<HD_, NT_, true>(D, A, P, n, s) : pn_launch<HD_, NT_>(D, A, P, n, s)
         PN(64, 1); PN(64, 2); PN(64, 3); PN(128, 1); PN(128, 2); PN(128, 3); PN(256, 1);
 #undef PN
         CS_TRY(rc);
-    }
-    if (nsplit > 1) {
-        int lanes = 0;
-        while (4 << lanes < p->head_dim) ++lanes;
-        const int64_t rh = (int64_t)R * n_heads;
-        const unsigned n = (unsigned)cs_ceil_div(rh, 256 >> lanes);
-        const int32_t* end = d_row0 ? d_row0 + p->batch : nullptr;
-        if (f32) k_paged_merge<float><<<n, 256, 0, s>>>(po, pml, nsplit, rh, n_heads, p->head_dim, lanes, end, (float*)out, out_row, out_head);
-        else k_paged_merge<bf16_t><<<n, 256, 0, s>>>(po, pml, nsplit, rh, n_heads, p->head_dim, lanes, end, (bf16_t*)out, out_row, out_head);
-        return cs_launch_ok("k_paged_merge");
+        CS_TRY(pm_launch(D, A, P, c.narrow, s));
     }
     return CS_OK;
 }

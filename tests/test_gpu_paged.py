@@ -531,7 +531,7 @@ def test_workspace_of_the_callers():
     c = Cache([9000, 20011], [11, 11], 2, 128, 64, BF)
     q = randn((22, 8, 128), gen(1), BF)
     want = cs.cs_paged_attention(c.pages, q, max_rows=11, max_len=20022)
-    need = cs.load_library().cs_paged_attention_workspace(cs.C.byref(c.pages.c), 8, 0, 22, 11, 20022)
+    need = cs.cs_paged_attention_workspace(c.pages, 8, 22, max_rows=11, max_len=20022)
     ws = torch.full((need + 64,), 0xA5, dtype=torch.uint8, device=DEV)
     assert torch.equal(cs.cs_paged_attention(c.pages, q, max_rows=11, max_len=20022, workspace=ws[:need] if need else None), want)
     assert bool((ws[need:] == 0xA5).all())
