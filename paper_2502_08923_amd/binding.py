@@ -820,9 +820,11 @@ def cs_paged_attention(pages: Pages, q: torch.Tensor, row0: Optional[torch.Tenso
         raise TypeError("out must have the type of q")
     lib, r0 = load_library(), pages._row0(row0)
     if workspace is None:
-        need = cs_paged_attention_workspace(pages, H, R, r0 is not None, max_rows, max_len)
+        need = lib.cs_paged_attention_workspace(pages.ref, H, 1 if r0 else 0, R, max_rows, max_len)
         if need > 0:
-            workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+            workspace = q.new_empty(need, dtype=torch.uint8)
+        elif need < 0:
+            _check(need)
     elif not workspace.is_contiguous():
         raise ValueError("workspace must be contiguous")
     _check(lib.cs_paged_attention(pages.ref, *qp, H, r0, R, 1.0 / math.sqrt(hd) if scale is None else scale, window,
