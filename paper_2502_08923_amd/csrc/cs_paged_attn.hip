@@ -19,63 +19,131 @@ struct pa_args {
     float scale2;             // scale * log2(e): scores in base-2 units
 };
 
-// ---- which query rows a workgroup has ----------------------------------------------------
+// ---- which query rows and tokens a workgroup has --------------------------------------------------
 // The G * rows query rows of a stream's KV head (row n: block row n / G, head n % G of the group) are cut into tiles of TR.
-// Streams with qr_lo < G * rows <= qr_hi take part in a launch.
+// Streams with qr_lo < G * rows <= qr_hi take part in a launch.  The tokens of a tile are cut into ranges of `chunk`, where that fills the
+// chip better; lengths are only known on the device, so the cut is made there, by every workgroup for itself: each lane
+// prices another number of ranges for the longest stream (rounds of the chip that all ranges of all streams then take, a round
+// costing its tokens and, in the same unit, a workgroup's start and end), and the cheapest is taken.  Batches of more than 64 streams
+// have workgroups enough and take the host's cut.
 struct pa_tile {
     int b, n0, QR;            // stream, first query row, query rows of the stream
     int row0, rows, L;        // its first row, rows, length
 };
 struct pa_plan {
     int TR, qr_lo, qr_hi;
-    int nsplit;               // token ranges
-    int chunk;                // tokens of a range; the last one takes what is left
-    int tiles_per;            // tiles of a stream where all have the same rows, else 0
-    float* po;                // [nsplit][R][H][hd] partial outputs
-    float2* pml;              // [nsplit][R][H] their (maximum, sum)
+    int slots, start, join;   // workgroups that run at once; tokens' worth of a workgroup's ends, and of the merge
+    int n_max, step;          // most ranges; distance of the numbers priced
+    int chunk;                // the host's cut
+    int entries;              // (tile, range) pairs that there is room for
+    float* po;                // [entry][KVH][TR][hd] partial outputs
+    float2* pml;              // [entry][KVH][TR] their (maximum, sum)
+    int4* who;                // [entry] (first row, first query row, query rows, range | ranges << 16) for the merge; ranges 0: nobody
+};
+struct pa_work {
+    pa_tile T;
+    int entry;                // this (tile, range) among all; the ranges of a tile follow each other
+    int split, nsplit, chunk; // range, ranges of the stream's tiles, tokens of one (the last takes what is left)
 };
 
-__device__ __forceinline__ bool pa_find_tile(const cs_pages_dev& D, int G, const pa_plan& P, int tile, pa_tile& o) {
-    int b = -1, k = 0;
-    if (P.tiles_per) {
-        b = tile / P.tiles_per;
-        k = tile - b * P.tiles_per;
-        if (b >= D.p.batch) return false;
+// tiles of stream b, and the tokens that one of them walks
+__device__ __forceinline__ int2 pa_extent(const cs_pages_dev& D, int G, int window, const pa_plan& P, int b) {
+    const int rows = cs_stream_rows(D, b).y;
+    const int64_t qr = (int64_t)rows * G;
+    if (qr <= P.qr_lo || qr > P.qr_hi) return make_int2(0, 0);
+    int span = min(cs_stream_len(D, b) + rows, D.cap);
+    if (window) span = (int)min((int64_t)span, (int64_t)window + min(rows, P.TR / G + 1) + 32);
+    return make_int2((int)((qr + P.TR - 1) / P.TR), max(span, 1));
+}
+// Reductions over the wave in registers (data-parallel primitives: rows of 16, then row ends to the rows behind them); a lane that a step does
+// not reach combines with `id`.  Lane 63 has everything.
+template <typename F>
+__device__ __forceinline__ int pa_wave_reduce(int v, int id, F f) {
+#define PA_DPP(ctrl, rows) v = f(v, __builtin_amdgcn_update_dpp(id, v, ctrl, rows, 0xf, false))
+    PA_DPP(0x111, 0xf);
+    PA_DPP(0x112, 0xf);
+    PA_DPP(0x114, 0xf);
+    PA_DPP(0x118, 0xf);
+    PA_DPP(0x142, 0xa);
+    PA_DPP(0x143, 0xc);
+#undef PA_DPP
+    return v;
+}
+__device__ __forceinline__ int pa_wave_scan(int v) {                       // inclusive
+    return pa_wave_reduce(v, 0, [](int a, int b) { return a + b; });
+}
+
+__device__ __forceinline__ bool pa_find_entry(const cs_pages_dev& D, int G, int window, const pa_plan& P, int wg, pa_work& o) {
+    const int lane = threadIdx.x & 63, B = D.p.batch;
+    int chunk = P.chunk, b = -1, at = 0, n_b = 1;
+    if (B <= 64) {            // (a wave has a lane for each stream)
+        const int2 e = lane < B ? pa_extent(D, G, window, P, lane) : make_int2(0, 0);
+        if (P.n_max > 1) {
+            const int longest = __builtin_amdgcn_readlane(pa_wave_reduce(e.y, 0, [](int a, int b) { return max(a, b); }), 63);
+            const int n = 1 + lane * P.step;
+            const int cut = max(((longest + n - 1) / n + 31) & ~31, 32);
+            const float inv = 1.0f / (float)cut;
+            int count = 0;
+            for (int i = 0; i < B; ++i) {
+                const int tokens = __builtin_amdgcn_readlane(e.y, i), q = (int)((float)tokens * inv), r = tokens - q * cut;
+                count += __builtin_amdgcn_readlane(e.x, i) * (q + (r > 0) + (r > cut));       // (q is off by one at most)
+            }
+            float cost = ceilf((float)count * (float)D.p.n_kv_heads / (float)P.slots) * (float)(cut + P.start) + (n > 1 ? (float)(P.join + n) : 0.f);
+            if (n > 1 && (n > P.n_max || cut < 64 || count > P.entries)) cost = INFINITY;
+            // (costs are positive: their bits are ordered as they are)
+            const int best = __builtin_amdgcn_readlane(pa_wave_reduce(__float_as_int(cost), 0x7f800000, [](int a, int b) { return min(a, b); }), 63);
+            chunk = __builtin_amdgcn_readlane(cut, __ffsll(__ballot(__float_as_int(cost) == best)) - 1);
+        }
+        const int n = e.x ? min(P.n_max, max(1, (e.y + chunk - 1) / chunk)) : 1;
+        const int mine = e.x * n, incl = pa_wave_scan(mine), total = min(__builtin_amdgcn_readlane(incl, 63), P.entries);
+        if (wg >= total) return false;
+        const int idx = total - 1 - wg;                     // the last tiles of a prompt see most: they go first
+        const int l = __ffsll(__ballot(incl > idx)) - 1;
+        b = l;
+        n_b = __builtin_amdgcn_readlane(n, l);
+        at = idx - (__builtin_amdgcn_readlane(incl, l) - __builtin_amdgcn_readlane(mine, l));
+        o.entry = idx;
     } else {
-        const int lane = threadIdx.x & 63;
         int base = 0;
-        for (int b0 = 0; b0 < D.p.batch; b0 += 64) {
-            int n = 0;
-            if (b0 + lane < D.p.batch) {
-                const int64_t qr = (int64_t)cs_stream_rows(D, b0 + lane).y * G;
-                n = qr > P.qr_lo && qr <= P.qr_hi ? (int)((qr + P.TR - 1) / P.TR) : 0;
-            }
-            int incl = n;
-#pragma unroll
-            for (int s = 1; s < 64; s <<= 1) {
-                const int v = __shfl_up(incl, s, 64);
-                incl += lane >= s ? v : 0;
-            }
-            const unsigned long long past = __ballot(base + incl > tile);
+        for (int b0 = 0; b0 < B; b0 += 64) {
+            const int2 e = b0 + lane < B ? pa_extent(D, G, window, P, b0 + lane) : make_int2(0, 0);
+            const int n = e.x ? min(P.n_max, max(1, (e.y + chunk - 1) / chunk)) : 1;
+            const int mine = e.x * n, incl = pa_wave_scan(mine);
+            const unsigned long long past = __ballot(base + incl > wg);
             if (past) {
                 const int l = __ffsll(past) - 1;
                 b = b0 + l;
-                k = tile - base - (__shfl(incl, l, 64) - __shfl(n, l, 64));
+                n_b = __builtin_amdgcn_readlane(n, l);
+                at = wg - base - (__builtin_amdgcn_readlane(incl, l) - __builtin_amdgcn_readlane(mine, l));
                 break;
             }
-            base += __shfl(incl, 63, 64);
+            base += __builtin_amdgcn_readlane(incl, 63);
         }
         if (b < 0) return false;
+        o.entry = wg;
     }
     b = __builtin_amdgcn_readfirstlane(b);
+    at = __builtin_amdgcn_readfirstlane(at);
+    n_b = __builtin_amdgcn_readfirstlane(n_b);
     const int2 sr = cs_stream_rows(D, b);
-    o.b = b;
-    o.row0 = __builtin_amdgcn_readfirstlane(sr.x);
-    o.rows = __builtin_amdgcn_readfirstlane(sr.y);
-    o.QR = o.rows * G;
-    o.n0 = __builtin_amdgcn_readfirstlane(k) * P.TR;
-    o.L = __builtin_amdgcn_readfirstlane(cs_stream_len(D, b));
-    return o.n0 < o.QR;
+    o.T.b = b;
+    o.T.row0 = __builtin_amdgcn_readfirstlane(sr.x);
+    o.T.rows = __builtin_amdgcn_readfirstlane(sr.y);
+    o.T.QR = o.T.rows * G;
+    o.T.n0 = at / n_b * P.TR;
+    o.T.L = __builtin_amdgcn_readfirstlane(cs_stream_len(D, b));
+    o.split = at % n_b;
+    o.nsplit = n_b;
+    o.chunk = __builtin_amdgcn_readfirstlane(chunk);
+    return true;
+}
+
+// the same, noted down for the merge
+__device__ __forceinline__ bool pa_find(const cs_pages_dev& D, int G, int window, const pa_plan& P, int wg, int kvh, pa_work& o) {
+    const bool work = pa_find_entry(D, G, window, P, wg, o);
+    if (P.n_max > 1 && kvh == 0 && threadIdx.x == 0)
+        P.who[work ? o.entry : wg] = work ? make_int4(o.T.row0, o.T.n0, o.T.QR, o.split | o.nsplit << 16) : make_int4(0, 0, 0, 0);
+    return work;
 }
 
 __device__ __forceinline__ void pa_store4(float* p, f32x4 v) { *reinterpret_cast<f32x4*>(p) = v; }
@@ -86,8 +154,9 @@ __device__ __forceinline__ void pa_store4(bf16_t* p, f32x4 v) {
 // The (max, sum, O) triples of W waves side by side in LDS -> the tile's rows: the output itself where the tokens are in one
 // range, else this range's partial result.
 template <int W, int HD, int ROWS, typename T_>
-__device__ __forceinline__ void pa_finish(const cs_pages_dev& D, const pa_args& A, const pa_plan& P, const pa_tile& T, int kvh, int split,
-                                          int n_rows, const float* s_o, const float2* s_ml, int tid, int n_threads) {
+__device__ __forceinline__ void pa_finish(const cs_pages_dev& D, const pa_args& A, const pa_plan& P, const pa_work& K, int kvh, int n_rows,
+                                          const float* s_o, const float2* s_ml, int tid, int n_threads) {
+    const pa_tile& T = K.T;
     constexpr int OROW = HD + 4;
     const int hd = D.p.head_dim;
 #pragma unroll 1
@@ -110,13 +179,13 @@ __device__ __forceinline__ void pa_finish(const cs_pages_dev& D, const pa_args& 
             l += f * ml[w].y;
         }
         const int i = (T.n0 + n) / A.G, h = kvh * A.G + T.n0 + n - i * A.G;
-        const int64_t r = T.row0 + i, rh = r * A.H + h;
-        if (P.nsplit == 1) {
+        const int64_t r = T.row0 + i;
+        if (K.nsplit == 1) {
             const float inv = l > 0.f ? 1.0f / l : 0.f;           // a row that sees nothing: 0
             if (d < hd) pa_store4((T_*)A.out + r * A.out_row + h * A.out_head + d, o * inv);
             continue;
         }
-        const int64_t at = (int64_t)split * D.R * A.H + rh;
+        const int64_t at = ((int64_t)K.entry * D.p.n_kv_heads + kvh) * P.TR + n;
         if (d < hd) *reinterpret_cast<f32x4*>(P.po + at * hd + d) = o;
         if (d == 0) P.pml[at] = make_float2(M, l);
     }
@@ -150,16 +219,17 @@ __global__ __launch_bounds__(64 * PN_WAVES) void k_paged_narrow(cs_pages_dev D, 
     __shared__ __attribute__((aligned(16))) unsigned char smem[MERGE_BYTES > Q_BYTES ? MERGE_BYTES : Q_BYTES];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int c = lane & 15, g = lane >> 4;
-    const int KVH = D.p.n_kv_heads, kvh = blockIdx.x % KVH, rest = blockIdx.x / KVH, split = rest % P.nsplit;
-    pa_tile T;
-    if (!pa_find_tile(D, A.G, P, rest / P.nsplit, T)) return;
+    const int KVH = D.p.n_kv_heads, kvh = blockIdx.x % KVH;
+    pa_work K;
+    if (!pa_find(D, A.G, A.window, P, blockIdx.x / KVH, kvh, K)) return;
+    const pa_tile& T = K.T;
     const int hd = D.p.head_dim;
     const int n_rows = min(ROWS, T.QR - T.n0);          // live query rows of the tile
     const int i_lo = T.n0 / A.G, i_hi = (T.n0 + n_rows - 1) / A.G;
     const int n_tok = min(T.L + i_hi + 1, D.cap);       // tokens that the tile's last row sees
     const int base = A.window ? max(0, T.L + i_lo - A.window + 1) & ~31 : 0;
-    const int w_begin = (int)min((int64_t)base + (int64_t)split * P.chunk, (int64_t)n_tok);
-    const int t_end = split == P.nsplit - 1 ? n_tok : (int)min((int64_t)w_begin + P.chunk, (int64_t)n_tok);
+    const int w_begin = (int)min((int64_t)base + (int64_t)K.split * K.chunk, (int64_t)n_tok);
+    const int t_end = K.split == K.nsplit - 1 ? n_tok : (int)min((int64_t)w_begin + K.chunk, (int64_t)n_tok);
     // blocks between these need no mask
     const int open_lo = A.window ? T.L + i_hi - A.window + 1 : 0, open_hi = min(T.L + i_lo + 1, D.cap);
 
@@ -399,7 +469,7 @@ __global__ __launch_bounds__(64 * PN_WAVES) void k_paged_narrow(cs_pages_dev D, 
                 }
     }
     __syncthreads();
-    pa_finish<PN_WAVES, HD, ROWS, bf16_t>(D, A, P, T, kvh, split, n_rows, s_o, s_ml, tid, 64 * PN_WAVES);
+    pa_finish<PN_WAVES, HD, ROWS, bf16_t>(D, A, P, K, kvh, n_rows, s_o, s_ml, tid, 64 * PN_WAVES);
 }
 
 // As cs_load_to_lds, where the base comes straight from a lane: five wait states lie between a v_readlane and the load that takes
@@ -433,19 +503,19 @@ __global__ __launch_bounds__(64 * PW_WAVES) void k_paged_wide(cs_pages_dev D, pa
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int c = lane & 15, g = lane >> 4;
     const int KVH = D.p.n_kv_heads;
-    // KV heads in turn, so that with eight of them each stays on one die and its cache; a stream's last rows, which see most, first
-    const int kvh = blockIdx.x % KVH, rest = blockIdx.x / KVH;
-    const int split = rest % P.nsplit, tile = (int)(gridDim.x / (KVH * P.nsplit)) - 1 - rest / P.nsplit;
-    pa_tile T;
-    if (!pa_find_tile(D, A.G, P, tile, T)) return;
+    // KV heads in turn, so that with eight of them each stays on one die and its cache
+    const int kvh = blockIdx.x % KVH;
+    pa_work K;
+    if (!pa_find(D, A.G, A.window, P, blockIdx.x / KVH, kvh, K)) return;
+    const pa_tile& T = K.T;
     const int hd = D.p.head_dim, G = A.G;
     const int n_rows = min(TR, T.QR - T.n0);
     const int i_lo = T.n0 / G, i_hi = (T.n0 + n_rows - 1) / G;
     const int n_lim = min(T.L + i_hi + 1, D.cap);              // tokens that the tile's last row sees
     const int n_tok = min(T.L + T.rows, D.cap);                // tokens that are there
     const int base = A.window ? max(0, T.L + i_lo - A.window + 1) & ~31 : 0;
-    const int w_begin = (int)min((int64_t)base + (int64_t)split * P.chunk, (int64_t)n_lim);
-    const int t_end = split == P.nsplit - 1 ? n_lim : (int)min((int64_t)w_begin + P.chunk, (int64_t)n_lim);
+    const int w_begin = (int)min((int64_t)base + (int64_t)K.split * K.chunk, (int64_t)n_lim);
+    const int t_end = K.split == K.nsplit - 1 ? n_lim : (int)min((int64_t)w_begin + K.chunk, (int64_t)n_lim);
     const int nblocks = (t_end - w_begin + 31) / 32;
 
     // query fragments, once; they must have arrived before the first counted request
@@ -701,9 +771,9 @@ __global__ __launch_bounds__(64 * PW_WAVES) void k_paged_wide(cs_pages_dev D, pa
         const int n = n0 + nt * 16;
         if (n >= T.QR) continue;
         const int i = n / G, h = kvh * G + n - i * G;
-        const int64_t r = T.row0 + i, rh = r * A.H + h;
+        const int64_t r = T.row0 + i;
         const float l = lacc[nt][0];
-        if (P.nsplit == 1) {
+        if (K.nsplit == 1) {
             const float inv = l > 0.f ? 1.0f / l : 0.f;
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt) {
@@ -712,7 +782,7 @@ __global__ __launch_bounds__(64 * PW_WAVES) void k_paged_wide(cs_pages_dev D, pa
             }
             continue;
         }
-        const int64_t at = (int64_t)split * D.R * A.H + rh;
+        const int64_t at = ((int64_t)K.entry * KVH + kvh) * P.TR + n - T.n0;
         if (g == 0) P.pml[at] = make_float2(m_run[nt], l);
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
@@ -738,17 +808,17 @@ __global__ __launch_bounds__(64 * PF_WAVES, !TOKENS && HD <= 128 ? 2 : 1) void k
     __shared__ __attribute__((aligned(16))) float smem[MERGE_FLOATS > Q_FLOATS ? MERGE_FLOATS : Q_FLOATS];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int c = lane & 15, g = lane >> 4;
-    const int KVH = D.p.n_kv_heads, kvh = blockIdx.x % KVH, rest = blockIdx.x / KVH;
-    const int split = rest % P.nsplit, tile = (int)(gridDim.x / (KVH * P.nsplit)) - 1 - rest / P.nsplit;
-    pa_tile T;
-    if (!pa_find_tile(D, A.G, P, tile, T)) return;
+    const int KVH = D.p.n_kv_heads, kvh = blockIdx.x % KVH;
+    pa_work K;
+    if (!pa_find(D, A.G, A.window, P, blockIdx.x / KVH, kvh, K)) return;
+    const pa_tile& T = K.T;
     const int hd = D.p.head_dim, G = A.G;
     const int n_rows = min(TR, T.QR - T.n0);
     const int i_hi = (T.n0 + n_rows - 1) / G;
     const int n_lim = min(T.L + i_hi + 1, D.cap);
     const int base = A.window ? max(0, T.L + T.n0 / G - A.window + 1) & ~31 : 0;
-    const int w_begin = (int)min((int64_t)base + (int64_t)split * P.chunk, (int64_t)n_lim);
-    const int t_end = split == P.nsplit - 1 ? n_lim : (int)min((int64_t)w_begin + P.chunk, (int64_t)n_lim);
+    const int w_begin = (int)min((int64_t)base + (int64_t)K.split * K.chunk, (int64_t)n_lim);
+    const int t_end = K.split == K.nsplit - 1 ? n_lim : (int)min((int64_t)w_begin + K.chunk, (int64_t)n_lim);
     for (int idx = tid; idx < TR * (HD / 4); idx += 64 * PF_WAVES) {
         const int n = idx / (HD / 4), d = idx % (HD / 4) * 4;
         f32x4 v = (f32x4){0.f, 0.f, 0.f, 0.f};
@@ -946,15 +1016,15 @@ __global__ __launch_bounds__(64 * PF_WAVES, !TOKENS && HD <= 128 ? 2 : 1) void k
                         (f32x4){oacc[x * 4][nt][j], oacc[x * 4 + 1][nt][j], oacc[x * 4 + 2][nt][j], oacc[x * 4 + 3][nt][j]};
         }
         __syncthreads();
-        pa_finish<PF_WAVES, HD, WROWS, float>(D, A, P, T, kvh, split, n_rows, s_o, s_ml, tid, 64 * PF_WAVES);
+        pa_finish<PF_WAVES, HD, WROWS, float>(D, A, P, K, kvh, n_rows, s_o, s_ml, tid, 64 * PF_WAVES);
     } else {
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
             const int n = wrow + nt * 16 + c;
             if (n >= n_rows) continue;
             const int i = (T.n0 + n) / G, h = kvh * G + T.n0 + n - i * G;
-            const int64_t r = T.row0 + i, rh = r * A.H + h, at = (int64_t)split * D.R * A.H + rh;
-            const bool whole = P.nsplit == 1;
+            const int64_t r = T.row0 + i, at = ((int64_t)K.entry * KVH + kvh) * P.TR + n;
+            const bool whole = K.nsplit == 1;
             const float inv = l_run[nt] > 0.f ? 1.0f / l_run[nt] : 0.f;
             if (g == 0 && !whole) P.pml[at] = make_float2(m_run[nt], l_run[nt]);
 #pragma unroll
@@ -973,43 +1043,45 @@ __global__ __launch_bounds__(64 * PF_WAVES, !TOKENS && HD <= 128 ? 2 : 1) void k
 
 // ---- joining token ranges ---------------------------------------------------------------------
 // out[r][h] = sum_s 2^(m_s - M) O_s / sum_s 2^(m_s - M) l_s.  2^lanes_log2 lanes have a query row's hd features, four each; a lane
-// reads the (max, sum) pairs of every lanes-th range, and the weights go round by shuffles.  A workgroup has 256 >> lanes_log2 query
-// rows of a tile, the same tiles as the kernel before it: rows that had no launch, or went without ranges, are not touched.
+// reads the (max, sum) pairs of every lanes-th range, and the weights go round by shuffles.  The workgroups are those of the kernel
+// before it: the ones that had the ranges of a tile share out its rows.
 #define PM_THREADS 256
 template <typename T_>
-__global__ __launch_bounds__(PM_THREADS) void k_paged_merge(cs_pages_dev D, pa_args A, pa_plan P, int lanes_log2, int groups) {
-    const int KVH = D.p.n_kv_heads, group = blockIdx.x % groups, item = blockIdx.x / groups, kvh = item % KVH;
-    const int lanes = 1 << lanes_log2, sub = threadIdx.x & (lanes - 1), d = sub * 4;
-    const int n = group * (PM_THREADS >> lanes_log2) + (threadIdx.x >> lanes_log2);
-    pa_tile T;
-    if (!pa_find_tile(D, A.G, P, item / KVH, T)) return;
-    if (n >= P.TR || T.n0 + n >= T.QR) return;
-    const int i = (T.n0 + n) / A.G, h = kvh * A.G + T.n0 + n - i * A.G, hd = D.p.head_dim;
-    const int64_t r = T.row0 + i, rh = r * A.H + h, n_rh = (int64_t)D.R * A.H;
-    float M = -INFINITY;
-    for (int s = sub; s < P.nsplit; s += lanes) M = fmaxf(M, P.pml[s * n_rh + rh].x);
-    for (int o = lanes >> 1; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor(M, o, 64));
-    const float Ms = M == -INFINITY ? 0.f : M;
-    f32x4 acc = (f32x4){0.f, 0.f, 0.f, 0.f};
-    float l = 0.f;
-    for (int s0 = 0; s0 < P.nsplit; s0 += lanes) {
-        float2 ml = make_float2(-INFINITY, 0.f);
-        if (s0 + sub < P.nsplit) ml = P.pml[(s0 + sub) * n_rh + rh];
-        const float w = __builtin_amdgcn_exp2f(ml.x - Ms), wl = w * ml.y;
-        const int ns = min(lanes, P.nsplit - s0);
-        const float* __restrict__ src = P.po + ((int64_t)s0 * n_rh + rh) * hd + min(d, hd - 4);
-        for (int s = 0; s < ns; s += 4)
+__global__ __launch_bounds__(PM_THREADS) void k_paged_merge(cs_pages_dev D, pa_args A, pa_plan P, int lanes_log2) {
+    const int KVH = D.p.n_kv_heads, kvh = blockIdx.x % KVH;
+    const int entry = blockIdx.x / KVH;
+    const int4 who = P.who[entry];
+    const int split = who.w & 0xffff, nsplit = who.w >> 16;
+    if (nsplit <= 1) return;
+    const int lanes = 1 << lanes_log2, sub = threadIdx.x & (lanes - 1), d = sub * 4, per = PM_THREADS >> lanes_log2, hd = D.p.head_dim;
+    const int64_t step = (int64_t)KVH * P.TR;                      // from one range's row to the next one's
+    for (int n = split * per + (threadIdx.x >> lanes_log2); n < P.TR && who.y + n < who.z; n += nsplit * per) {
+        const int64_t at = ((int64_t)(entry - split) * KVH + kvh) * P.TR + n;
+        float M = -INFINITY;
+        for (int s = sub; s < nsplit; s += lanes) M = fmaxf(M, P.pml[at + s * step].x);
+        for (int o = lanes >> 1; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor(M, o, 64));
+        const float Ms = M == -INFINITY ? 0.f : M;
+        f32x4 acc = (f32x4){0.f, 0.f, 0.f, 0.f};
+        float l = 0.f;
+        for (int s0 = 0; s0 < nsplit; s0 += lanes) {
+            float2 ml = make_float2(-INFINITY, 0.f);
+            if (s0 + sub < nsplit) ml = P.pml[at + (s0 + sub) * step];
+            const float w = __builtin_amdgcn_exp2f(ml.x - Ms), wl = w * ml.y;
+            const int ns = min(lanes, nsplit - s0);
+            const float* __restrict__ src = P.po + (at + s0 * step) * hd + min(d, hd - 4);
+            for (int s = 0; s < ns; s += 4)
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                // (past the last range: weight 0, its row once more; a range that saw nothing has stored zeros)
-                const int from = (threadIdx.x & 63 & ~(lanes - 1)) + min(s + u, ns - 1);
-                const float keep = s + u < ns ? 1.f : 0.f;
-                l += keep * __shfl(wl, from, 64);
-                acc += keep * __shfl(w, from, 64) * *reinterpret_cast<const f32x4*>(src + (int64_t)min(s + u, ns - 1) * n_rh * hd);
-            }
+                for (int u = 0; u < 4; ++u) {
+                    // (past the last range: weight 0, its row once more; a range that saw nothing has stored zeros)
+                    const int from = (threadIdx.x & 63 & ~(lanes - 1)) + min(s + u, ns - 1);
+                    const float keep = s + u < ns ? 1.f : 0.f;
+                    l += keep * __shfl(wl, from, 64);
+                    acc += keep * __shfl(w, from, 64) * *reinterpret_cast<const f32x4*>(src + min(s + u, ns - 1) * step * hd);
+                }
+        }
+        const int i = (who.y + n) / A.G, h = kvh * A.G + who.y + n - i * A.G;
+        if (d < hd) pa_store4((T_*)A.out + (int64_t)(who.x + i) * A.out_row + h * A.out_head + d, acc * (l > 0.f ? 1.0f / l : 0.f));
     }
-    if (d >= hd) return;
-    pa_store4((T_*)A.out + r * A.out_row + h * A.out_head + d, acc * (l > 0.f ? 1.0f / l : 0.f));
 }
 
 // ---- entry points --------------------------------------------------------------------------
@@ -1025,43 +1097,46 @@ static int check_shape(const char* who, const cs_pages* p, int32_t n_heads, int3
 
 // How a call is cut: the same for the workspace and the launches.
 struct pa_part {
-    int nt, TR, qr_lo, qr_hi, tiles, tiles_per, nsplit, chunk;      // tiles 0: no launch
+    int nt, TR, qr_lo, qr_hi, tiles;          // tiles: an upper bound; 0: no launch
+    int slots, start, join, n_max, step, chunk, entries;
 };
 struct pa_cut {
     int hdt;
     pa_part narrow, wide;
-    int64_t at_w, bytes;              // where the second launch's partial results start; bytes in all
+    int64_t at_w, bytes;                      // where the second launch's partial results start; bytes in all
 };
-static int64_t pa_part_bytes(int64_t nsplit, int64_t rh, int hd) { return nsplit > 1 ? cs_round_up(nsplit * rh * (hd * 4 + 8), 16) : 0; }
-#define PA_MOST_RANGES 256
 #define PN_MOST 48                // query rows up to which a stream takes the kernel of few rows
-// Token ranges: as many as make the launch's rounds of the chip cheapest, a round costing what a range's tokens cost and, in the same unit,
-// what a workgroup's start and end cost; joining ranges costs a launch more.
-struct pa_cost {
-    int slots, start, join;           // workgroups that run at once; tokens' worth of a workgroup's ends, and of the merge
-};
-static void pa_ranges(pa_part& t, int64_t span, int64_t items, const pa_cost& k, int most) {
+#define PA_MOST_RANGES 256
+// The host's cut prices the ranges as the device does, with every stream as long as the longest; batches of more than 64 streams take it.
+// For the others it says how many (tile, range) pairs there is room for: one round of the chip, or what the host's cut has.
+// (A workgroup without a pair ends at once, but where one fills a compute unit it waits for its turn.)
+static int64_t pa_ranges(pa_part& t, int64_t len, int B, int KVH, int hd, int slots, int start, int join) {
+    if (!t.tiles) return 0;
+    t.slots = slots, t.start = start, t.join = join;
+    const int64_t items = (int64_t)t.tiles * KVH;
+    // (no ranges where the chip is full twice over, or where even the shortest would not pay for the merge)
+    const bool one = items >= 2 * slots || (items <= slots && len <= 64 + join);
+    const int most = one ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>(PA_MOST_RANGES, len / 64));
     int64_t best = 0;
-    for (int n = 1; n <= most && (n == 1 || n * 64 <= span); ++n) {
-        const int64_t chunk = cs_round_up(cs_ceil_div(span, n), 32);
-        const int64_t cost = cs_ceil_div(items * n, k.slots) * (chunk + k.start) + (n > 1 ? k.join + n : 0);
-        if (n == 1 || cost < best) {
-            best = cost;
-            t.chunk = (int)chunk;
-            t.nsplit = (int)cs_ceil_div(span, chunk);
-        }
+    int n_best = 1;
+    for (int n = 1; n <= most; ++n) {
+        const int64_t chunk = cs_round_up(std::max<int64_t>(cs_ceil_div(len, n), 1), 32);
+        const int64_t cost = cs_ceil_div(items * n, slots) * (chunk + start) + (n > 1 ? join + n : 0);
+        if (n == 1 || cost < best) best = cost, n_best = n, t.chunk = (int)chunk;
     }
+    t.entries = (int)std::max<int64_t>((int64_t)t.tiles * n_best, most > 1 && B <= 64 ? cs_ceil_div(slots, KVH) : 0);
+    t.n_max = B > 64 ? n_best : std::min(most, t.entries);
+    t.step = (int)cs_ceil_div(t.n_max, 64);
+    return t.n_max > 1 ? cs_round_up((int64_t)t.entries * KVH * t.TR * (hd * 4 + 8), 16) + (int64_t)t.entries * 16 : 0;
 }
-static pa_cut pa_make_cut(const cs_pages* p, int H, bool has_row0, int R, int max_rows, int64_t max_len, int window) {
+static pa_cut pa_make_cut(const cs_pages* p, int H, bool has_row0, int R, int max_rows, int64_t max_len) {
     pa_cut c = {};
     const int KVH = p->n_kv_heads, G = H / KVH, B = p->batch, cap = p->table_pages * p->page_size;
     const int rows = has_row0 ? (max_rows ? std::min(max_rows, R) : R) : R / B;
-    const int64_t qr = (int64_t)rows * G, all = (int64_t)R * G;
-    c.hdt = p->head_dim <= 64 ? 64 : p->head_dim <= 128 ? 128 : 256;
-    const int64_t len = max_len && max_len < cap ? max_len : cap;
-    const int64_t span = window ? std::min<int64_t>(len, (int64_t)window + rows + 32) : len;
-    pa_part &N = c.narrow, &W = c.wide;
+    const int64_t qr = (int64_t)rows * G, all = (int64_t)R * G, len = max_len && max_len < cap ? max_len : cap;
     const bool f32 = p->dtype == CS_F32;
+    c.hdt = p->head_dim <= 64 ? 64 : p->head_dim <= 128 ? 128 : 256;
+    pa_part &N = c.narrow, &W = c.wide;
     // Streams of up to n_most query rows per KV head go to the kernel of few rows.  Where a batch has longer ones too, that kernel is
     // made for single tokens: a tile of 48 rows would cost every one of them three tiles' products.
     const int n_most = c.hdt == 256 || qr > PN_MOST ? 16 : PN_MOST;
@@ -1069,28 +1144,19 @@ static pa_cut pa_make_cut(const cs_pages* p, int H, bool has_row0, int R, int ma
         N.nt = (int)std::min<int64_t>(n_most / 16, cs_ceil_div(qr, 16));
         N.TR = 16 * N.nt;
         N.qr_hi = qr <= n_most ? 0x7fffffff : n_most;
-        N.tiles_per = has_row0 ? 0 : 1;
-        N.tiles = !has_row0 ? B : qr <= n_most ? (int)std::min<int64_t>(all / N.TR + std::min(B, R), 0x7fffffff) : std::min(B, R);
+        N.tiles = !has_row0 ? B : (int)(qr <= n_most ? all / N.TR + std::min(B, R) : std::min(B, R));
     }
     if (qr > n_most) {
         W.nt = c.hdt == 256 ? 1 : 2;
         W.TR = (f32 ? PF_WAVES : PW_WAVES) * 16 * W.nt;
         W.qr_lo = has_row0 ? n_most : 0;
         W.qr_hi = 0x7fffffff;
-        W.tiles_per = has_row0 ? 0 : (int)cs_ceil_div(qr, W.TR);
-        W.tiles = has_row0 ? (int)(all / W.TR + std::min<int64_t>(B, all / (n_most + 1))) : B * W.tiles_per;
+        W.tiles = (int)(has_row0 ? all / W.TR + std::min<int64_t>(B, all / (n_most + 1)) : B * cs_ceil_div(qr, W.TR));
     }
-    // the workspace is sized without a window, which is not given more ranges
-    const int64_t rh = (int64_t)R * H;
-    auto ranges = [&](pa_part& t, const pa_cost& k) -> int64_t {
-        if (!t.tiles) return 0;
-        pa_ranges(t, len, (int64_t)t.tiles * KVH, k, PA_MOST_RANGES);
-        const int64_t bytes = pa_part_bytes(t.nsplit, rh, p->head_dim);
-        if (span < len) pa_ranges(t, span, (int64_t)t.tiles * KVH, k, t.nsplit);
-        return bytes;
-    };
-    c.at_w = ranges(N, f32 ? pa_cost{256, 128, 384} : pa_cost{256, 256, 768});
-    c.bytes = c.at_w + ranges(W, f32 ? pa_cost{512, 16, 128} : pa_cost{256, 128, 192});
+    // The chip's slots: one workgroup per compute unit, two of the float32 kernel for many rows.  What a workgroup's ends and the merge cost
+    // was measured in tokens of each kernel's own pace; between half and twice these figures nothing moves by more than 2 %.
+    c.at_w = f32 ? pa_ranges(N, len, B, KVH, p->head_dim, 256, 128, 384) : pa_ranges(N, len, B, KVH, p->head_dim, 256, 256, 768);
+    c.bytes = c.at_w + (f32 ? pa_ranges(W, len, B, KVH, p->head_dim, 512, 16, 128) : pa_ranges(W, len, B, KVH, p->head_dim, 256, 128, 192));
     return c;
 }
 
@@ -1101,7 +1167,7 @@ extern "C" int64_t cs_paged_attention_workspace(const cs_pages* p, int32_t n_hea
     CS_REQUIRE(has_row0 || p->batch == 0 || R % p->batch == 0, CS_E_ARG, "%s: R rows cannot be shared out among %d streams without d_row0",
                who, p->batch);
     if (R == 0 || p->batch == 0) return 0;
-    return pa_make_cut(p, n_heads, has_row0 != 0, R, max_rows, max_len, 0).bytes;
+    return pa_make_cut(p, n_heads, has_row0 != 0, R, max_rows, max_len).bytes;
 }
 
 template <int HD, int NT>
@@ -1119,19 +1185,19 @@ static int pw_launch(const cs_pages_dev& D, const pa_args& A, const pa_plan& P, 
     k_paged_wide<HD, NT><<<grid, 64 * PW_WAVES, 0, s>>>(D, A, P);
     return cs_launch_ok("k_paged_wide");
 }
-static pa_plan pa_plan_of(const pa_part& t, char* ws, int64_t rh, int hd) {
+static pa_plan pa_plan_of(const pa_part& t, char* ws, int KVH, int hd) {
+    const int64_t rows = (int64_t)t.entries * KVH * t.TR;
     float* po = (float*)ws;
-    return {t.TR, t.qr_lo, t.qr_hi, t.nsplit, t.chunk, t.tiles_per, po, (float2*)(po + t.nsplit * rh * hd)};
+    float2* pml = (float2*)(po + rows * hd);
+    return {t.TR, t.qr_lo, t.qr_hi, t.slots, t.start, t.join, t.n_max, t.step, t.chunk, t.entries, po, pml,
+            (int4*)(ws + cs_round_up(rows * (hd * 4 + 8), 16))};
 }
-static int pm_launch(const cs_pages_dev& D, const pa_args& A, const pa_plan& P, const pa_part& t, hipStream_t s) {
-    if (t.nsplit <= 1) return CS_OK;
+static int pm_launch(const cs_pages_dev& D, const pa_args& A, const pa_plan& P, unsigned grid, hipStream_t s) {
+    if (P.n_max <= 1) return CS_OK;
     int lanes = 0;
     while (4 << lanes < D.p.head_dim) ++lanes;
-    const int groups = (int)cs_ceil_div(t.TR, PM_THREADS >> lanes);
-    const int64_t grid = (int64_t)t.tiles * D.p.n_kv_heads * groups;
-    CS_REQUIRE(grid <= 0x7fffffff, CS_E_UNSUPPORTED, "cs_paged_attention: too many tiles");
-    if (D.p.dtype == CS_F32) k_paged_merge<float><<<(unsigned)grid, PM_THREADS, 0, s>>>(D, A, P, lanes, groups);
-    else k_paged_merge<bf16_t><<<(unsigned)grid, PM_THREADS, 0, s>>>(D, A, P, lanes, groups);
+    if (D.p.dtype == CS_F32) k_paged_merge<float><<<grid, PM_THREADS, 0, s>>>(D, A, P, lanes);
+    else k_paged_merge<bf16_t><<<grid, PM_THREADS, 0, s>>>(D, A, P, lanes);
     return cs_launch_ok("k_paged_merge");
 }
 
@@ -1151,31 +1217,30 @@ extern "C" int cs_paged_attention(const cs_pages* p, const void* q, int64_t q_ro
     CS_TRY(cs_check_rows(who, "out", out, out_row, out_head, esz));
     pa_args A = {q, q_row, q_head, out, out_row, out_head, n_heads, n_heads / p->n_kv_heads, window, scale * 1.4426950408889634f};
     hipStream_t s = (hipStream_t)stream;
-    pa_cut c = pa_make_cut(p, n_heads, d_row0 != nullptr, R, max_rows, max_len, window);
+    const pa_cut c = pa_make_cut(p, n_heads, d_row0 != nullptr, R, max_rows, max_len);
     CS_REQUIRE(c.bytes <= 0 || (workspace && workspace_bytes >= c.bytes), CS_E_CAPACITY, "%s: the workspace has %lld bytes, %lld are needed",
                who, (long long)(workspace ? workspace_bytes : 0), (long long)c.bytes);
     CS_REQUIRE(((uintptr_t)workspace & 15) == 0, CS_E_ARG, "%s: the workspace is not aligned to 16 bytes", who);
-    const int64_t rh = (int64_t)R * n_heads;
-    const int64_t grid_n = (int64_t)c.narrow.tiles * p->n_kv_heads * c.narrow.nsplit, grid_w = (int64_t)c.wide.tiles * p->n_kv_heads * c.wide.nsplit;
+    const int64_t grid_n = (int64_t)c.narrow.entries * p->n_kv_heads, grid_w = (int64_t)c.wide.entries * p->n_kv_heads;
     CS_REQUIRE(grid_n <= 0x7fffffff && grid_w <= 0x7fffffff, CS_E_UNSUPPORTED, "%s: too many tiles", who);
     const bool f32 = p->dtype == CS_F32;
     int rc = CS_OK;
     if (grid_w) {
-        const pa_plan P = pa_plan_of(c.wide, (char*)workspace + c.at_w, rh, p->head_dim);
+        const pa_plan P = pa_plan_of(c.wide, (char*)workspace + c.at_w, p->n_kv_heads, p->head_dim);
         const unsigned n = (unsigned)grid_w;
         if (f32) rc = c.hdt == 64 ? pf_launch<64, 2, false>(D, A, P, n, s) : c.hdt == 128 ? pf_launch<128, 2, false>(D, A, P, n, s) : pf_launch<256, 1, false>(D, A, P, n, s);
         else rc = c.hdt == 64 ? pw_launch<64, 2>(D, A, P, n, s) : c.hdt == 128 ? pw_launch<128, 2>(D, A, P, n, s) : pw_launch<256, 1>(D, A, P, n, s);
         CS_TRY(rc);
-        CS_TRY(pm_launch(D, A, P, c.wide, s));
+        CS_TRY(pm_launch(D, A, P, n, s));
     }
     if (grid_n) {
-        const pa_plan P = pa_plan_of(c.narrow, (char*)workspace, rh, p->head_dim);
+        const pa_plan P = pa_plan_of(c.narrow, (char*)workspace, p->n_kv_heads, p->head_dim);
         const unsigned n = (unsigned)grid_n;
 #define PN(HD_, NT_) if (c.hdt == HD_ && c.narrow.nt == NT_) rc = f32 ? pf_launch<HD_, NT_, true>(D, A, P, n, s) : pn_launch<HD_, NT_>(D, A, P, n, s)
         PN(64, 1); PN(64, 2); PN(64, 3); PN(128, 1); PN(128, 2); PN(128, 3); PN(256, 1);
 #undef PN
         CS_TRY(rc);
-        CS_TRY(pm_launch(D, A, P, c.narrow, s));
+        CS_TRY(pm_launch(D, A, P, n, s));
     }
     return CS_OK;
 }
