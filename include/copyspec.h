@@ -426,9 +426,9 @@ int cs_kv_set_len_dev(cs_kv*, const int32_t* d_len /*device [B]*/, int64_t len_u
  * writes the rows, cs_paged_attention lets them attend, and the caller then advances len by what it
  * keeps (a rejected draft is a smaller advance: rows at and beyond len are dead).
  *
- * Table entries are only read for pages that hold tokens below L_b + rows.  An entry outside
+ * Table entries behind the page of a stream's last token may hold anything.  An entry outside
  * 0 .. n_pages-1 names no page: nothing is written there, and its tokens are not attended to (an
- * evicted page).  A length is taken as 0 if it is negative, and positions at and beyond
+ * evicted page).  Dead slots may hold anything as well; keys and values of live tokens must be finite.  A length is taken as 0 if it is negative, and positions at and beyond
  * table_pages * page_size do not exist: their rows are not written, and their tokens not attended to.
  *
  * Rows of a call: R rows in all, those of stream b being d_row0[b] .. d_row0[b+1]-1 (device,
@@ -437,7 +437,8 @@ int cs_kv_set_len_dev(cs_kv*, const int32_t* d_len /*device [B]*/, int64_t len_u
  * A stream may have no rows.  R == 0 or batch == 0 is a no-op.
  *
  * Limits: page_size a power of two in 16..32768, head_dim a multiple of 8 up to 256, n_heads a multiple of
- * n_kv_heads, table_pages * page_size <= 2^30.  Every pointer to rows or pools is aligned to 16 bytes, every
+ * n_kv_heads, table_pages * page_size <= 2^30, batch <= 65536, heads <= 4096, R <= 2^26 and, for the attention,
+ * R * n_heads <= 2^30.  Every pointer to rows or pools is aligned to 16 bytes, every
  * stride (in elements, >= 0, at most 2^40) is a multiple of 16 bytes; the elements of one head's row are contiguous.
  * token_stride * page_size elements of a pool must stay below 2^31 bytes.
  * ---------------------------------------------------------------------------------- */

@@ -94,8 +94,13 @@ __device__ __forceinline__ bool pa_find_entry(const cs_pages_dev& D, int G, int 
             const int best = __builtin_amdgcn_readlane(pa_wave_reduce(__float_as_int(cost), 0x7f800000, [](int a, int b) { return min(a, b); }), 63);
             chunk = __builtin_amdgcn_readlane(cut, __ffsll(__ballot(__float_as_int(cost) == best)) - 1);
         }
-        const int n = e.x ? min(P.n_max, max(1, (e.y + chunk - 1) / chunk)) : 1;
-        const int mine = e.x * n, incl = pa_wave_scan(mine), total = min(__builtin_amdgcn_readlane(incl, 63), P.entries);
+        int n = e.x ? min(P.n_max, max(1, (e.y + chunk - 1) / chunk)) : 1, mine = e.x * n, incl = pa_wave_scan(mine);
+        if (__builtin_amdgcn_readlane(incl, 63) > P.entries) {   // (row offsets that make no sense: more tiles than rows allow)
+            n = 1;
+            mine = e.x;
+            incl = pa_wave_scan(mine);
+        }
+        const int total = min(__builtin_amdgcn_readlane(incl, 63), P.entries);
         if (wg >= total) return false;
         const int idx = total - 1 - wg;                     // the last tiles of a prompt see most: they go first
         const int l = __ffsll(__ballot(incl > idx)) - 1;
@@ -119,7 +124,7 @@ __device__ __forceinline__ bool pa_find_entry(const cs_pages_dev& D, int G, int 
             }
             base += __builtin_amdgcn_readlane(incl, 63);
         }
-        if (b < 0) return false;
+        if (b < 0 || wg - at % n_b + n_b > P.entries) return false;       // (the second: as above)
         o.entry = wg;
     }
     b = __builtin_amdgcn_readfirstlane(b);
@@ -1090,7 +1095,7 @@ static int check_shape(const char* who, const cs_pages* p, int32_t n_heads, int3
     CS_REQUIRE(n_heads >= 1 && n_heads <= 4096 && n_heads % p->n_kv_heads == 0, CS_E_ARG,
                "%s: n_heads must be a multiple of n_kv_heads, up to 4096", who);
     CS_REQUIRE(R >= 0 && R <= 1 << 26, CS_E_ARG, "%s: R out of range", who);
-    CS_REQUIRE((int64_t)R * n_heads <= 0x7fffffff, CS_E_UNSUPPORTED, "%s: more than 2^31 - 1 query rows", who);
+    CS_REQUIRE((int64_t)R * n_heads <= 1 << 30, CS_E_UNSUPPORTED, "%s: R * n_heads exceeds 2^30", who);
     CS_REQUIRE(max_rows >= 0 && max_len >= 0, CS_E_ARG, "%s: negative max_rows or max_len", who);
     return CS_OK;
 }

@@ -310,6 +310,30 @@ def test_attention_long_contexts(dtype, rows, lens):
 
 
 @pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("rows,lens,window", [(1, [30000, 50], 0), (40, [9000], 0), (70, [9000, 9], 0), (300, [7001], 0), (2, [20000], 9000),
+                                              (90, [12000], 5000)])
+def test_attention_one_range_over_a_long_context(rows, lens, window, dtype):
+    """A hint of short contexts leaves one workgroup a whole one: more blocks than its lanes hold page numbers for."""
+    holes = [(0, j) for j in (0, 63, 64, 65, 127, 128, 200)]
+    Cache(lens, [rows] * len(lens), 1, 64, 16, dtype, seed=rows, holes=holes).check(2, max_rows=rows, max_len=16, window=window)
+    Cache(lens, [rows] * len(lens), 1, 128, 32, dtype, seed=rows).check(3, max_rows=rows, max_len=16, window=window)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("B", [2, 63, 64, 65, 130])
+def test_attention_many_ragged_streams(B, dtype):
+    """Lengths and rows of every size, on either side of what a wave's lanes can cut; two streams carry most of the tokens."""
+    lens = [(37 * b * b) % 90 for b in range(B)]
+    lens[0], lens[B // 2 if B > 2 else 1] = 5000, 2500
+    rows = [(b * 7) % 5 for b in range(B)]
+    rows[0] = 3
+    Cache(lens, rows, 1, 64, 16, dtype, seed=B, pad=2).check(4)
+    rows[B - 1] = 140                                     # one prompt block among them
+    Cache(lens, rows, 1, 64, 16, dtype, seed=B, pad=2).check(4, max_rows=140, max_len=5003)
+    Cache(lens, [2] * B, 1, 64, 32, dtype, seed=B).check(4, max_rows=2, max_len=5003, window=700)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
 def test_attention_scale_and_peaked_scores(dtype):
     c = Cache([300, 1], [5, 2], 2, 64, 16, dtype)
     c.check(4, scale=0.01)
@@ -339,6 +363,12 @@ def test_attention_row_offsets_that_make_no_sense():
         row0 = torch.tensor(bad, dtype=torch.int32, device=DEV)
         cs.cs_paged_attention(c.pages, q, row0=row0, out=out)
         cs.cs_paged_append(c.pages, q[:, :2].contiguous(), q[:, :2].contiguous(), row0=row0)
+    c = Cache([3000, 40, 1000] + [9] * 70, [2] * 73, 1, 64, 16, BF)        # with token ranges, and more streams than a wave has lanes
+    q = randn((146, 2, 64), gen(1), BF)
+    for n in (3, 73):
+        p = cs.Pages(c.k, c.v, c.table[:n], c.length[:n])
+        for bad in ([0, 146] * 37, [146 - 2 * b for b in range(74)], [0] * 73 + [146], [(b * 97) % 300 - 50 for b in range(74)]):
+            cs.cs_paged_attention(p, q, row0=torch.tensor(bad[:n + 1], dtype=torch.int32, device=DEV), max_rows=2, max_len=3002)
     torch.cuda.synchronize()
 
 
@@ -522,6 +552,7 @@ def test_two_streams_at_once():
     got = []
     for _ in range(5):
         got.append((cs.cs_paged_attention(a.pages, qa, stream=s1), cs.cs_paged_attention(b.pages, qb, stream=s2.cuda_stream)))
+        got.append((cs.cs_paged_attention(a.pages, qa, stream=0), cs.cs_paged_attention(b.pages, qb, stream=torch.cuda.default_stream())))
     torch.cuda.synchronize()
     for x, y in got:
         assert torch.equal(x, wa) and torch.equal(y, wb)
@@ -558,6 +589,15 @@ def test_pool_beyond_two_to_the_32_bytes():
     row = randn((8, KVH, hd), g, BF)
     cs.cs_paged_append(c.pages, row, -row)
     assert torch.equal(k[9000, :, P - 8:].transpose(0, 1), row) and torch.equal(v[9000, :, P - 8:].transpose(0, 1), -row)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_results_repeat_bit_for_bit(dtype):
+    """Nothing depends on the order in which workgroups finish."""
+    c = Cache([3000, 17, 900], [40, 1, 5], 2, 128, 16, dtype, pad=1)
+    q, got = c.check(8)
+    for _ in range(5):
+        assert torch.equal(cs.cs_paged_attention(c.pages, q, row0=c.row0)[:46], got[:46])
 
 
 def test_no_rows_and_no_streams():

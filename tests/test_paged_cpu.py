@@ -31,7 +31,7 @@ BAD_PAGES = [dict(dtype=2), dict(dtype=-1), dict(reserved=1), dict(batch=-1), di
              dict(table=None), dict(len=None), dict(table_stride=9), dict(head_dim=0), dict(head_dim=60), dict(head_dim=264),
              dict(page_size=8), dict(page_size=48), dict(page_size=0), dict(page_size=65536), dict(table_pages=1 << 27, table_stride=1 << 27),
              dict(k=None), dict(v=None), dict(k=A + 8), dict(v=A + 2), dict(k_page=-8), dict(k_head=4), dict(v_head=-64), dict(v_page=1 << 41),
-             dict(k_token=56), dict(v_token=68), dict(k_token=1 << 30), dict(batch=1 << 17)]
+             dict(k_token=56), dict(v_token=68), dict(k_token=1 << 30), dict(batch=1 << 17), dict(n_kv_heads=4097)]
 
 
 def norm_rope(lib, **kw):
@@ -88,7 +88,7 @@ def test_append_of_16_bit_rows_into_a_float32_cache(lib):
 
 @pytest.mark.parametrize("bad", [dict(q=None), dict(out=None), dict(q=A + 2), dict(out_row=2044), dict(out_head=-64), dict(H=0), dict(H=12),
                                  dict(H=8192), dict(R=-1), dict(row0=None, R=5), dict(scale=0.0), dict(scale=-1.0), dict(scale=float("nan")),
-                                 dict(scale=float("inf")), dict(window=-1), dict(max_rows=-1), dict(max_len=-1), dict(R=1 << 27)], ids=str)
+                                 dict(scale=float("inf")), dict(window=-1), dict(max_rows=-1), dict(max_len=-1), dict(R=1 << 27), dict(R=(1 << 25) + 1)], ids=str)
 def test_attention_refuses(lib, bad):
     assert attention(lib, **bad) in (-2, -6)
 
