@@ -697,7 +697,7 @@ def _dtype(t: torch.Tensor, name: str) -> int:
 def _vec(t: Optional[torch.Tensor], name: str, dtype, n: int):
     if t is None:
         return None
-    if t.dtype != dtype or t.dim() != 1 or t.shape[0] != n or (n > 1 and t.stride(0) != 1):
+    if t.dtype is not dtype or t.numel() != n or not t.is_contiguous():
         raise TypeError(f"{name} must be a contiguous {dtype} tensor of {n} elements")
     return t.data_ptr()
 
@@ -750,25 +750,30 @@ def cs_op_qk_norm_rope(q: torch.Tensor, k: Optional[torch.Tensor] = None, pos: O
     odt = out_dtype or (q.dtype if qo is None else qo.dtype)
     if qo is None:
         qo = q.new_empty(qs, dtype=odt)
+        qop = qo.data_ptr(), H * hd, hd
+    else:
+        qop = _rows3(qo, "q_out", qs)
     kp, kop, KVH = (None, 0, 0), (None, 0, 0), 0
     if k is not None:
         ks = k.shape
         if len(ks) != 3 or ks[0] != R or ks[2] != hd or k.dtype != q.dtype:
             raise ValueError("q and k must have the same rows, head_dim and type")
-        KVH = ks[1]
-        if ko is None:
-            if out is not None:
-                raise ValueError("out must be (q_out, k_out)")
+        KVH, kp = ks[1], _rows3(k, "k", ks)
+        if out is None:
             ko = q.new_empty(ks, dtype=odt)
-        kp, kop = _rows3(k, "k", ks), _rows3(ko, "k_out", ks)
-        if ko.dtype != odt:
-            raise TypeError("q_out and k_out must be of one type, out_dtype if that is given")
+            kop = ko.data_ptr(), KVH * hd, hd
+        elif ko is None:
+            raise ValueError("out must be (q_out, k_out)")
+        else:
+            kop = _rows3(ko, "k_out", ks)
+            if ko.dtype != odt:
+                raise TypeError("q_out and k_out must be of one type, out_dtype if that is given")
     if qo.dtype != odt:
         raise TypeError("q_out and k_out must be of one type, out_dtype if that is given")
     _check(load_library().cs_op_qk_norm_rope(
         dt, _dtype(qo, "q_out"), *qp, *kp, R, H, KVH, hd, _vec(q_gain, "q_gain", torch.float32, hd),
         _vec(k_gain, "k_gain", torch.float32, hd), eps, _vec(pos, "pos", torch.int32, R),
-        _vec(inv_freq, "inv_freq", torch.float64, rot // 2), rot, *_rows3(qo, "q_out", qs), *kop, _stream_of(dev)))
+        _vec(inv_freq, "inv_freq", torch.float64, rot // 2), rot, *qop, *kop, _stream_of(dev)))
     return qo, ko
 
 
