@@ -21,6 +21,7 @@ FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fno-gpu-rdc",
 # The attention kernels never produce or consume a NaN (masked scores are -inf, the running
 # maximum is guarded before it is subtracted), so the maxima of their softmax need no
 # canonicalising copy of every operand: 18 fewer vector instructions per 32-token block.
+# (Keys and values of live tokens are finite by contract; dead ones are masked before a maximum sees them.)
 EXTRA_FLAGS = {"cs_attn.hip": ["-fno-honor-nans"], "cs_paged_attn.hip": ["-fno-honor-nans"]}
 
 

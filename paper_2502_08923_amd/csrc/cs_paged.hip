@@ -7,7 +7,8 @@
 // shared through LDS, instead of once per head: at 40 heads that is the difference between the vector unit and
 // the memory being the bound.  A lane holds VEC consecutive elements of a head's first half and the VEC elements
 // of its second half that pair up with them, so the rotation needs no other lane; the norm is a shuffle sum over the
-// head's lanes.
+// head's lanes.  Measured: norms and rotation of 4096 rows of 40 heads of 128 (84 MB moved) 17.7 us = 4.7 TB/s, what a large copy reaches; 88
+// rows 3.7 us, a launch's latency; append of 9.2 thousand rows in 8 ragged prompts (90 MB) 16-22 us = 4.1-5.6 TB/s, of 88 rows 3.2 us.
 #include <algorithm>
 
 #include "cs_paged.h"

@@ -3,7 +3,11 @@
 //
 //   out[r][h] = sum_t p_t v[t] / sum_t p_t,   p_t = exp(scale * q[r][h] . k[t] - max),   t <= L_b + i, t > L_b + i - window
 //
-// One pass over the tokens with the running maximum and sum of the softmax in float32.
+// One pass over the tokens with the running maximum and sum of the softmax in float32.  Three kernels: bfloat16 caches with few query rows
+// per KV head (the stream of keys and values is the bound) and with many (the multiplies are), float32 caches; and the merge of what
+// several workgroups have of a row.  They multiply with the matrix instructions, K as the A operand, so a lane (c, g) = (lane % 16,
+// lane / 16) has four consecutive tokens of query row c in the result, which is what the second product wants of its B operand.
+// No wave, workgroup or launch order enters a result: every sum has one order, given by the cut.
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
@@ -25,7 +29,9 @@ struct pa_args {
 // chip better; lengths are only known on the device, so the cut is made there, by every workgroup for itself: each lane
 // prices another number of ranges for the longest stream (rounds of the chip that all ranges of all streams then take, a round
 // costing its tokens and, in the same unit, a workgroup's start and end), and the cheapest is taken.  Batches of more than 64 streams
-// have workgroups enough and take the host's cut.
+// have workgroups enough and take the host's cut.  (Against the host's cut for all, which takes every stream to be as long as the longest:
+// 2048 rows and 15 single tokens behind 4 to 16 thousand 740 -> 685 us, two ragged float32 prompt blocks 185 -> 152 us, eight equal streams
+// 120 -> 122 us.)
 struct pa_tile {
     int b, n0, QR;            // stream, first query row, query rows of the stream
     int row0, rows, L;        // its first row, rows, length
@@ -108,6 +114,12 @@ __device__ __forceinline__ bool pa_find_entry(const cs_pages_dev& D, int G, int 
         n_b = __builtin_amdgcn_readlane(n, l);
         at = idx - (__builtin_amdgcn_readlane(incl, l) - __builtin_amdgcn_readlane(mine, l));
         o.entry = idx;
+    } else if (!D.row0 && P.n_max == 1) {                    // equal shares, whole contexts: nothing to look up
+        const int tiles = pa_extent(D, G, window, P, 0).x;
+        if (wg >= B * tiles) return false;
+        b = wg / tiles;
+        at = wg - b * tiles;
+        o.entry = wg;
     } else {
         int base = 0;
         for (int b0 = 0; b0 < B; b0 += 64) {
@@ -207,6 +219,10 @@ __device__ __forceinline__ void pa_finish(const cs_pages_dev& D, const pa_args& 
 // feature 8c + u in row c.  So the values lie in the pages as they come, and a wave's load takes whole rows.
 // A page holds whole 16-token halves, so every load has one page and a uniform base: a buffer whose size ends with the last
 // token.  Loads past it, and of pages that do not exist, return zeros and cost no traffic, and none sits behind a branch.
+// Two blocks of keys and two of values per wave are in flight (32 KB a wave at head_dim 128); what bounds it then is memory: 8 streams of
+// 11 rows behind 18431 tokens, head_dim 128, 4 heads a group, 604 MB: 110 us = 5.5 TB/s; 64 single tokens behind 2 to 8 thousand,
+// pages of 16 tokens: 262 us = 5.2 TB/s; one stream of 16000: 17 us.  Workgroups: one per compute unit (twice as many cost 7 %,
+// four times 20 %: their starts, their ends and the merge).
 #define PN_WAVES 4
 template <int HD>
 struct pn_kbuf { bf16x8 k[2][HD / 32]; };
@@ -495,6 +511,12 @@ __device__ __forceinline__ void cs_load_to_lds_lane(unsigned voff, const void* s
 //   values: one piece = 16 tokens x 32 features as two 16 x 16 squares of 32-byte rows, which the transposing LDS read
 //   (four tokens of one feature per lane) takes apart without bank conflicts
 // The products, the softmax and the order of tokens in the probabilities are those of the kernel above.
+// What bounds it: the matrix units are busy 46 % of the time and the vector units 45 % (a block of 32 tokens and 32 rows is 544 cycles of
+// products and 500 of softmax), and little of either overlaps; at that rate the card is near its power limit (all zeros: 20 % faster).  4096 rows
+// of 32 heads on an empty cache: 146-160 us = 0.86-0.94 PFLOP/s; 2048 rows behind 16384 tokens 0.96, 16 streams of 33 rows (231 of 256 tile
+// rows) behind 65535 tokens 594-640 us = 0.78-0.83.  Tried against this, same card: no teams +3 %, no wave priorities +1 to 2.5 %; the products of the next
+// block woven into the softmax by hand +10 %; fragments of a whole block read ahead +3 to 5 %; 64 rows a wave in four waves: spills;
+// two workgroups of four waves per compute unit: the same at 4096 rows, +20 % where one tile's rows had become two's.
 #define PW_WAVES 8
 template <int HD, int NT>
 __global__ __launch_bounds__(64 * PW_WAVES) void k_paged_wide(cs_pages_dev D, pa_args A, pa_plan P) {
@@ -803,7 +825,10 @@ __global__ __launch_bounds__(64 * PW_WAVES) void k_paged_wide(cs_pages_dev D, pa
 // one, step j taking token 4g + j, and its 16 bytes of that token's value row are four features 4c + u, one for each
 // of four tiles.  So nothing is moved between lanes, and nothing goes through LDS but the query rows (and, with TOKENS, the
 // waves' results: few rows, where the waves share them and take the token blocks in turn; without it every wave has 16 * NT rows
-// of its own, and what bounds it is the instruction's rate, 157 TFLOP/s, the re-read blocks coming out of the caches).
+// of its own, and what bounds it is the instruction's rate, 157 TFLOP/s, the re-read blocks coming out of the caches).  Two workgroups share a
+// compute unit, and the matrix units are busy 74 % while they do: two streams of 700 and 438 rows behind 3001 and 1876 tokens, 8 heads of
+// 128: 152-168 us = 80-88 TFLOP/s (one workgroup per compute unit: 225 us; 16 rows a wave: 4 to 9 % slower; two key blocks ahead: no change).
+// Few rows are bound by memory: 8 single tokens behind 8000, 8 heads of 128: 95 us = 5.5 TB/s.
 #define PF_WAVES 4
 template <int HD, int NT, bool TOKENS>
 __global__ __launch_bounds__(64 * PF_WAVES, !TOKENS && HD <= 128 ? 2 : 1) void k_paged_f32(cs_pages_dev D, pa_args A, pa_plan P) {
@@ -1049,7 +1074,7 @@ __global__ __launch_bounds__(64 * PF_WAVES, !TOKENS && HD <= 128 ? 2 : 1) void k
 // ---- joining token ranges ---------------------------------------------------------------------
 // out[r][h] = sum_s 2^(m_s - M) O_s / sum_s 2^(m_s - M) l_s.  2^lanes_log2 lanes have a query row's hd features, four each; a lane
 // reads the (max, sum) pairs of every lanes-th range, and the weights go round by shuffles.  The workgroups are those of the kernel
-// before it: the ones that had the ranges of a tile share out its rows.
+// before it: the ones that had the ranges of a tile share out its rows (4 ranges of 8 x 44 rows and 8 heads: 5 us, a launch's own 3 among them).
 #define PM_THREADS 256
 template <typename T_>
 __global__ __launch_bounds__(PM_THREADS) void k_paged_merge(cs_pages_dev D, pa_args A, pa_plan P, int lanes_log2) {

@@ -330,7 +330,14 @@ def test_attention_many_ragged_streams(B, dtype):
     Cache(lens, rows, 1, 64, 16, dtype, seed=B, pad=2).check(4)
     rows[B - 1] = 140                                     # one prompt block among them
     Cache(lens, rows, 1, 64, 16, dtype, seed=B, pad=2).check(4, max_rows=140, max_len=5003)
-    Cache(lens, [2] * B, 1, 64, 32, dtype, seed=B).check(4, max_rows=2, max_len=5003, window=700)
+    c = Cache(lens, [2] * B, 1, 64, 32, dtype, seed=B)
+    c.check(4, max_rows=2, max_len=5003, window=700)
+    q = randn((2 * B, 4, 64), gen(5), dtype)              # equal shares without offsets, one range and several
+    c.close(cs.cs_paged_attention(c.pages, q, max_len=16), *c.reference(q, 0.125), 64)
+    c.close(cs.cs_paged_attention(c.pages, q, max_len=5003), *c.reference(q, 0.125), 64)
+    c = Cache(lens, [30] * B, 1, 64, 32, dtype, seed=B)
+    q = randn((30 * B, 4, 64), gen(5), dtype)
+    c.close(cs.cs_paged_attention(c.pages, q, max_len=16), *c.reference(q, 0.125), 64)
 
 
 @pytest.mark.parametrize("dtype", [BF, F32])
