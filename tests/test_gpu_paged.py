@@ -309,6 +309,16 @@ def test_attention_long_contexts(dtype, rows, lens):
     c.check(8, max_rows=rows, max_len=max(lens) + rows)
 
 
+@pytest.mark.parametrize("hd,H,KVH", [(128, 8, 2), (64, 4, 4), (256, 4, 2), (96, 6, 1)])
+@pytest.mark.parametrize("lens,rows", [([0], [985]), ([0, 300], [130, 700]), ([2000, 0, 70], [200, 49, 1]), ([8000], [90])])
+def test_attention_prompt_blocks(lens, rows, hd, H, KVH):
+    """Prompt blocks on empty and on filled caches, alone and ragged: tiles of 128 and of 256 query rows."""
+    c = Cache(lens, rows, KVH, hd, 32, BF, seed=hd, pad=2)
+    c.check(H)
+    c.check(H, max_rows=max(rows), max_len=max(a + b for a, b in zip(lens, rows)))
+    c.check(H, window=100)
+
+
 @pytest.mark.parametrize("dtype", [BF, F32])
 @pytest.mark.parametrize("rows,lens,window", [(1, [30000, 50], 0), (40, [9000], 0), (70, [9000, 9], 0), (300, [7001], 0), (2, [20000], 9000),
                                               (90, [12000], 5000)])
