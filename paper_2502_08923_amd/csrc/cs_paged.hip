@@ -8,7 +8,7 @@
 // the memory being the bound.  A lane holds VEC consecutive elements of a head's first half and the VEC elements
 // of its second half that pair up with them, so the rotation needs no other lane; the norm is a shuffle sum over the
 // head's lanes.  Measured: norms and rotation of 4096 rows of 40 heads of 128 (84 MB moved) 17.7 us = 4.7 TB/s, what a large copy reaches; 88
-// rows 3.7 us, a launch's latency; append of 9.2 thousand rows in 8 ragged prompts (90 MB) 16-22 us = 4.1-5.6 TB/s, of 88 rows 3.2 us.
+// rows 3.7 us, a launch's latency; append of 11 thousand rows in 8 ragged prompts (90 MB) 16-22 us = 4.1-5.6 TB/s, of 88 rows 3.2 us.
 #include <algorithm>
 
 #include "cs_paged.h"
@@ -348,7 +348,7 @@ extern "C" int cs_paged_append(const cs_pages* p, int32_t src_dtype, const void*
     const bool wide = wide_segments(src_dtype, p->head_dim, rot);
     A.segs = p->head_dim / (wide ? 16 : 8);
     A.lanes_log2 = lanes_log2_of(A.segs);
-    // four rows share the look-up of their places, which is a chain of three loads (9.2 thousand rows of 8 heads: 27 us with one row, 22 with
+    // four rows share the look-up of their places, which is a chain of three loads (11 thousand rows of 8 heads: 27 us with one row, 22 with
     // four); few rows are better spread out (88 rows: 4.0 with four, 3.2 with one)
     A.rpw = R >= 1024 ? NR_ROWS : 1;
     const dim3 grid((unsigned)cs_ceil_div(R, A.rpw));

@@ -221,7 +221,7 @@ __device__ __forceinline__ void pa_finish(const cs_pages_dev& D, const pa_args& 
 // token.  Loads past it, and of pages that do not exist, return zeros and cost no traffic, and none sits behind a branch.
 // Two blocks of keys and two of values per wave are in flight (32 KB a wave at head_dim 128); what bounds it then is memory: 8 streams of
 // 11 rows behind 18431 tokens, head_dim 128, 4 heads a group, 604 MB: 110 us = 5.5 TB/s; 64 single tokens behind 2 to 8 thousand,
-// pages of 16 tokens: 262 us = 5.2 TB/s; one stream of 16000: 17 us.  Workgroups: one per compute unit (twice as many cost 7 %,
+// pages of 16 tokens: 262 us = 5.2 TB/s; one stream of 16000: 22 us with the merge.  Workgroups: one per compute unit (twice as many cost 7 %,
 // four times 20 %: their starts, their ends and the merge).
 #define PN_WAVES 4
 template <int HD>
@@ -1074,7 +1074,7 @@ __global__ __launch_bounds__(64 * PF_WAVES, !TOKENS && HD <= 128 ? 2 : 1) void k
 // ---- joining token ranges ---------------------------------------------------------------------
 // out[r][h] = sum_s 2^(m_s - M) O_s / sum_s 2^(m_s - M) l_s.  2^lanes_log2 lanes have a query row's hd features, four each; a lane
 // reads the (max, sum) pairs of every lanes-th range, and the weights go round by shuffles.  The workgroups are those of the kernel
-// before it: the ones that had the ranges of a tile share out its rows (4 ranges of 8 x 44 rows and 8 heads: 5 us, a launch's own 3 among them).
+// before it: the ones that had the ranges of a tile share out its rows (4 ranges of 8 x 44 rows and 8 heads: 6 us, a launch's own 3 among them).
 #define PM_THREADS 256
 template <typename T_>
 __global__ __launch_bounds__(PM_THREADS) void k_paged_merge(cs_pages_dev D, pa_args A, pa_plan P, int lanes_log2) {
@@ -1188,8 +1188,9 @@ static pa_cut pa_make_cut(const cs_pages* p, int H, bool has_row0, int R, int ma
         W.tiles = (int)(has_row0 ? all / W.TR + std::min<int64_t>(B, all / (n_most + 1)) : B * cs_ceil_div(qr, W.TR));
     }
     // The chip's slots: one workgroup per compute unit, two of the float32 kernel for many rows.  What a workgroup's ends and the merge cost
-    // was measured in tokens of each kernel's own pace; between half and twice these figures nothing moves by more than 2 %.
-    c.at_w = f32 ? pa_ranges(N, len, B, KVH, p->head_dim, 256, 128, 384) : pa_ranges(N, len, B, KVH, p->head_dim, 256, 256, 768);
+    // was measured in tokens of each kernel's own pace: twice these figures change no case by more than 1 %, half of them cost up to 5 %
+    // (4096 rows on an empty cache are cut where they should not be).
+    c.at_w = f32 ? pa_ranges(N, len, B, KVH, p->head_dim, 256, 128, 512) : pa_ranges(N, len, B, KVH, p->head_dim, 256, 256, 768);
     c.bytes = c.at_w + (f32 ? pa_ranges(W, len, B, KVH, p->head_dim, 512, 16, 128) : pa_ranges(W, len, B, KVH, p->head_dim, 256, 128, 192));
     return c;
 }
