@@ -428,7 +428,8 @@ int cs_kv_set_len_dev(cs_kv*, const int32_t* d_len /*device [B]*/, int64_t len_u
  *
  * Table entries behind the page of a stream's last token may hold anything.  An entry outside
  * 0 .. n_pages-1 names no page: nothing is written there, and its tokens are not attended to (an
- * evicted page).  Dead slots may hold anything as well; keys and values of live tokens must be finite.  A length is taken as 0 if it is negative, and positions at and beyond
+ * evicted page).  Dead slots may hold anything as well, and so may tokens that have left
+ * the window of a stream's first new row; other keys and values of live tokens must be finite.  A length is taken as 0 if it is negative, and positions at and beyond
  * table_pages * page_size do not exist: their rows are not written, and their tokens not attended to.
  *
  * Rows of a call: R rows in all, those of stream b being d_row0[b] .. d_row0[b+1]-1 (device,

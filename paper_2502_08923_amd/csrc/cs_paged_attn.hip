@@ -253,6 +253,7 @@ __global__ __launch_bounds__(64 * PN_WAVES) void k_paged_narrow(cs_pages_dev D, 
     const int t_end = K.split == K.nsplit - 1 ? n_tok : (int)min((int64_t)w_begin + K.chunk, (int64_t)n_tok);
     // blocks between these need no mask
     const int open_lo = A.window ? T.L + i_hi - A.window + 1 : 0, open_hi = min(T.L + i_lo + 1, D.cap);
+    const int w_first = A.window ? T.L + i_lo - A.window + 1 : 0;       // tokens before it are seen by no row of the tile
 
     // query rows into LDS
     for (int idx = tid; idx < ROWS * (HD / 8); idx += 64 * PN_WAVES) {
@@ -381,6 +382,14 @@ __global__ __launch_bounds__(64 * PN_WAVES) void k_paged_narrow(cs_pages_dev D, 
                             const bool sees = t <= q_last[nt] && t >= q_first[nt] && t < D.cap && (a ? p1 : p0) >= 0;
                             sacc[a][nt][j] = sees ? sacc[a][nt][j] : -INFINITY;
                         }
+                if (t0 < w_first) {                     // (what has left every window may be anything, and 0 * anything must stay 0)
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        const bool gone = t0 + 16 * (j >> 2) + 4 * g + (j & 3) < w_first;
+#pragma unroll
+                        for (int d = 0; d < VD; ++d) vb.v[j][d] = gone ? 0u : vb.v[j][d];
+                    }
+                }
             }
             bool moved = false;
             float alpha[NT];
@@ -540,6 +549,7 @@ __global__ __launch_bounds__(64 * PW_WAVES) void k_paged_wide(cs_pages_dev D, pa
     const int i_lo = T.n0 / G, i_hi = (T.n0 + n_rows - 1) / G;
     const int n_lim = min(T.L + i_hi + 1, D.cap);              // tokens that the tile's last row sees
     const int n_tok = min(T.L + T.rows, D.cap);                // tokens that are there
+    const int w_first = A.window ? T.L + i_lo - A.window + 1 : 0;       // tokens before it are seen by no row of the tile
     const int base = A.window ? max(0, T.L + i_lo - A.window + 1) & ~31 : 0;
     const int w_begin = (int)min((int64_t)base + (int64_t)K.split * K.chunk, (int64_t)n_lim);
     const int t_end = K.split == K.nsplit - 1 ? n_lim : (int)min((int64_t)w_begin + K.chunk, (int64_t)n_lim);
@@ -723,10 +733,13 @@ __global__ __launch_bounds__(64 * PW_WAVES) void k_paged_wide(cs_pages_dev D, pa
                 const unsigned char* p = sp + V_AT + (a * KS + (mt >> 1)) * 1024 + (mt & 1) * 512 + lane * 8;
                 h[a] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(__attribute__((address_space(3))) unsigned char*)p);
                 if (MASKED) {
-                    // what lies behind the last token or in place of a page may be anything, and 0 * anything must stay 0
+                    // what lies behind the last token, in place of a page or before every window may be anything, and 0 * anything
+                    // must stay 0
 #pragma unroll
-                    for (int j = 0; j < 4; ++j)
-                        if (t0 + 16 * a + 4 * g + j >= n_tok || !(a ? ok1 : ok0)) h[a][j] = 0;
+                    for (int j = 0; j < 4; ++j) {
+                        const int t = t0 + 16 * a + 4 * g + j;
+                        if (t >= n_tok || t < w_first || !(a ? ok1 : ok0)) h[a][j] = 0;
+                    }
                 }
             }
             return __builtin_bit_cast(bf16x8, (s16x8){h[0][0], h[0][1], h[0][2], h[0][3], h[1][0], h[1][1], h[1][2], h[1][3]});
@@ -864,6 +877,7 @@ __global__ __launch_bounds__(64 * PF_WAVES, !TOKENS && HD <= 128 ? 2 : 1) void k
     const int p_lo = T.L + (T.n0 + wrow) / G, p_hi = T.L + (T.n0 + wrow + max(w_rows, 1) - 1) / G;
     const int my_end = w_rows ? min(t_end, min(p_hi + 1, D.cap)) : w_begin;
     const int open_lo = A.window ? p_hi - A.window + 1 : 0, open_hi = min(p_lo + 1, D.cap);
+    const int w_first = A.window ? T.L + T.n0 / G - A.window + 1 : 0;   // tokens before it are seen by no row of the tile
     int q_last[NT];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
@@ -960,6 +974,14 @@ __global__ __launch_bounds__(64 * PF_WAVES, !TOKENS && HD <= 128 ? 2 : 1) void k
                         const bool sees = t <= q_last[nt] && (A.window == 0 || t > q_last[nt] - A.window) && t < D.cap && page >= 0;
                         sacc[nt][j] = sees ? sacc[nt][j] : -INFINITY;
                     }
+                if (t0 < w_first) {                     // (what has left every window may be anything, and 0 * anything must stay 0)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+#pragma unroll
+                        for (int x = 0; x < VX; ++x)
+#pragma unroll
+                            for (int u = 0; u < 4; ++u) vb[j][x][u] = t0 + 4 * g + j < w_first ? 0.f : vb[j][x][u];
+                }
             }
             bool moved = false;
             float alpha[NT];

@@ -269,6 +269,21 @@ def test_attention_window(rows, window, dtype):
 
 
 @pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("rows", [1, 11, 70, 150])
+@pytest.mark.parametrize("window", [1, 20, 33, 100])
+def test_attention_behind_the_window_anything(window, rows, dtype):
+    """Tokens that no new row's window reaches any more may hold NaN or infinities."""
+    for hd, P in ((64, 16), (128, 64)):
+        c = Cache([30, 333, 64], [rows] * 3, 2, hd, P, dtype, seed=window)
+        table = c.table.cpu()
+        for b, n in enumerate(c.lens):
+            for t in range(max(0, n - window + 1)):
+                c.k[int(table[b][t // P]), :, t % P] = (math.nan, math.inf, -math.inf)[t % 3]
+                c.v[int(table[b][t // P]), :, t % P] = (math.inf, math.nan, -math.inf)[t % 3]
+        c.check(4, window=window)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
 @pytest.mark.parametrize("rows", [1, 6, 100])
 @pytest.mark.parametrize("P", [16, 32, 64])
 def test_attention_evicted_pages(P, rows, dtype):
