@@ -584,7 +584,8 @@ __global__ __launch_bounds__(64 * PW_WAVES) void k_paged_wide(cs_pages_dev D, pa
     const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)&stage[0][0];
 
     // A lane has one of the next 64 blocks: where in the pool each of the wave's pieces of it starts, so that a request costs the scalar
-    // unit no multiplication.  A half whose page does not exist is read from page 0 and masked.
+    // unit no multiplication.  A half whose page does not exist is read from page 0 and masked: from a whole half of it, also
+    // where a range that lies behind all its tile sees begins at a token that is no multiple of 16.
     const int32_t* tab = D.p.table + T.b * D.p.table_stride;
     unsigned from_lo[LD], from_hi[LD];
     unsigned long long okay0 = 0, okay1 = 0, old0 = 0, old1 = 0;     // halves that exist, of these and of the 64 blocks before
@@ -602,7 +603,7 @@ __global__ __launch_bounds__(64 * PW_WAVES) void k_paged_wide(cs_pages_dev D, pa
 #pragma unroll
         for (int u = 0; u < LD; ++u) {
             const int id = wave + PW_WAVES * u, v = id >= 2 * KS, half = id / KS & 1;
-            const int page = half ? (ok1 ? page1 : 0) : (ok0 ? page0 : 0), slot = (int)(t + 16 * half) & (D.p.page_size - 1);
+            const int page = half ? (ok1 ? page1 : 0) : (ok0 ? page0 : 0), slot = (int)(t + 16 * half) & (D.p.page_size - 16);
             const int64_t at = v ? page * D.p.v_page + kvh * D.p.v_head + slot * D.p.v_token : page * D.p.k_page + kvh * D.p.k_head + slot * D.p.k_token;
             const uint64_t from = (uint64_t)(v ? D.p.v : D.p.k) + 2 * at;
             from_lo[u] = (unsigned)from;

@@ -643,3 +643,20 @@ def test_no_rows_and_no_streams():
     out = q.clone()
     cs.cs_paged_attention(none, q, out=out)
     assert torch.equal(out, q)
+
+
+@pytest.mark.parametrize("hd,H,KVH", [(128, 8, 2), (64, 7, 1), (256, 4, 2)])
+@pytest.mark.parametrize("P,L,rows", [(1024, 683, 336), (2048, 1501, 543), (1024, 1, 1021)])
+def test_attention_pool_of_one_page(P, L, rows, hd, H, KVH):
+    """A pool that ends with its only page, cut into ranges of which the early tiles have nothing: those begin where a tile's
+    tokens end, at no multiple of 16, and what they ask for has to lie in the page all the same."""
+    c = Cache([L], [rows], KVH, hd, P, BF, seed=hd, spare=0)
+    assert c.k.shape[0] == 1
+    q = randn((rows, H, hd), gen(1), BF, 2.0)
+    want = c.reference(q, 1 / math.sqrt(hd))
+    for call in (dict(max_len=L + rows), dict(row0=c.row0), dict(row0=c.row0, max_rows=rows, max_len=L + rows)):
+        c.close(cs.cs_paged_attention(c.pages, q, **call), *want, hd)
+    # the same page named by every entry of a longer table, and an entry that names none
+    twice = torch.tensor([[-1, int(c.table[0, 0]), 1 << 30]], dtype=torch.int32, device=DEV)
+    length = torch.tensor([P + L], dtype=torch.int32, device=DEV)
+    c.close(cs.cs_paged_attention(cs.Pages(c.k, c.v, twice, length), q), *want, hd)
