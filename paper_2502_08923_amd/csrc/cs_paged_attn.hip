@@ -1160,6 +1160,12 @@ struct pa_cut {
 };
 #define PN_MOST 48                // query rows up to which a stream takes the kernel of few rows
 #define PA_MOST_RANGES 256
+// Pairs that there is room for beyond one per tile, in rounds of the chip.  With room for as many as even out the rounds best the
+// partial results, which are the workspace, come to 2.1 GB (3968 rows of 32 heads over a table of 2^20 tokens); with eight rounds they
+// stay under 0.4 GB.  The cut is the same where that was never used (2048 rows of 32 heads behind 129000 tokens, a table of 2^17:
+// 1.1 GB -> 0.3, 3.8 ms); else the rounds are less even, and there is less to join: 11 x 252 float32 rows of 28 heads behind 31225 tokens
+// 9.75 -> 10.2 ms, a float32 block of 1251 rows of 64 heads beside 23 single tokens, all behind 273 to 1090: 1000 -> 784 us.
+#define PA_MOST_ROUNDS 8
 // The host's cut prices the ranges as the device does, with every stream as long as the longest; batches of more than 64 streams take it.
 // For the others it says how many (tile, range) pairs there is room for: one round of the chip, or what the host's cut has.
 // (A workgroup without a pair ends at once, but where one fills a compute unit it waits for its turn.)
@@ -1170,14 +1176,15 @@ static int64_t pa_ranges(pa_part& t, int64_t len, int B, int KVH, int hd, int sl
     // (no ranges where the chip is full twice over, or where even the shortest would not pay for the merge)
     const bool one = items >= 2 * slots || (items <= slots && len <= 64 + join);
     const int most = one ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>(PA_MOST_RANGES, len / 64));
+    const int64_t room = t.tiles + cs_ceil_div((int64_t)PA_MOST_ROUNDS * slots, KVH);
     int64_t best = 0;
     int n_best = 1;
-    for (int n = 1; n <= most; ++n) {
+    for (int n = 1; n <= most && (n == 1 || B <= 64 || (int64_t)t.tiles * n <= room); ++n) {
         const int64_t chunk = cs_round_up(std::max<int64_t>(cs_ceil_div(len, n), 1), 32);
         const int64_t cost = cs_ceil_div(items * n, slots) * (chunk + start) + (n > 1 ? join + n : 0);
         if (n == 1 || cost < best) best = cost, n_best = n, t.chunk = (int)chunk;
     }
-    t.entries = (int)std::max<int64_t>((int64_t)t.tiles * n_best, most > 1 && B <= 64 ? cs_ceil_div(slots, KVH) : 0);
+    t.entries = (int)std::min(room, std::max<int64_t>((int64_t)t.tiles * n_best, most > 1 && B <= 64 ? cs_ceil_div(slots, KVH) : 0));
     t.n_max = B > 64 ? n_best : std::min(most, t.entries);
     t.step = (int)cs_ceil_div(t.n_max, 64);
     return t.n_max > 1 ? cs_round_up((int64_t)t.entries * KVH * t.TR * (hd * 4 + 8), 16) + (int64_t)t.entries * 16 : 0;

@@ -117,3 +117,24 @@ def test_binding_refuses_host_tensors():
 
 def test_struct_layout_matches_the_header():
     assert C.sizeof(cs.cs_pages) == 2 * 8 + 6 * 8 + 3 * 8 + 8 * 4
+
+
+@pytest.mark.parametrize("dtype", [cs.CS_BF16, cs.CS_F32])
+@pytest.mark.parametrize("hd", [64, 128, 256])
+@pytest.mark.parametrize("H,KVH", [(32, 8), (28, 4), (8, 1), (16, 16)])
+def test_the_workspace_does_not_grow_with_the_table(lib, H, KVH, hd, dtype):
+    """Without hints a call has room for token ranges of streams as long as the table.  A partial result of a workgroup is at most
+    256 rows of 128 (or 128 of 256) float32 features with two statistics, 133120 bytes, and there are at most those of
+    the tiles (less than two rounds of the chip, where ranges are cut at all) and of eight more rounds: 10 x 256 (bfloat16; 10 x 512 of half
+    the rows in float32) and less than one for each KV head of a round; the kernel of few rows has at most 48 rows."""
+    few, many = 48 * (min(hd, 128) * 4 + 8) * 2, 133120
+    most = (10 * 256 + KVH) * (few + many) + (1 << 20)
+    d = dict(k_page=KVH * 16 * hd, k_head=16 * hd, k_token=hd, v_page=KVH * 16 * hd, v_head=16 * hd, v_token=hd, n_kv_heads=KVH,
+             head_dim=hd, dtype=dtype)
+    for table in (1 << 10, 1 << 13, 1 << 16, 1 << 20):
+        for batch in (1, 3, 16, 64, 65, 100, 300):
+            p = pages(batch=batch, table_pages=table, table_stride=table, **d)
+            for R in (1, 7, 64, 300, 520, 1040, 1488, 2048, 2976, 3968, 5000, 40000):
+                for has_row0, rows in ((1, R), (0, R * batch)):
+                    need = lib.cs_paged_attention_workspace(C.byref(p), H, has_row0, rows, 0, 0)
+                    assert 0 <= need <= most, (table, batch, R, has_row0, need)
