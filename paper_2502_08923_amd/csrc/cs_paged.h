@@ -21,6 +21,14 @@ __device__ __forceinline__ int2 cs_stream_rows(const cs_pages_dev& d, int b) {
 }
 __device__ __forceinline__ int cs_stream_len(const cs_pages_dev& d, int b) { return min(max(d.p.len[b], 0), d.cap); }
 
+// A launch takes fewer than 2^32 threads along a dimension of its grid: workgroups from 2^CS_GRID_LOG2 on (512 threads: 2^31) stand along z.
+// Numbers past the last one come up there, and have no work.
+#define CS_GRID_LOG2 22
+static inline dim3 cs_paged_grid(int64_t n, unsigned y = 1) {
+    return n >> CS_GRID_LOG2 ? dim3(1u << CS_GRID_LOG2, y, (unsigned)cs_ceil_div(n, 1 << CS_GRID_LOG2)) : dim3((unsigned)n, y);
+}
+__device__ __forceinline__ unsigned cs_paged_wg() { return blockIdx.x | blockIdx.z << CS_GRID_LOG2; }
+
 // cos and sin of pos * inv_freq.  The angle is formed in turns in float64 and reduced there to an eighth of a
 // turn around the nearest quarter, so far positions lose nothing (at position 2^20 the float32 product would be off by
 // 1/16 rad); what is left goes through the Taylor series in float32, whose first dropped terms are 1.8e-9

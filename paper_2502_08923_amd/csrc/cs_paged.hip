@@ -146,7 +146,7 @@ template <typename TI, typename TO, int VEC>
 __global__ __launch_bounds__(NR_THREADS) void k_qk_norm_rope(nr_args A) {
     __shared__ float2 turn[NR_ROWS * 128];
     const int tid = threadIdx.x;
-    const int r0 = blockIdx.x * A.rpw, nr = min(A.rpw, A.R - r0), heads = A.H + A.KVH;
+    const int r0 = (int)cs_paged_wg() * A.rpw, nr = min(A.rpw, A.R - r0), heads = A.H + A.KVH;
     const int seg = tid & ((1 << A.lanes_log2) - 1), per_pass = NR_THREADS >> A.lanes_log2;
     // one task = one head of one row; the heads of a launch's second grid dimension are shared out in turn
     const int n_tasks = nr * heads, first = blockIdx.y * per_pass + (tid >> A.lanes_log2), step = gridDim.y * per_pass;
@@ -249,7 +249,7 @@ extern "C" int cs_op_qk_norm_rope(int32_t in_dtype, int32_t out_dtype, const voi
     // pass over them more than once (88 rows of 40 heads: 4.6 -> 3.7 us with two; 4096 rows: 21.0 -> 17.7 us with four rows and two workgroups
     // against four rows and one, 19.9 with one row; 1531 float32 rows of 32 heads: 13.8 with four rows, 10.1 with two).
     A.rpw = R >= 2048 ? NR_ROWS : R >= 1024 ? 2 : 1;
-    const dim3 grid((unsigned)cs_ceil_div(R, A.rpw), H + KVH > NR_THREADS >> A.lanes_log2 ? 2 : 1);
+    const dim3 grid = cs_paged_grid(cs_ceil_div(R, A.rpw), H + KVH > NR_THREADS >> A.lanes_log2 ? 2 : 1);
     hipStream_t s = (hipStream_t)stream;
     if (in_dtype == CS_BF16 && wide) k_qk_norm_rope<bf16_t, bf16_t, 8><<<grid, NR_THREADS, 0, s>>>(A);
     else if (in_dtype == CS_BF16) k_qk_norm_rope<bf16_t, bf16_t, 4><<<grid, NR_THREADS, 0, s>>>(A);
@@ -284,7 +284,7 @@ __global__ __launch_bounds__(NR_THREADS) void k_paged_append(cs_pages_dev D, ap_
     __shared__ float2 turn[NR_ROWS * 128];
     __shared__ int2 dest[NR_ROWS];              // (page, position) of a row, page -1: nowhere
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int r0 = blockIdx.x * A.rpw, nr = min(A.rpw, D.R - r0), KVH = D.p.n_kv_heads, heads = 2 * KVH;
+    const int r0 = (int)cs_paged_wg() * A.rpw, nr = min(A.rpw, D.R - r0), KVH = D.p.n_kv_heads, heads = 2 * KVH;
     const int seg = tid & ((1 << A.lanes_log2) - 1), per_pass = NR_THREADS >> A.lanes_log2;
     const int n_tasks = nr * heads, first = blockIdx.y * per_pass + (tid >> A.lanes_log2), step = gridDim.y * per_pass;
     int lo, hi, ang;
@@ -351,7 +351,7 @@ extern "C" int cs_paged_append(const cs_pages* p, int32_t src_dtype, const void*
     // four rows share the look-up of their places, which is a chain of three loads (11 thousand rows of 8 heads: 27 us with one row, 22 with
     // four); few rows are better spread out (88 rows: 4.0 with four, 3.2 with one)
     A.rpw = R >= 1024 ? NR_ROWS : 1;
-    const dim3 grid((unsigned)cs_ceil_div(R, A.rpw));
+    const dim3 grid = cs_paged_grid(cs_ceil_div(R, A.rpw));
     hipStream_t s = (hipStream_t)stream;
     if (src_dtype == CS_BF16 && wide) k_paged_append<bf16_t, bf16_t, 8><<<grid, NR_THREADS, 0, s>>>(D, A);
     else if (src_dtype == CS_BF16) k_paged_append<bf16_t, bf16_t, 4><<<grid, NR_THREADS, 0, s>>>(D, A);

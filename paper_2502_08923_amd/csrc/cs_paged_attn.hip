@@ -240,9 +240,10 @@ __global__ __launch_bounds__(64 * PN_WAVES) void k_paged_narrow(cs_pages_dev D, 
     __shared__ __attribute__((aligned(16))) unsigned char smem[MERGE_BYTES > Q_BYTES ? MERGE_BYTES : Q_BYTES];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int c = lane & 15, g = lane >> 4;
-    const int KVH = D.p.n_kv_heads, kvh = blockIdx.x % KVH;
+    const unsigned wg = cs_paged_wg();
+    const int KVH = D.p.n_kv_heads, kvh = wg % KVH;
     pa_work K;
-    if (!pa_find(D, A.G, A.window, P, blockIdx.x / KVH, kvh, K)) return;
+    if (!pa_find(D, A.G, A.window, P, wg / KVH, kvh, K)) return;
     const pa_tile& T = K.T;
     const int hd = D.p.head_dim;
     const int n_rows = min(ROWS, T.QR - T.n0);          // live query rows of the tile
@@ -540,9 +541,10 @@ __global__ __launch_bounds__(64 * PW_WAVES) void k_paged_wide(cs_pages_dev D, pa
     const int c = lane & 15, g = lane >> 4;
     const int KVH = D.p.n_kv_heads;
     // KV heads in turn, so that with eight of them each stays on one die and its cache
-    const int kvh = blockIdx.x % KVH;
+    const unsigned wg = cs_paged_wg();
+    const int kvh = wg % KVH;
     pa_work K;
-    if (!pa_find(D, A.G, A.window, P, blockIdx.x / KVH, kvh, K)) return;
+    if (!pa_find(D, A.G, A.window, P, wg / KVH, kvh, K)) return;
     const pa_tile& T = K.T;
     const int hd = D.p.head_dim, G = A.G;
     const int n_rows = min(TR, T.QR - T.n0);
@@ -852,9 +854,10 @@ __global__ __launch_bounds__(64 * PF_WAVES, !TOKENS && HD <= 128 ? 2 : 1) void k
     __shared__ __attribute__((aligned(16))) float smem[MERGE_FLOATS > Q_FLOATS ? MERGE_FLOATS : Q_FLOATS];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int c = lane & 15, g = lane >> 4;
-    const int KVH = D.p.n_kv_heads, kvh = blockIdx.x % KVH;
+    const unsigned wg = cs_paged_wg();
+    const int KVH = D.p.n_kv_heads, kvh = wg % KVH;
     pa_work K;
-    if (!pa_find(D, A.G, A.window, P, blockIdx.x / KVH, kvh, K)) return;
+    if (!pa_find(D, A.G, A.window, P, wg / KVH, kvh, K)) return;
     const pa_tile& T = K.T;
     const int hd = D.p.head_dim, G = A.G;
     const int n_rows = min(TR, T.QR - T.n0);
@@ -1236,17 +1239,17 @@ extern "C" int64_t cs_paged_attention_workspace(const cs_pages* p, int32_t n_hea
 }
 
 template <int HD, int NT>
-static int pn_launch(const cs_pages_dev& D, const pa_args& A, const pa_plan& P, unsigned grid, hipStream_t s) {
+static int pn_launch(const cs_pages_dev& D, const pa_args& A, const pa_plan& P, dim3 grid, hipStream_t s) {
     k_paged_narrow<HD, NT><<<grid, 64 * PN_WAVES, 0, s>>>(D, A, P);
     return cs_launch_ok("k_paged_narrow");
 }
 template <int HD, int NT, bool TOKENS>
-static int pf_launch(const cs_pages_dev& D, const pa_args& A, const pa_plan& P, unsigned grid, hipStream_t s) {
+static int pf_launch(const cs_pages_dev& D, const pa_args& A, const pa_plan& P, dim3 grid, hipStream_t s) {
     k_paged_f32<HD, NT, TOKENS><<<grid, 64 * PF_WAVES, 0, s>>>(D, A, P);
     return cs_launch_ok("k_paged_f32");
 }
 template <int HD, int NT>
-static int pw_launch(const cs_pages_dev& D, const pa_args& A, const pa_plan& P, unsigned grid, hipStream_t s) {
+static int pw_launch(const cs_pages_dev& D, const pa_args& A, const pa_plan& P, dim3 grid, hipStream_t s) {
     k_paged_wide<HD, NT><<<grid, 64 * PW_WAVES, 0, s>>>(D, A, P);
     return cs_launch_ok("k_paged_wide");
 }
@@ -1257,8 +1260,8 @@ static pa_plan pa_plan_of(const pa_part& t, char* ws, int KVH, int hd) {
     return {t.TR, t.qr_lo, t.qr_hi, t.slots, t.start, t.join, t.n_max, t.step, t.chunk, t.entries, po, pml,
             (int4*)(ws + cs_round_up(rows * (hd * 4 + 8), 16))};
 }
-static int pm_launch(const cs_pages_dev& D, const pa_args& A, const pa_plan& P, unsigned grid, hipStream_t s) {
-    if (P.n_max <= 1) return CS_OK;
+static int pm_launch(const cs_pages_dev& D, const pa_args& A, const pa_plan& P, dim3 grid, hipStream_t s) {
+    if (P.n_max <= 1) return CS_OK;        // (with ranges a grid is some rounds of the chip: it needs x only)
     int lanes = 0;
     while (4 << lanes < D.p.head_dim) ++lanes;
     if (D.p.dtype == CS_F32) k_paged_merge<float><<<grid, PM_THREADS, 0, s>>>(D, A, P, lanes);
@@ -1292,7 +1295,7 @@ extern "C" int cs_paged_attention(const cs_pages* p, const void* q, int64_t q_ro
     int rc = CS_OK;
     if (grid_w) {
         const pa_plan P = pa_plan_of(c.wide, (char*)workspace + c.at_w, p->n_kv_heads, p->head_dim);
-        const unsigned n = (unsigned)grid_w;
+        const dim3 n = cs_paged_grid(grid_w);
         if (f32) rc = c.hdt == 64 ? pf_launch<64, 2, false>(D, A, P, n, s) : c.hdt == 128 ? pf_launch<128, 2, false>(D, A, P, n, s) : pf_launch<256, 1, false>(D, A, P, n, s);
         else if (c.wide.nt == 2) rc = c.hdt == 64 ? pw_launch<64, 2>(D, A, P, n, s) : pw_launch<128, 2>(D, A, P, n, s);
         else rc = c.hdt == 64 ? pw_launch<64, 1>(D, A, P, n, s) : c.hdt == 128 ? pw_launch<128, 1>(D, A, P, n, s) : pw_launch<256, 1>(D, A, P, n, s);
@@ -1301,7 +1304,7 @@ extern "C" int cs_paged_attention(const cs_pages* p, const void* q, int64_t q_ro
     }
     if (grid_n) {
         const pa_plan P = pa_plan_of(c.narrow, (char*)workspace, p->n_kv_heads, p->head_dim);
-        const unsigned n = (unsigned)grid_n;
+        const dim3 n = cs_paged_grid(grid_n);
 #define PN(HD_, NT_) if (c.hdt == HD_ && c.narrow.nt == NT_) rc = f32 ? pf_launch<HD_, NT_, true>(D, A, P, n, s) : pn_launch<HD_, NT_>(D, A, P, n, s)
         PN(64, 1); PN(64, 2); PN(64, 3); PN(128, 1); PN(128, 2); PN(128, 3); PN(256, 1);
 #undef PN

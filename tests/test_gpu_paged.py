@@ -660,3 +660,51 @@ def test_attention_pool_of_one_page(P, L, rows, hd, H, KVH):
     twice = torch.tensor([[-1, int(c.table[0, 0]), 1 << 30]], dtype=torch.int32, device=DEV)
     length = torch.tensor([P + L], dtype=torch.int32, device=DEV)
     c.close(cs.cs_paged_attention(cs.Pages(c.k, c.v, twice, length), q), *want, hd)
+
+
+# ------------------------------------------------------------------------------------------------------
+# the largest numbers of rows and workgroups
+# ------------------------------------------------------------------------------------------------------
+
+def test_norm_rope_and_append_of_the_most_rows():
+    """2^26 rows: their workgroups of four rows have 2^32 threads."""
+    R, hd, P = 1 << 26, 8, 32768
+    g, f = gen(3), inv_freq_of(hd)
+    x = randn((1, 1, hd), g, F32).expand(R, 1, hd)                        # one row, R times
+    pos = torch.arange(R, device=DEV, dtype=torch.int32)
+    out = torch.full((R, 1, hd), 9.0, dtype=BF, device=DEV)
+    cs.cs_op_qk_norm_rope(x, None, pos, f, out=(out, None))
+    some = torch.tensor([0, 1, (1 << 24) - 1, 1 << 24, (1 << 24) + 1, R // 2, R - 5, R - 4, R - 1], device=DEV)
+    want, bound = ref_norm_rope(x[some], None, pos[some], f, 0.0)
+    # (a position of 26 bits: two roundings of 2^-53 in the angle on either side, as for far positions)
+    tol = bound * (1 + HALF[BF]) + want.abs() * HALF[BF] + x[some].double().abs().amax() * 8 * R * 2.0 ** -53
+    assert bool(((out[some].double() - want).abs() <= tol).all())
+    assert not bool((out == 9.0).all(-1).any())
+    del out
+    k, v = randn((1, 1, hd), g, BF).expand(R, 1, hd), randn((1, 1, hd), g, BF).expand(R, 1, hd)
+    pool = torch.zeros((2, 2, 1, P, hd), dtype=BF, device=DEV)
+    table = torch.full((1, R // P), -1, dtype=torch.int32, device=DEV)    # only the first and the last page exist
+    table[0, 0], table[0, -1] = 1, 0
+    cs.cs_paged_append(cs.Pages(pool[0], pool[1], table, torch.zeros(1, dtype=torch.int32, device=DEV)), k, v)
+    assert torch.equal(pool[0], k[:1].expand(2, 1, P, hd)) and torch.equal(pool[1], v[:1].expand(2, 1, P, hd))
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_attention_of_the_most_workgroups(dtype):
+    """65536 streams of 256 KV heads, one token each: 2^24 workgroups of 256 threads.  All streams have the same page."""
+    B, H, hd, P, L = 65536, 256, 8, 16, 3
+    g = gen(4)
+    k, v = randn((1, H, P, hd), g, dtype), randn((1, H, P, hd), g, dtype)
+    pages = cs.Pages(k, v, torch.zeros((B, 1), dtype=torch.int32, device=DEV), torch.full((B,), L, dtype=torch.int32, device=DEV))
+    q = randn((B, H, hd), g, dtype)
+    out = cs.cs_paged_attention(pages, q, max_rows=1, max_len=P)
+    c = Cache([L], [1], H, hd, P, dtype)
+    x = q.double()                                                        # all of them against the definition
+    s = torch.stack([(x * k[0, :, t].double()).sum(-1) for t in range(L + 1)]) / math.sqrt(hd)
+    d = torch.stack([(x * k[0, :, t].double()).abs().sum(-1) for t in range(L + 1)]).amax(0) / math.sqrt(hd)
+    p = torch.softmax(s, 0)
+    want, mag = torch.zeros_like(x), torch.zeros_like(x)
+    for t in range(L + 1):
+        want += p[t][..., None] * v[0, :, t].double()
+        mag += p[t][..., None] * v[0, :, t].double().abs()
+    c.close(out, want, mag, d[..., None], hd)
