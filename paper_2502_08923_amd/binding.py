@@ -656,6 +656,13 @@ def _device_of(tensors) -> int:
     return dev
 
 
+def _forward_only(*tensors):
+    """There is no backward pass: a gradient that a caller expects is refused, not lost."""
+    for t in tensors:
+        if t is not None and t.requires_grad and torch.is_grad_enabled():
+            raise RuntimeError("the operators of a paged cache have no gradients: call them under torch.no_grad(), or detach the tensors")
+
+
 @contextlib.contextmanager
 def _on(dev: int, stream):
     """The tensors' device is the current one, and `stream` its current stream (also what new tensors belong to)."""
@@ -706,9 +713,10 @@ class Pages:
     """cs_pages: the caller's pools, page table and lengths of one layer of a paged cache.  k and v: [n_pages][n_kv_heads]
     [page_size][head_dim], bfloat16 or float32, any strides with contiguous head rows (a token-major pool is passed
     transposed); table: int32 [batch][pages]; length: int32 [batch].  The tensors stay the caller's: tables and lengths
-    may be changed in place between calls."""
+    may be changed in place between calls.  Inference only: tensors that require gradients are refused while autograd records."""
 
     def __init__(self, k: torch.Tensor, v: torch.Tensor, table: torch.Tensor, length: torch.Tensor):
+        _forward_only(k, v)
         self.device = _device_of((k, v, table, length))
         if k.dim() != 4 or k.shape != v.shape or k.dtype != v.dtype or k.dtype not in _DTYPES:
             raise TypeError("k and v must be [n_pages][n_kv_heads][page_size][head_dim] of one type, float32 or bfloat16")
@@ -737,6 +745,7 @@ def cs_op_qk_norm_rope(q: torch.Tensor, k: Optional[torch.Tensor] = None, pos: O
     pos[r] * inv_freq[j] (float64 [rot/2]; None: no rotation).  Returns (q, k) rows in new tensors, or in
     out = (q_out, k_out), which may be the inputs."""
     qo, ko = out if out is not None else (None, None)
+    _forward_only(q, k, q_gain, k_gain)
     dev = _device_of((q, k, pos, inv_freq, q_gain, k_gain, qo, ko))
     if _elsewhere(dev, stream):
         with _on(dev, stream):
@@ -781,6 +790,7 @@ def cs_paged_append(pages: Pages, k: torch.Tensor, v: torch.Tensor, row0: Option
                     inv_freq: Optional[torch.Tensor] = None, stream=None):
     """New rows k, v [R][KVH][hd] into the pages of their streams, at positions length[b] + i; keys are rotated on the way
     if inv_freq (float64 [rot/2]) is given.  row0: int32 [batch + 1] offsets of the streams' rows, None: equal shares."""
+    _forward_only(k, v)
     dev = _device_of((pages.k, k, v, row0, inv_freq))
     if _elsewhere(dev, stream):
         with _on(dev, stream):
@@ -810,6 +820,7 @@ def cs_paged_attention(pages: Pages, q: torch.Tensor, row0: Optional[torch.Tenso
     stream are left as they were).  scale: 1/sqrt(head_dim) by default.  max_rows, max_len: hints, see copyspec.h.
     workspace: a contiguous tensor of at least the size that cs_paged_attention_workspace gives; by default one is allocated
     for the call."""
+    _forward_only(q)
     dev = _device_of((pages.k, q, row0, out, workspace))
     if _elsewhere(dev, stream):
         with _on(dev, stream):

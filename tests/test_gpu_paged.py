@@ -708,3 +708,17 @@ def test_attention_of_the_most_workgroups(dtype):
         want += p[t][..., None] * v[0, :, t].double()
         mag += p[t][..., None] * v[0, :, t].double().abs()
     c.close(out, want, mag, d[..., None], hd)
+
+
+def test_parameters_without_autograd():
+    """Gains and rows that are parameters of a model give what plain tensors give, where no gradient is recorded."""
+    g = gen(6)
+    q, gain = randn((5, 4, 64), g, BF), 1 + 0.1 * randn((64,), g, F32)
+    want, _ = cs.cs_op_qk_norm_rope(q, q_gain=gain)
+    p, pg = torch.nn.Parameter(q.clone()), torch.nn.Parameter(gain.clone())
+    with pytest.raises(RuntimeError):
+        cs.cs_op_qk_norm_rope(p, q_gain=pg)
+    for mode in (torch.no_grad, torch.inference_mode):
+        with mode():
+            assert torch.equal(cs.cs_op_qk_norm_rope(p, q_gain=pg)[0], want)
+    assert torch.equal(cs.cs_op_qk_norm_rope(p.detach(), q_gain=pg.detach())[0], want)

@@ -138,3 +138,19 @@ def test_the_workspace_does_not_grow_with_the_table(lib, H, KVH, hd, dtype):
                 for has_row0, rows in ((1, R), (0, R * batch)):
                     need = lib.cs_paged_attention_workspace(C.byref(p), H, has_row0, rows, 0, 0)
                     assert 0 <= need <= most, (table, batch, R, has_row0, need)
+
+
+def test_binding_refuses_tensors_that_want_gradients():
+    """Refused before the devices are looked at; without autograd the host tensors are what is refused."""
+    x = torch.zeros((2, 4, 64), requires_grad=True)
+    y, gain = torch.zeros((2, 4, 64)), torch.ones(64, requires_grad=True)
+    pool = torch.zeros((4, 1, 16, 64))
+    calls = [lambda: cs.cs_op_qk_norm_rope(x), lambda: cs.cs_op_qk_norm_rope(y, x), lambda: cs.cs_op_qk_norm_rope(y, q_gain=gain),
+             lambda: cs.cs_op_qk_norm_rope(y, y, k_gain=gain), lambda: cs.cs_paged_append(None, x, y), lambda: cs.cs_paged_append(None, y, x),
+             lambda: cs.cs_paged_attention(None, x),
+             lambda: cs.Pages(pool.clone().requires_grad_(), pool, torch.zeros((1, 2), dtype=torch.int32), torch.zeros(1, dtype=torch.int32))]
+    for call in calls:
+        with pytest.raises(RuntimeError, match="no gradients"):
+            call()
+    with torch.no_grad(), pytest.raises(TypeError, match="CUDA"):
+        cs.cs_op_qk_norm_rope(x)
