@@ -682,6 +682,13 @@ def _elsewhere(dev: int, stream) -> bool:
     return stream is not None or _current_device() != dev
 
 
+def _fits(*sizes):
+    """Sizes of the C entries are 32 bits wide; ctypes would pass the low ones of a larger number."""
+    for n in sizes:
+        if not -0x80000000 <= n <= 0x7fffffff:
+            raise ValueError(f"a size of {n} does not fit 32 bits")
+
+
 def _stream_of(dev: int) -> int:
     return _raw_stream(dev) if _raw_stream else torch.cuda.current_stream(dev).cuda_stream
 
@@ -725,6 +732,7 @@ class Pages:
         if table.dtype != torch.int32 or table.dim() != 2 or (table.shape[1] > 1 and table.stride(1) != 1):
             raise TypeError("table must be int32 [batch][pages] with contiguous rows")
         _vec(length, "length", torch.int32, table.shape[0])
+        _fits(*k.shape, *table.shape)
         self.k, self.v, self.table, self.length = k, v, table, length
         self.dtype = k.dtype
         st = [[t.stride(d) if t.shape[d] > 1 else (0 if d < 2 else t.shape[3]) for d in range(3)] for t in (k, v)]
@@ -753,6 +761,7 @@ def cs_op_qk_norm_rope(q: torch.Tensor, k: Optional[torch.Tensor] = None, pos: O
     qs = q.shape
     dt, qp = _dtype(q, "q"), _rows3(q, "q", qs)
     R, H, hd = qs
+    _fits(R, H, hd)
     rot = 0 if inv_freq is None else 2 * inv_freq.numel()
     if rot and pos is None:
         raise ValueError("a rotation needs positions")
@@ -768,6 +777,7 @@ def cs_op_qk_norm_rope(q: torch.Tensor, k: Optional[torch.Tensor] = None, pos: O
         if len(ks) != 3 or ks[0] != R or ks[2] != hd or k.dtype != q.dtype:
             raise ValueError("q and k must have the same rows, head_dim and type")
         KVH, kp = ks[1], _rows3(k, "k", ks)
+        _fits(KVH)
         if out is None:
             ko = q.new_empty(ks, dtype=odt)
             kop = ko.data_ptr(), KVH * hd, hd
@@ -796,6 +806,7 @@ def cs_paged_append(pages: Pages, k: torch.Tensor, v: torch.Tensor, row0: Option
         with _on(dev, stream):
             return cs_paged_append(pages, k, v, row0, inv_freq)
     R, c = k.shape[0], pages.c
+    _fits(R)
     want = (R, c.n_kv_heads, c.head_dim)
     dt = _dtype(k, "k")
     if v.dtype != k.dtype:
@@ -807,6 +818,7 @@ def cs_paged_append(pages: Pages, k: torch.Tensor, v: torch.Tensor, row0: Option
 
 def cs_paged_attention_workspace(pages: Pages, n_heads: int, R: int, row0: bool = False, max_rows: int = 0, max_len: int = 0) -> int:
     """Bytes that cs_paged_attention needs for these arguments (row0: whether it is given offsets)."""
+    _fits(n_heads, R, max_rows)
     need = load_library().cs_paged_attention_workspace(pages.ref, n_heads, 1 if row0 else 0, R, max_rows, max_len)
     if need < 0:
         _check(need)
@@ -828,6 +840,7 @@ def cs_paged_attention(pages: Pages, q: torch.Tensor, row0: Optional[torch.Tenso
     qs, c = q.shape, pages.c
     qp = _rows3(q, "q", qs)
     R, H, hd = qs
+    _fits(R, H, window, max_rows)
     if q.dtype != pages.dtype or hd != c.head_dim:
         raise TypeError(f"q must have the cache's type and head_dim, {pages.dtype} and {c.head_dim}")
     if out is None:

@@ -722,3 +722,21 @@ def test_parameters_without_autograd():
         with mode():
             assert torch.equal(cs.cs_op_qk_norm_rope(p, q_gain=pg)[0], want)
     assert torch.equal(cs.cs_op_qk_norm_rope(p.detach(), q_gain=pg.detach())[0], want)
+
+
+def test_sizes_that_need_more_than_32_bits_are_refused():
+    """The C entries take 32 bits: a larger number is not cut to its low bits (2^32 + 5 would be a window of 5)."""
+    c = Cache([40, 3], [2, 2], 2, 64, 16, BF)
+    q = randn((4, 4, 64), gen(1), BF)
+    one = q[:1, :2]
+    many = one.expand((1 << 32) + 1, 2, 64)                               # (a view: one row)
+    out = torch.empty_like(q)
+    big = (1 << 32) + 5
+    for call in (lambda: cs.cs_paged_attention(c.pages, q, window=big, out=out), lambda: cs.cs_paged_attention(c.pages, q, max_rows=big, out=out),
+                 lambda: cs.cs_paged_attention(c.pages, many, out=many), lambda: cs.cs_paged_append(c.pages, many, many),
+                 lambda: cs.cs_op_qk_norm_rope(many, out=(many, None)), lambda: cs.cs_paged_attention_workspace(c.pages, 4, big),
+                 lambda: cs.cs_op_qk_norm_rope(one, one[:, :1].expand(1, big, 64), out=(out[:1, :2], one[:, :1].expand(1, big, 64))),
+                 lambda: cs.Pages(c.k[:1].expand(big, *c.k.shape[1:]), c.v[:1].expand(big, *c.v.shape[1:]), c.table, c.length)):
+        with pytest.raises(ValueError, match="32 bits"):
+            call()
+    assert torch.equal(cs.cs_paged_attention(c.pages, q, window=(1 << 31) - 1), cs.cs_paged_attention(c.pages, q))
