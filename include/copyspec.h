@@ -441,7 +441,9 @@ int cs_kv_set_len_dev(cs_kv*, const int32_t* d_len /*device [B]*/, int64_t len_u
  * n_kv_heads, table_pages * page_size <= 2^30, batch <= 65536, heads <= 4096, R <= 2^26 and, for the attention,
  * R * n_heads <= 2^30.  Every pointer to rows or pools is aligned to 16 bytes, every
  * stride (in elements, >= 0, at most 2^40) is a multiple of 16 bytes; the elements of one head's row are contiguous.
- * token_stride * page_size elements of a pool must stay below 2^31 bytes.
+ * token_stride * page_size elements of a pool must stay below 2^31 bytes.  What is read may be broadcast (a
+ * stride of 0); what is written (outputs; the pools of cs_paged_append) may not: its strides are at least head_dim, where there
+ * is more than one to step over.
  * ---------------------------------------------------------------------------------- */
 typedef struct cs_pages {
     void *k, *v;                            /* device pools of one layer, elements of `dtype` */

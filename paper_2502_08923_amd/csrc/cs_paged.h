@@ -48,5 +48,7 @@ __device__ __forceinline__ float2 cs_turn(int pos, double inv_freq) {
 int cs_check_pages(const char* who, const cs_pages* p);
 // fills d from checked arguments; CS_E_ARG if R rows cannot be shared out
 int cs_pages_view(const char* who, const cs_pages* p, const int32_t* d_row0, int32_t R, cs_pages_dev* d);
+// strides of what a call writes: n0 rows, pages .. and n1 heads that lie apart (a stride that is never taken may be anything)
+int cs_check_apart(const char* who, const char* name, int64_t stride0, int64_t n0, int64_t stride1, int64_t n1, int head_dim);
 // base pointer and two strides of a tensor of rows of heads
 int cs_check_rows(const char* who, const char* name, const void* base, int64_t row, int64_t head, size_t esz);

@@ -25,6 +25,12 @@ int cs_check_rows(const char* who, const char* name, const void* base, int64_t r
     return CS_OK;
 }
 
+int cs_check_apart(const char* who, const char* name, int64_t stride0, int64_t n0, int64_t stride1, int64_t n1, int head_dim) {
+    CS_REQUIRE((n0 < 2 || stride0 >= head_dim) && (n1 < 2 || stride1 >= head_dim), CS_E_ARG,
+               "%s: a stride of %s is less than head_dim: what the call writes would overlap itself", who, name);
+    return CS_OK;
+}
+
 int cs_check_pages(const char* who, const cs_pages* p) {
     CS_REQUIRE(p, CS_E_ARG, "%s: NULL pages", who);
     CS_REQUIRE(p->dtype == CS_F32 || p->dtype == CS_BF16, CS_E_ARG, "%s: unknown dtype %d", who, p->dtype);
@@ -232,9 +238,11 @@ extern "C" int cs_op_qk_norm_rope(int32_t in_dtype, int32_t out_dtype, const voi
     const size_t isz = in_dtype == CS_BF16 ? 2 : 4, osz = out_dtype == CS_BF16 ? 2 : 4;
     CS_TRY(cs_check_rows(who, "q", q, q_row, q_head, isz));
     CS_TRY(cs_check_rows(who, "q_out", q_out, q_out_row, q_out_head, osz));
+    CS_TRY(cs_check_apart(who, "q_out", q_out_row, R, q_out_head, H, head_dim));
     if (KVH) {
         CS_TRY(cs_check_rows(who, "k", k, k_row, k_head, isz));
         CS_TRY(cs_check_rows(who, "k_out", k_out, k_out_row, k_out_head, osz));
+        CS_TRY(cs_check_apart(who, "k_out", k_out_row, R, k_out_head, KVH, head_dim));
     }
     CS_REQUIRE((((uintptr_t)q_gain | (uintptr_t)(KVH ? k_gain : nullptr)) & 15) == 0, CS_E_ARG, "%s: gains are not aligned to 16 bytes", who);
     nr_args A;
@@ -344,6 +352,8 @@ extern "C" int cs_paged_append(const cs_pages* p, int32_t src_dtype, const void*
     const size_t isz = src_dtype == CS_BF16 ? 2 : 4;
     CS_TRY(cs_check_rows(who, "k", k, k_row, k_head, isz));
     CS_TRY(cs_check_rows(who, "v", v, v_row, v_head, isz));
+    CS_TRY(cs_check_apart(who, "k pool", p->k_page, p->n_pages, p->k_head, p->n_kv_heads, p->head_dim));
+    CS_TRY(cs_check_apart(who, "v pool", p->v_page, p->n_pages, p->v_head, p->n_kv_heads, p->head_dim));
     ap_args A = {k, v, k_row, k_head, v_row, v_head, rot, 1, 0, 0, inv_freq};
     const bool wide = wide_segments(src_dtype, p->head_dim, rot);
     A.segs = p->head_dim / (wide ? 16 : 8);

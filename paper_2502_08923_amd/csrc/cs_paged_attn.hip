@@ -1283,6 +1283,7 @@ extern "C" int cs_paged_attention(const cs_pages* p, const void* q, int64_t q_ro
     const size_t esz = p->dtype == CS_BF16 ? 2 : 4;
     CS_TRY(cs_check_rows(who, "q", q, q_row, q_head, esz));
     CS_TRY(cs_check_rows(who, "out", out, out_row, out_head, esz));
+    CS_TRY(cs_check_apart(who, "out", out_row, R, out_head, n_heads, p->head_dim));
     pa_args A = {q, q_row, q_head, out, out_row, out_head, n_heads, n_heads / p->n_kv_heads, window, scale * 1.4426950408889634f};
     hipStream_t s = (hipStream_t)stream;
     const pa_cut c = pa_make_cut(p, n_heads, d_row0 != nullptr, R, max_rows, max_len);

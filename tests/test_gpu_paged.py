@@ -740,3 +740,21 @@ def test_sizes_that_need_more_than_32_bits_are_refused():
         with pytest.raises(ValueError, match="32 bits"):
             call()
     assert torch.equal(cs.cs_paged_attention(c.pages, q, window=(1 << 31) - 1), cs.cs_paged_attention(c.pages, q))
+
+
+def test_broadcast_inputs_and_strides_that_are_never_taken():
+    """One row for all, one KV head's pool for all; single rows and heads of outputs have no stride that counts."""
+    c = Cache([40, 3], [2, 2], 1, 64, 16, BF)
+    q = randn((1, 4, 64), gen(1), BF)
+    wide = cs.Pages(c.k.expand(-1, 2, -1, -1), c.v.expand(-1, 2, -1, -1), c.table, c.length)
+    want = cs.cs_paged_attention(c.pages, q.expand(4, 4, 64).contiguous())
+    c.close(want, *c.reference(q.expand(4, 4, 64).contiguous(), 0.125), 64)
+    assert torch.equal(cs.cs_paged_attention(wide, q.expand(4, 4, 64)), want)
+    one = torch.zeros((1, 1, 64), dtype=BF, device=DEV)
+    y, _ = cs.cs_op_qk_norm_rope(q[:, :1], q_gain=torch.ones(64, device=DEV), out=(one.as_strided((1, 1, 64), (0, 0, 1)), None))
+    assert torch.equal(one, cs.cs_op_qk_norm_rope(q, q_gain=torch.ones(64, device=DEV))[0][:, :1])
+    for call in (lambda: cs.cs_paged_attention(c.pages, q.expand(4, 4, 64), out=q.expand(4, 4, 64)),
+                 lambda: cs.cs_op_qk_norm_rope(q.expand(4, 4, 64), out=(q.expand(4, 4, 64), None)),
+                 lambda: cs.cs_paged_append(wide, want[:, :2], want[:, :2])):
+        with pytest.raises(cs.CopySpecError, match="overlap"):
+            call()

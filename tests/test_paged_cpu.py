@@ -154,3 +154,16 @@ def test_binding_refuses_tensors_that_want_gradients():
             call()
     with torch.no_grad(), pytest.raises(TypeError, match="CUDA"):
         cs.cs_op_qk_norm_rope(x)
+
+
+def test_what_is_written_does_not_overlap_itself(lib):
+    """Rows, heads and pages that a call writes lie apart; a stride that is never taken may be 0, and so may one of an input."""
+    for bad in (dict(qo_row=0), dict(qo_head=0), dict(qo_row=56), dict(ko_row=0), dict(ko_head=32)):
+        assert norm_rope(lib, **bad) == -2, bad
+    for bad in (dict(out_row=0), dict(out_head=0), dict(out_head=56)):
+        assert attention(lib, **bad) == -2, bad
+    for bad in (dict(k_head=0), dict(v_head=0), dict(k_page=0), dict(v_page=56), dict(v_head=32)):
+        assert append(lib, pages(**bad)) == -2, bad
+        # such pools may be read: what is refused here is the missing workspace
+        long = pages(table_pages=1 << 16, table_stride=1 << 16, **bad)
+        assert attention(lib, long, max_rows=1, max_len=1 << 20, ws=None, ws_bytes=0) == -3, bad
