@@ -758,3 +758,92 @@ def test_broadcast_inputs_and_strides_that_are_never_taken():
                  lambda: cs.cs_paged_append(wide, want[:, :2], want[:, :2])):
         with pytest.raises(cs.CopySpecError, match="overlap"):
             call()
+
+
+class Guarded:
+    """Tensors inside larger ones that hold a pattern; the surroundings must keep it."""
+
+    def __init__(self):
+        self.all = []
+
+    def like(self, shape, dtype, fill=None):
+        n = math.prod(shape) * torch.tensor([], dtype=dtype).element_size()
+        raw = torch.full((n + 8192,), 0xA5, dtype=torch.uint8, device=DEV)
+        self.all.append((raw, n))
+        t = raw[4096:4096 + n].view(dtype).view(shape)
+        if fill is not None:
+            t.fill_(fill)
+        return t
+
+    def check(self):
+        for raw, n in self.all:
+            assert bool((raw[:4096] == 0xA5).all()) and bool((raw[4096 + n:] == 0xA5).all()), "written outside the tensor"
+
+
+def _claimed(offsets, R):
+    """Rows that some stream has, by the offsets brought into 0..R."""
+    rows = set()
+    for a, e in zip(offsets, offsets[1:]):
+        rows |= set(range(min(max(a, 0), R), min(max(e, 0), R)))
+    return rows
+
+
+NO_SENSE = {3: ([0, 100, 3, 6], [-50, 2, 2000000000, 6], [6, 4, 2, 0], [0, -1, -2, -3], [2 ** 31 - 1] * 4, [0, 6, 0, 6]),
+            73: ([0, 146] * 37, [146 - 2 * b for b in range(74)], [0] * 73 + [146], [(b * 97) % 300 - 50 for b in range(74)])}
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("B,hint", [(3, 0), (3, 2), (3, 200), (73, 0), (73, 2), (73, 100)])
+def test_row_offsets_that_make_no_sense_stay_inside(B, hint, dtype):
+    """Offsets outside 0..R or decreasing: nothing around the output, the workspace (of exactly the size asked for) and the pools is
+    written, and rows that no stream has are left as they were.  (Which of the others are computed is not said: a row that two streams
+    claim, or one more tile than the rows allow, has no right answer.)"""
+    lens = [3000, 40, 1000] + [9] * (B - 3)
+    c = Cache(lens, [2] * B, 2, 64, 16, dtype)
+    R = 2 * B
+    guard = Guarded()
+    k, v = guard.like(c.k.shape, dtype), guard.like(c.v.shape, dtype)
+    q = randn((R, 4, 64), gen(1), dtype)
+    for bad in NO_SENSE[B]:
+        k.copy_(c.k), v.copy_(c.v)
+        pages = cs.Pages(k, v, c.table, c.length)
+        row0 = torch.tensor(bad, dtype=torch.int32, device=DEV)
+        call = dict(max_rows=hint, max_len=3002 if hint else 0)
+        need = cs.cs_paged_attention_workspace(pages, 4, R, row0=True, **call)
+        ws, out = guard.like((need,), torch.uint8) if need else None, guard.like((R, 4, 64), dtype, 5.0)
+        cs.cs_paged_attention(pages, q, row0=row0, out=out, workspace=ws, **call)
+        rows = _claimed(bad, R)
+        for r in range(R):
+            if r not in rows:
+                assert bool((out[r] == 5.0).all()), (bad, r)
+        assert torch.equal(torch.nan_to_num(k, nan=1e30), torch.nan_to_num(c.k, nan=1e30))
+        # appended rows lie in the slots that the streams' lengths and the offsets name, and nowhere else
+        cs.cs_paged_append(pages, q[:, :2], q[:, :2], row0=row0)
+        slots = torch.zeros((k.shape[0], 16), dtype=torch.bool)
+        table = c.table.cpu()
+        for b, (a, e) in enumerate(zip(bad, bad[1:])):
+            for i in range(min(max(e, 0), R) - min(max(a, 0), R)):
+                at = lens[b] + i
+                if at < 16 * table.shape[1] and 0 <= int(table[b][at // 16]) < k.shape[0]:
+                    slots[int(table[b][at // 16]), at % 16] = True
+        rest = ~slots.to(DEV)
+        for new, old in ((k, c.k), (v, c.v)):
+            x, y = new.permute(0, 2, 1, 3)[rest], old.permute(0, 2, 1, 3)[rest]
+            assert torch.equal(torch.nan_to_num(x, nan=1e30), torch.nan_to_num(y, nan=1e30)), bad
+        guard.check()
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("P", [16, 1024])
+@pytest.mark.parametrize("rows", [1, 4, 11, 13, 33, 70, 150, 300])
+def test_attention_equal_rows_without_offsets(rows, P, dtype):
+    """Equal shares, with right hints, none and too small ones, into guarded outputs with guarded workspaces of exactly the size."""
+    c = Cache([0, 31, 257, 1100], [rows] * 4, 2, 128, P, dtype, seed=rows)
+    q = randn((4 * rows, 8, 128), gen(3), dtype, 2.0)
+    want = c.reference(q, 1 / math.sqrt(128))
+    guard = Guarded()
+    for call in (dict(max_rows=rows, max_len=1100 + rows), {}, dict(max_rows=1, max_len=16)):
+        need = cs.cs_paged_attention_workspace(c.pages, 8, 4 * rows, **call)
+        ws, out = guard.like((need,), torch.uint8) if need else None, guard.like(q.shape, dtype, 7.0)
+        c.close(cs.cs_paged_attention(c.pages, q, out=out, workspace=ws, **call), *want, 128)
+    guard.check()
