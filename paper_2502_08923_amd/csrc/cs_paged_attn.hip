@@ -1176,9 +1176,15 @@ static int64_t pa_ranges(pa_part& t, int64_t len, int B, int KVH, int hd, int sl
     if (!t.tiles) return 0;
     t.slots = slots, t.start = start, t.join = join;
     const int64_t items = (int64_t)t.tiles * KVH;
-    // (no ranges where the chip is full twice over, or where even the shortest would not pay for the merge)
-    const bool one = items >= 2 * slots || (items <= slots && len <= 64 + join);
-    const int most = one ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>(PA_MOST_RANGES, len / 64));
+    // (no ranges where the chip is full twice over, or where none would pay for the merge if they all ran at once)
+    const int ranges = (int)std::max<int64_t>(1, std::min<int64_t>(PA_MOST_RANGES, len / 64));
+    bool one = items >= 2 * slots;
+    if (items <= slots) {
+        bool pays = false;
+        for (int n = 2; n <= ranges; ++n) pays |= cs_round_up(cs_ceil_div(len, n), 32) + join + n < cs_round_up(len, 32);
+        one |= !pays;
+    }
+    const int most = one ? 1 : ranges;
     const int64_t room = t.tiles + cs_ceil_div((int64_t)PA_MOST_ROUNDS * slots, KVH);
     int64_t best = 0;
     int n_best = 1;
@@ -1221,9 +1227,12 @@ static pa_cut pa_make_cut(const cs_pages* p, int H, bool has_row0, int R, int ma
         W.tiles = (int)(has_row0 ? all / W.TR + std::min<int64_t>(B, all / (n_most + 1)) : B * cs_ceil_div(qr, W.TR));
     }
     // The chip's slots: one workgroup per compute unit, two of the float32 kernel for many rows.  What a workgroup's ends and the merge cost
-    // was measured in tokens of each kernel's own pace: twice these figures change no case by more than 1 %, half of them cost up to 5 %
-    // (4096 rows on an empty cache are cut where they should not be).
-    c.at_w = f32 ? pa_ranges(N, len, B, KVH, p->head_dim, 256, 128, 512) : pa_ranges(N, len, B, KVH, p->head_dim, 256, 256, 768);
+    // is in tokens of each kernel's own pace.  That of float32 blocks of few rows goes with the features, and so does what a merge costs in
+    // its tokens: 384 of 64 features, 192 of 128, 96 of 256 (captured calls, one price of 512 for all before: a row each of 4 streams behind
+    // 450, 8 heads of 128: 16.7 -> 12.5 us, behind 1000: 13.0 both; a row behind 565, 8 heads of 256: 30.5 -> 17.1; 11 rows
+    // behind 565, 4 heads of 64: 11.9 -> 9.5, behind 450, where it still does not pay, 11.4 both; called one by one from Python the last of
+    // these is bound by its two launches instead of one, 11.8 -> 12.5).
+    c.at_w = f32 ? pa_ranges(N, len, B, KVH, p->head_dim, 256, 128, 384 * 64 / c.hdt) : pa_ranges(N, len, B, KVH, p->head_dim, 256, 256, 768);
     c.bytes = c.at_w + (f32 ? pa_ranges(W, len, B, KVH, p->head_dim, 512, 16, 128) : pa_ranges(W, len, B, KVH, p->head_dim, 256, 128, 192));
     return c;
 }

@@ -167,3 +167,13 @@ def test_what_is_written_does_not_overlap_itself(lib):
         # such pools may be read: what is refused here is the missing workspace
         long = pages(table_pages=1 << 16, table_stride=1 << 16, **bad)
         assert attention(lib, long, max_rows=1, max_len=1 << 20, ws=None, ws_bytes=0) == -3, bad
+
+
+@pytest.mark.parametrize("hd,short,long", [(64, 300, 600), (128, 180, 450), (256, 120, 400)])
+def test_float32_contexts_are_cut_where_it_pays(lib, hd, short, long):
+    """The merge of token ranges costs a time, not a number of tokens: the more features a token has, the shorter are the contexts that
+    are cut.  A call that cannot have ranges asks for no workspace."""
+    p = pages(dtype=cs.CS_F32, k_page=16 * hd, k_head=16 * hd, k_token=hd, v_page=16 * hd, v_head=16 * hd, v_token=hd, n_kv_heads=1,
+              head_dim=hd, table_pages=1 << 10, table_stride=1 << 10)
+    assert lib.cs_paged_attention_workspace(C.byref(p), 4, 0, 2, 1, short) == 0
+    assert lib.cs_paged_attention_workspace(C.byref(p), 4, 0, 2, 1, long) > 0
