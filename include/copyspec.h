@@ -428,22 +428,24 @@ int cs_kv_set_len_dev(cs_kv*, const int32_t* d_len /*device [B]*/, int64_t len_u
  *
  * Table entries behind the page of a stream's last token may hold anything.  An entry outside
  * 0 .. n_pages-1 names no page: nothing is written there, and its tokens are not attended to (an
- * evicted page).  Dead slots may hold anything as well, and so may tokens that have left
- * the window of a stream's first new row; other keys and values of live tokens must be finite.  A length is taken as 0 if it is negative, and positions at and beyond
- * table_pages * page_size do not exist: their rows are not written, and their tokens not attended to.
+ * evicted page).  Dead slots may hold anything as well, and so may tokens that have left the window
+ * of a stream's first new row; other keys and values of live tokens must be finite.  A length is
+ * taken as 0 if it is negative, and positions at and beyond table_pages * page_size do not exist:
+ * their rows are not written, and their tokens not attended to.
  *
  * Rows of a call: R rows in all, those of stream b being d_row0[b] .. d_row0[b+1]-1 (device,
  * [batch + 1], not decreasing, first entry 0).  Rows from d_row0[batch] on belong to nobody: they
  * are not read, and their outputs are left as they were.  d_row0 NULL: R / batch rows each.
  * A stream may have no rows.  R == 0 or batch == 0 is a no-op.
  *
- * Limits: page_size a power of two in 16..32768, head_dim a multiple of 8 up to 256, n_heads a multiple of
- * n_kv_heads, table_pages * page_size <= 2^30, batch <= 65536, heads <= 4096, R <= 2^26 and, for the attention,
- * R * n_heads <= 2^30.  Every pointer to rows or pools is aligned to 16 bytes, every
- * stride (in elements, >= 0, at most 2^40) is a multiple of 16 bytes; the elements of one head's row are contiguous.
- * token_stride * page_size elements of a pool must stay below 2^31 bytes.  What is read may be broadcast (a
- * stride of 0); what is written (outputs; the pools of cs_paged_append) may not: its strides are at least head_dim, where there
- * is more than one to step over.
+ * Limits: page_size a power of two in 16..32768, head_dim a multiple of 8 up to 256, n_heads a
+ * multiple of n_kv_heads, table_pages * page_size <= 2^30, batch <= 65536, heads <= 4096, R <= 2^26
+ * and, for the attention, R * n_heads <= 2^30.  Every pointer to rows or pools is aligned to 16
+ * bytes, every stride (in elements, >= 0, at most 2^40) is a multiple of 16 bytes; the elements of
+ * one head's row are contiguous.  token_stride * page_size elements of a pool must stay below 2^31
+ * bytes.  What is read may be broadcast (a stride of 0); what is written (outputs; the pools of
+ * cs_paged_append) may not: its strides are at least head_dim, where there is more than one to step
+ * over.  There is no backward pass.
  * ---------------------------------------------------------------------------------- */
 typedef struct cs_pages {
     void *k, *v;                            /* device pools of one layer, elements of `dtype` */
@@ -463,10 +465,10 @@ typedef struct cs_pages {
  *   y = x / sqrt(mean(x^2) + eps) * gain          (q_gain, k_gain: device float32 [head_dim]; NULL: y = x)
  *   (y[j], y[j + rot/2]) turned by pos[r] * inv_freq[j] for j < rot/2; elements from rot on as they are
  * inv_freq: device float64 [rot/2]; rot 0 (inv_freq and pos may be NULL): no rotation.  rot is a
- * multiple of 8 up to head_dim.  The angle is formed in float64, norm and rotation in float32, and the result is
- * rounded once.  in_dtype -> out_dtype: CS_F32 -> CS_F32, CS_BF16 -> CS_BF16, CS_F32 -> CS_BF16.
- * KVH == 0: queries only.  The outputs may be the inputs (same pointers, strides and type); otherwise
- * they must not overlap.  Strides in elements, limits as above.  Asynchronous on `stream`. */
+ * multiple of 8 up to head_dim.  The angle is formed in float64, norm and rotation in float32, and
+ * the result is rounded once.  in_dtype -> out_dtype: CS_F32 -> CS_F32, CS_BF16 -> CS_BF16, CS_F32 ->
+ * CS_BF16.  KVH == 0: queries only.  The outputs may be the inputs (same pointers, strides and type);
+ * otherwise they must not overlap.  Strides in elements, limits as above.  Asynchronous on `stream`. */
 int cs_op_qk_norm_rope(int32_t in_dtype, int32_t out_dtype, const void* q, int64_t q_row, int64_t q_head,
                        const void* k, int64_t k_row, int64_t k_head, int32_t R, int32_t H, int32_t KVH,
                        int32_t head_dim, const float* q_gain, const float* k_gain, float eps,
@@ -474,10 +476,10 @@ int cs_op_qk_norm_rope(int32_t in_dtype, int32_t out_dtype, const void* q, int64
                        void* q_out, int64_t q_out_row, int64_t q_out_head,
                        void* k_out, int64_t k_out_row, int64_t k_out_head, void* stream);
 
-/* Writes R new key and value rows [R][n_kv_heads][head_dim] into the pages of their streams.  With rot > 0
- * the keys are turned by their position on the way, as in cs_op_qk_norm_rope.  src_dtype CS_F32 (into
- * either cache type) or CS_BF16 (into a CS_BF16 cache); rounded once.  Where two rows go to the same slot (a page
- * named twice), either may stay.  Asynchronous on `stream`. */
+/* Writes R new key and value rows [R][n_kv_heads][head_dim] into the pages of their streams.  With
+ * rot > 0 the keys are turned by their position on the way, as in cs_op_qk_norm_rope.  src_dtype CS_F32
+ * (into either cache type) or CS_BF16 (into a CS_BF16 cache); rounded once.  Where two rows go to the
+ * same slot (a page named twice), either may stay.  Asynchronous on `stream`. */
 int cs_paged_append(const cs_pages* p, int32_t src_dtype, const void* k, int64_t k_row, int64_t k_head,
                     const void* v, int64_t v_row, int64_t v_head, const int32_t* d_row0, int32_t R,
                     const double* inv_freq, int32_t rot, void* stream);
@@ -488,11 +490,12 @@ int cs_paged_append(const cs_pages* p, int32_t src_dtype, const void* k, int64_t
  *   out[r][h] = sum_t softmax_t(scale * q[r][h] . k[t]) v[t]       (a row that sees nothing: 0)
  * scale > 0 and finite.  Softmax statistics and sums are float32; in a CS_BF16 cache the
  * probabilities are rounded to bfloat16 for the product with V.  out may be q.
- * max_rows and max_len (host) say how many rows the longest stream brings and an upper bound of L_b + rows;
- * 0 = not known.  They steer how the work is split, and so the workspace and the rounding, and nothing else:
- * streams that exceed them get the same answer, later.  workspace: device, aligned to 16 bytes, at least
- * cs_paged_attention_workspace(...) bytes for the same arguments (NULL where that is 0), used until the call's work on
- * `stream` is done: calls that may overlap need one each.  Asynchronous on `stream`. */
+ * max_rows and max_len (host) say how many rows the longest stream brings and an upper bound of
+ * L_b + rows; 0 = not known.  They steer how the work is split, and so the workspace (under 0.5 GB
+ * whatever they are) and the rounding, and nothing else: streams that exceed them get the same
+ * answer, later.  workspace: device, aligned to 16 bytes, at least cs_paged_attention_workspace(...)
+ * bytes for the same arguments (NULL where that is 0), used until the call's work on `stream` is
+ * done: calls that may overlap need one each.  Asynchronous on `stream`. */
 int64_t cs_paged_attention_workspace(const cs_pages* p, int32_t n_heads, int32_t has_row0, int32_t R, int32_t max_rows,
                                      int64_t max_len);
 int cs_paged_attention(const cs_pages* p, const void* q, int64_t q_row, int64_t q_head, int32_t n_heads,

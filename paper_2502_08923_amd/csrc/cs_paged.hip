@@ -1,14 +1,16 @@
-// What goes into a paged cache: the norms of query and key heads with the rotary embedding, and the append of new
-// key and value rows to the pages of their streams (Sec. 3.2: the block is appended to the context; App. B.1-B.2:
-// the per-layer K, V it is appended to).
+// What goes into a paged cache: the norms of query and key heads with the rotary embedding, and the
+// append of new key and value rows to the pages of their streams (Sec. 3.2: the block is appended to
+// the context; App. B.1-B.2: the per-layer K, V it is appended to).
 //
-// Both are streams of memory with a little arithmetic on the way.  A workgroup takes a few rows with all their heads,
-// so that the angles of a row (head-independent, two float64 products and two series each) are made once and
-// shared through LDS, instead of once per head: at 40 heads that is the difference between the vector unit and
-// the memory being the bound.  A lane holds VEC consecutive elements of a head's first half and the VEC elements
-// of its second half that pair up with them, so the rotation needs no other lane; the norm is a shuffle sum over the
-// head's lanes.  Measured: norms and rotation of 4096 rows of 40 heads of 128 (84 MB moved) 17.7 us = 4.7 TB/s, what a large copy reaches; 88
-// rows 3.7 us, a launch's latency; append of 11 thousand rows in 8 ragged prompts (90 MB) 16-22 us = 4.1-5.6 TB/s, of 88 rows 3.2 us.
+// Both are streams of memory with a little arithmetic on the way.  A workgroup takes a few rows with
+// all their heads, so that the angles of a row (head-independent, two float64 products and two series
+// each) are made once and shared through LDS, instead of once per head: at 40 heads that is the
+// difference between the vector unit and the memory being the bound.  A lane holds VEC consecutive
+// elements of a head's first half and the VEC elements of its second half that pair up with them, so
+// the rotation needs no other lane; the norm is a shuffle sum over the head's lanes.  Measured: norms
+// and rotation of 4096 rows of 40 heads of 128 (84 MB moved) 17.0 to 17.5 us = 4.8 to 4.9 TB/s, what a
+// large copy reaches; 88 rows 4.2 us, a launch's latency; append of 11 thousand rows in 8 ragged
+// prompts (90 MB) 16.1 to 16.6 us = 5.4 to 5.6 TB/s, of 88 rows 3.4 to 3.6 us.
 #include <algorithm>
 
 #include "cs_paged.h"
@@ -71,8 +73,8 @@ int cs_pages_view(const char* who, const cs_pages* p, const int32_t* d_row0, int
 }
 
 // ---- one head's elements in a lane ------------------------------------------------------
-// VEC elements of either half.  Element pairs of the rotated part are (j, j + rot/2); the part behind it is split in two
-// halves the same way and passed through.
+// VEC elements of either half.  Element pairs of the rotated part are (j, j + rot/2); the part behind
+// it is split in two halves the same way and passed through.
 template <int VEC>
 struct pair_t { float a[VEC], b[VEC]; };
 
@@ -205,7 +207,8 @@ __global__ __launch_bounds__(NR_THREADS) void k_qk_norm_rope(nr_args A) {
     }
 }
 
-// VEC elements of a half per lane: 8 where rows of 16-bit elements have whole segments of them (16-byte loads), else 4
+// VEC elements of a half per lane: 8 where rows of 16-bit elements have whole segments of them (16-byte
+// loads), else 4
 static bool wide_segments(int in_dtype, int hd, int rot) { return in_dtype == CS_BF16 && rot % 16 == 0 && (hd - rot) % 16 == 0; }
 
 static int lanes_log2_of(int segs) {
@@ -252,10 +255,19 @@ extern "C" int cs_op_qk_norm_rope(int32_t in_dtype, int32_t out_dtype, const voi
     const bool wide = wide_segments(in_dtype, head_dim, rot);
     A.segs = head_dim / (wide ? 16 : 8);
     A.lanes_log2 = lanes_log2_of(A.segs);
-    // The angles of a row are made by every workgroup that has heads of it, and a workgroup has its start and its loads to wait for: one row
-    // while there are few, four where they fill the chip several times over, and two workgroups for the heads of a row where one would
-    // pass over them more than once (88 rows of 40 heads: 4.6 -> 3.7 us with two; 4096 rows: 21.0 -> 17.7 us with four rows and two workgroups
-    // against four rows and one, 19.9 with one row; 1531 float32 rows of 32 heads: 13.8 with four rows, 10.1 with two).
+    // The angles of a row are made by every workgroup that has heads of it, and a workgroup has its
+    // start and its loads to wait for: one row while there are few, four where they fill the chip
+    // several times over, and two workgroups for the heads of a row where one would pass over them more
+    // than once (88 rows of 40 heads: 4.6 -> 3.7 us with two; 4096 rows by fours 21.0 -> 17.7).  With
+    // one, two and four rows a workgroup, us of captured calls:
+    //                             512 rows           1531               2048               4096
+    //   40 x 128, bfloat16    5.0   5.4   6.8    9.2   8.6   9.4   11.3  10.3  10.8   18.7  17.2  16.7
+    //   32 x 128, bfloat16    4.3   5.4   7.7    7.5   8.2   9.9    8.8   9.3  10.5   15.3  14.6  15.7
+    //   32 x 128, float32     5.1   5.9   7.5   10.2  10.0  10.7   13.2  12.3  12.4   22.3  22.2  21.3
+    //    9 x 64, bfloat16     3.5   3.4   3.5    4.1   3.9   3.8    4.3   4.0   3.9    6.4   5.2   4.7
+    //   32 x 256, bfloat16    6.9   7.3   9.7   14.5  14.7  16.0   16.9  17.5  18.4   26.6  27.8  27.8
+    // The rule goes by the rows alone and is the best of the three or within 10 % of it, but around
+    // 2048 rows (32 bfloat16 heads of 128: 19 %, 9 float32 heads of 64: 15 %).
     A.rpw = R >= 2048 ? NR_ROWS : R >= 1024 ? 2 : 1;
     const dim3 grid = cs_paged_grid(cs_ceil_div(R, A.rpw), H + KVH > NR_THREADS >> A.lanes_log2 ? 2 : 1);
     hipStream_t s = (hipStream_t)stream;
@@ -358,8 +370,9 @@ extern "C" int cs_paged_append(const cs_pages* p, int32_t src_dtype, const void*
     const bool wide = wide_segments(src_dtype, p->head_dim, rot);
     A.segs = p->head_dim / (wide ? 16 : 8);
     A.lanes_log2 = lanes_log2_of(A.segs);
-    // four rows share the look-up of their places, which is a chain of three loads (11 thousand rows of 8 heads: 27 us with one row, 22 with
-    // four); few rows are better spread out (88 rows: 4.0 with four, 3.2 with one)
+    // four rows share the look-up of their places, which is a chain of three loads (11 thousand rows of
+    // 8 heads of 128: 19.3 us with one row, 14.4 with four, of 4 heads of 64 13.7 and 7.9; 2048 rows
+    // 5.4 and 5.5); few rows are better spread out (88 rows: 3.4 with one, 4.3 with four)
     A.rpw = R >= 1024 ? NR_ROWS : 1;
     const dim3 grid = cs_paged_grid(cs_ceil_div(R, A.rpw));
     hipStream_t s = (hipStream_t)stream;

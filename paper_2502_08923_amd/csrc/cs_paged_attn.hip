@@ -1,13 +1,15 @@
-// Attention of a chunk of new rows per stream over the pages of its cache (Sec. 3.2: the draft is appended to the context
-// and evaluated in one pass; App. B.2: per-layer K, V).
+// Attention of a chunk of new rows per stream over the pages of its cache (Sec. 3.2: the draft is
+// appended to the context and evaluated in one pass; App. B.2: per-layer K, V).
 //
 //   out[r][h] = sum_t p_t v[t] / sum_t p_t,   p_t = exp(scale * q[r][h] . k[t] - max),   t <= L_b + i, t > L_b + i - window
 //
-// One pass over the tokens with the running maximum and sum of the softmax in float32.  Three kernels: bfloat16 caches with few query rows
-// per KV head (the stream of keys and values is the bound) and with many (the multiplies are), float32 caches; and the merge of what
-// several workgroups have of a row.  They multiply with the matrix instructions, K as the A operand, so a lane (c, g) = (lane % 16,
-// lane / 16) has four consecutive tokens of query row c in the result, which is what the second product wants of its B operand.
-// No wave, workgroup or launch order enters a result: every sum has one order, given by the cut.
+// One pass over the tokens with the running maximum and sum of the softmax in float32.  Three kernels:
+// bfloat16 caches with few query rows per KV head (the stream of keys and values is the bound) and with
+// many (the multiplies are), float32 caches; and the merge of what several workgroups have of a row.
+// They multiply with the matrix instructions, K as the A operand, so a lane (c, g) = (lane % 16, lane /
+// 16) has four consecutive tokens of query row c in the result, which is what the second product wants
+// of its B operand. No wave, workgroup or launch order enters a result: every sum has one order, given
+// by the cut.
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
@@ -24,14 +26,18 @@ struct pa_args {
 };
 
 // ---- which query rows and tokens a workgroup has --------------------------------------------------
-// The G * rows query rows of a stream's KV head (row n: block row n / G, head n % G of the group) are cut into tiles of TR.
-// Streams with qr_lo < G * rows <= qr_hi take part in a launch.  The tokens of a tile are cut into ranges of `chunk`, where that fills the
-// chip better; lengths are only known on the device, so the cut is made there, by every workgroup for itself: each lane
-// prices another number of ranges for the longest stream (rounds of the chip that all ranges of all streams then take, a round
-// costing its tokens and, in the same unit, a workgroup's start and end), and the cheapest is taken.  Batches of more than 64 streams
-// have workgroups enough and take the host's cut.  (Against the host's cut for all, which takes every stream to be as long as the longest:
-// 2048 rows and 15 single tokens behind 4 to 16 thousand 740 -> 685 us, two ragged float32 prompt blocks 185 -> 152 us, eight equal streams
-// 120 -> 122 us.)
+// The G * rows query rows of a stream's KV head (row n: block row n / G, head n % G of the group) are
+// cut into tiles of TR. Streams with qr_lo < G * rows <= qr_hi take part in a launch.  The tokens of a
+// tile are cut into ranges of `chunk`, where that fills the chip better; lengths are only known on the
+// device, so the cut is made there, by every workgroup for itself: each lane prices another number of
+// ranges for the longest stream (rounds of the chip that all ranges of all streams then take, a round
+// costing its tokens and, in the same unit, a workgroup's start and end), and the cheapest is taken of
+// those that there is room for.  Room is what the host's cut needs, which takes every stream to be as
+// long as the longest, or one round of the chip: where single tiles of all streams fill the chip by
+// that count (32 streams of 8 KV heads), a long one among short ones is not cut finer. A batch of more
+// than 64 streams takes the host's cut itself, whatever its lengths are.  (Against the host's cut for
+// all: 2048 rows and 15 single tokens behind 4 to 16 thousand 740 -> 685 us, two ragged float32 prompt
+// blocks 185 -> 152 us, eight equal streams 120 -> 122 us.)
 struct pa_tile {
     int b, n0, QR;            // stream, first query row, query rows of the stream
     int row0, rows, L;        // its first row, rows, length
@@ -61,8 +67,8 @@ __device__ __forceinline__ int2 pa_extent(const cs_pages_dev& D, int G, int wind
     if (window) span = (int)min((int64_t)span, (int64_t)window + min(rows, P.TR / G + 1) + 32);
     return make_int2((int)((qr + P.TR - 1) / P.TR), max(span, 1));
 }
-// Reductions over the wave in registers (data-parallel primitives: rows of 16, then row ends to the rows behind them); a lane that a step does
-// not reach combines with `id`.  Lane 63 has everything.
+// Reductions over the wave in registers (data-parallel primitives: rows of 16, then row ends to the
+// rows behind them); a lane that a step does not reach combines with `id`.  Lane 63 has everything.
 template <typename F>
 __device__ __forceinline__ int pa_wave_reduce(int v, int id, F f) {
 #define PA_DPP(ctrl, rows) v = f(v, __builtin_amdgcn_update_dpp(id, v, ctrl, rows, 0xf, false))
@@ -168,8 +174,8 @@ __device__ __forceinline__ void pa_store4(bf16_t* p, f32x4 v) {
     *reinterpret_cast<bf16x4*>(p) = (bf16x4){(bf16_t)v[0], (bf16_t)v[1], (bf16_t)v[2], (bf16_t)v[3]};
 }
 
-// The (max, sum, O) triples of W waves side by side in LDS -> the tile's rows: the output itself where the tokens are in one
-// range, else this range's partial result.
+// The (max, sum, O) triples of W waves side by side in LDS -> the tile's rows: the output itself where
+// the tokens are in one range, else this range's partial result.
 template <int W, int HD, int ROWS, typename T_>
 __device__ __forceinline__ void pa_finish(const cs_pages_dev& D, const pa_args& A, const pa_plan& P, const pa_work& K, int kvh, int n_rows,
                                           const float* s_o, const float2* s_ml, int tid, int n_threads) {
@@ -209,20 +215,23 @@ __device__ __forceinline__ void pa_finish(const cs_pages_dev& D, const pa_args& 
 }
 
 // ---- few query rows: the stream of keys and values is the bound ---------------------------------
-// Four waves share a tile of up to 48 query rows and take the 32-token blocks of a token range in turn; keys, values,
-// scores and outputs stay in registers:
+// Four waves share a tile of up to 48 query rows and take the 32-token blocks of a token range in turn;
+// keys, values, scores and outputs stay in registers:
 //   S^T[token][row] = K . Q^T           A = 16 key rows (a lane: 8 features of one), B = query rows
 //   O^T[feature][row] += V^T . P^T      A = 16 features of 32 tokens, B = the probabilities as S^T left them
-// The k index of the second product may run over the block's tokens in any order that both operands share, so lane (c, g) takes
-// the tokens 4g..4g+3 of either 16-token half, which are the rows of S^T it holds already.  A lane loads 16 bytes of those eight
-// value rows (8 features of each) and turns the 8 x 8 square with 32 byte permutes into eight A fragments: fragment u has
-// feature 8c + u in row c.  So the values lie in the pages as they come, and a wave's load takes whole rows.
-// A page holds whole 16-token halves, so every load has one page and a uniform base: a buffer whose size ends with the last
-// token.  Loads past it, and of pages that do not exist, return zeros and cost no traffic, and none sits behind a branch.
-// Two blocks of keys and two of values per wave are in flight (32 KB a wave at head_dim 128); what bounds it then is memory: 8 streams of
-// 11 rows behind 18431 tokens, head_dim 128, 4 heads a group, 604 MB: 110 us = 5.5 TB/s; 64 single tokens behind 2 to 8 thousand,
-// pages of 16 tokens: 262 us = 5.2 TB/s; one stream of 16000: 22 us with the merge.  Workgroups: one per compute unit (twice as many cost 7 %,
-// four times 20 %: their starts, their ends and the merge).
+// The k index of the second product may run over the block's tokens in any order that both operands
+// share, so lane (c, g) takes the tokens 4g..4g+3 of either 16-token half, which are the rows of S^T it
+// holds already.  A lane loads 16 bytes of those eight value rows (8 features of each) and turns the 8
+// x 8 square with 32 byte permutes into eight A fragments: fragment u has feature 8c + u in row c.  So
+// the values lie in the pages as they come, and a wave's load takes whole rows. A page holds whole
+// 16-token halves, so every load has one page and a uniform base: a buffer whose size ends with the
+// last token.  Loads past it, and of pages that do not exist, return zeros and cost no traffic, and
+// none sits behind a branch. Two blocks of keys and two of values per wave are in flight (32 KB a wave
+// at head_dim 128); what bounds it then is memory: 8 streams of 11 rows behind 18431 tokens, head_dim
+// 128, 4 heads a group, 606 MB: 109 to 114 us = 5.3 to 5.6 TB/s; 64 single tokens behind 2 to 8
+// thousand, pages of 16 tokens, 1357 MB: 259 to 265 us = 5.1 to 5.2 TB/s; one stream of 16000: 22 us
+// with the merge. Workgroups: one per compute unit (twice as many cost 7 %, four times 20 %: their
+// starts, their ends and the merge).
 #define PN_WAVES 4
 template <int HD>
 struct pn_kbuf { bf16x8 k[2][HD / 32]; };
@@ -406,15 +415,17 @@ __global__ __launch_bounds__(64 * PN_WAVES) void k_paged_narrow(cs_pages_dev D, 
                 mx = fmaxf(fmaxf(mx, sv[3]), sv[4]);
                 mx = fmaxf(fmaxf(mx, sv[5]), fmaxf(sv[6], sv[7]));
                 mx = fa_row4_max(mx) * scale2;
-                // the reference maximum follows the true one only when it is left behind by 2^8: probabilities stay
-                // below 256, O and the row sum stay consistent, and O is rescaled a handful of times per wave
+                // the reference maximum follows the true one only when it is left behind by 2^8:
+                // probabilities stay below 256, O and the row sum stay consistent, and O is rescaled a
+                // handful of times per wave
                 const bool up = mx > m_run[nt] + FA_RESCALE_LOG2;
                 const float m_new = up ? mx : m_run[nt];
                 const float m_safe = m_new == -INFINITY ? 0.f : m_new;
                 alpha[nt] = up ? __builtin_amdgcn_exp2f(m_run[nt] - m_safe) : 1.0f;
                 moved |= up;
                 m_run[nt] = m_new;
-                // rounded to bfloat16, the type of V in the product; the row sum is that of the rounded values
+                // rounded to bfloat16, the type of V in the product; the row sum is that of the rounded
+                // values
 #pragma unroll
                 for (int j = 0; j < 8; ++j) pb[nt][j] = (bf16_t)__builtin_amdgcn_exp2f(fmaf(sv[j], scale2, -m_safe));
             }
@@ -480,8 +491,8 @@ __global__ __launch_bounds__(64 * PN_WAVES) void k_paged_narrow(cs_pages_dev D, 
     }
     __syncthreads();             // every wave is done with the query tile: LDS changes hands
 
-    // the waves' (max, sum, O) side by side in LDS, combined by all threads.  oacc[x*2*VW + u][nt][j]: query row nt*16 + c, feature
-    // (x*16 + 4g + j) * VF + u
+    // the waves' (max, sum, O) side by side in LDS, combined by all threads.  oacc[x*2*VW + u][nt][j]:
+    // query row nt*16 + c, feature (x*16 + 4g + j) * VF + u
     float* s_o = reinterpret_cast<float*>(smem);                               // [waves][ROWS][OROW]
     float2* s_ml = reinterpret_cast<float2*>(s_o + PN_WAVES * ROWS * OROW);    // [waves][ROWS]
 #pragma unroll
@@ -503,8 +514,8 @@ __global__ __launch_bounds__(64 * PN_WAVES) void k_paged_narrow(cs_pages_dev D, 
     pa_finish<PN_WAVES, HD, ROWS, bf16_t>(D, A, P, K, kvh, n_rows, s_o, s_ml, tid, 64 * PN_WAVES);
 }
 
-// As cs_load_to_lds, where the base comes straight from a lane: five wait states lie between a v_readlane and the load that takes
-// its address from the result.
+// As cs_load_to_lds, where the base comes straight from a lane: five wait states lie between a
+// v_readlane and the load that takes its address from the result.
 #pragma clang diagnostic push
 #pragma clang diagnostic ignored "-Winline-asm"
 __device__ __forceinline__ void cs_load_to_lds_lane(unsigned voff, const void* sbase, unsigned lds_addr) {
@@ -513,20 +524,26 @@ __device__ __forceinline__ void cs_load_to_lds_lane(unsigned voff, const void* s
 #pragma clang diagnostic pop
 
 // ---- many query rows: the matrix cores and the vector unit are the bound -----------------------------
-// Eight waves have 16 * NT query rows each and walk the tokens together: every 32-token block goes once from its pages to LDS and
-// serves all of them.  Each wave requests its share of a block (1 KB pieces, direct to LDS) into a ring of stages, so several
-// blocks are in flight while one is multiplied; the requests and the waits on them are counted exactly, by hand, and the
-// kernel has no other vector memory load in its loop but the page numbers of the next 64 blocks.
+// Eight waves have 16 * NT query rows each and walk the tokens together: every 32-token block goes once
+// from its pages to LDS and serves all of them.  Each wave requests its share of a block (1 KB pieces,
+// direct to LDS) into a ring of stages, so several blocks are in flight while one is multiplied; the
+// requests and the waits on them are counted exactly, by hand, and the kernel has no other vector
+// memory load in its loop but the page numbers of the next 64 blocks.
 //   keys: one piece = 16 tokens x 32 features in fragment order, a lane's 16 bytes are what it multiplies
 //   values: one piece = 16 tokens x 32 features as two 16 x 16 squares of 32-byte rows, which the transposing LDS read
 //   (four tokens of one feature per lane) takes apart without bank conflicts
 // The products, the softmax and the order of tokens in the probabilities are those of the kernel above.
-// What bounds it: the matrix units are busy 46 % of the time and the vector units 45 % (a block of 32 tokens and 32 rows is 544 cycles of
-// products and 500 of softmax), and little of either overlaps; at that rate the card is near its power limit (all zeros: 20 % faster).  4096 rows
-// of 32 heads on an empty cache: 146-160 us = 0.86-0.94 PFLOP/s; 2048 rows behind 16384 tokens 0.96, 16 streams of 33 rows (231 of 256 tile
-// rows) behind 65535 tokens 594-640 us = 0.78-0.83.  Tried against this, same card: no teams +3 %, no wave priorities +1 to 2.5 %; the products of the next
-// block woven into the softmax by hand +10 %; fragments of a whole block read ahead +3 to 5 %; 64 rows a wave in four waves: spills;
-// two workgroups of four waves per compute unit: the same at 4096 rows, +20 % where one tile's rows had become two's.
+// What bounds it: the matrix units are busy 46 % of the time and the vector units 45 % (a block of 32
+// tokens and 32 rows is 544 cycles of products and 500 of softmax), and little of either overlaps; at
+// that rate the card is near its power limit (all zeros: 20 % faster).  Calls one after the other,
+// median and range: 4096 rows of 32 heads on an empty cache 150 us (146 to 167) = 0.92 PFLOP/s; 2048
+// rows behind 16384 tokens, with the merge, 538 us (531 to 612) = 1.09; 16 streams of 33 rows of 28
+// heads (231 of 256 tile rows) behind 65535 tokens, with the merge, 608 us (600 to 645) = 0.82.  Under
+// the profiler, which spaces the launches, the kernel alone takes 175 to 185, 610 to 640 and 690 to 715
+// us at the median (0.76, 0.94 and 0.71).  Tried against this, same card: no teams +3 %, no wave
+// priorities +1 to 2.5 %; the products of the next block woven into the softmax by hand +10 %;
+// fragments of a whole block read ahead +3 to 5 %; 64 rows a wave in four waves: spills; two workgroups
+// of four waves per compute unit: the same at 4096 rows, +20 % where one tile's rows had become two's.
 #define PW_WAVES 8
 template <int HD, int NT>
 __global__ __launch_bounds__(64 * PW_WAVES) void k_paged_wide(cs_pages_dev D, pa_args A, pa_plan P) {
@@ -573,8 +590,9 @@ __global__ __launch_bounds__(64 * PW_WAVES) void k_paged_wide(cs_pages_dev D, pa
 #pragma unroll
         for (int s = 0; s < KS; ++s) asm volatile("" : "+v"(qreg[nt][s]));
 
-    // this wave's pieces: id = wave + 8u; below 2*KS keys (half id / KS, features 32 * (id % KS) ..), above values likewise.  Features that the
-    // head does not have are read at feature 0: their query elements are 0, their outputs are not stored.
+    // this wave's pieces: id = wave + 8u; below 2*KS keys (half id / KS, features 32 * (id % KS) ..),
+    // above values likewise.  Features that the head does not have are read at feature 0: their query
+    // elements are 0, their outputs are not stored.
     unsigned voff[LD];
 #pragma unroll
     for (int u = 0; u < LD; ++u) {
@@ -585,9 +603,10 @@ __global__ __launch_bounds__(64 * PW_WAVES) void k_paged_wide(cs_pages_dev D, pa
     }
     const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)&stage[0][0];
 
-    // A lane has one of the next 64 blocks: where in the pool each of the wave's pieces of it starts, so that a request costs the scalar
-    // unit no multiplication.  A half whose page does not exist is read from page 0 and masked: from a whole half of it, also
-    // where a range that lies behind all its tile sees begins at a token that is no multiple of 16.
+    // A lane has one of the next 64 blocks: where in the pool each of the wave's pieces of it starts,
+    // so that a request costs the scalar unit no multiplication.  A half whose page does not exist is
+    // read from page 0 and masked: from a whole half of it, also where a range that lies behind all its
+    // tile sees begins at a token that is no multiple of 16.
     const int32_t* tab = D.p.table + T.b * D.p.table_stride;
     unsigned from_lo[LD], from_hi[LD];
     unsigned long long okay0 = 0, okay1 = 0, old0 = 0, old1 = 0;     // halves that exist, of these and of the 64 blocks before
@@ -619,9 +638,10 @@ __global__ __launch_bounds__(64 * PW_WAVES) void k_paged_wide(cs_pages_dev D, pa
             cs_load_to_lds_lane(voff[u], (const void*)from, lds0 + st * STAGE_BYTES + (wave + PW_WAVES * u) * 1024);
         }
     };
-    // At most INFLIGHT of this wave's requests still in flight, then meet the other waves.  The two waves of a SIMD meet them at different
-    // points of a block: the first four behind it, the others between scores and softmax, so that one wave of every SIMD has the
-    // matrix unit while the other has the vector unit.  (One statement: see cs_load_to_lds_if.)
+    // At most INFLIGHT of this wave's requests still in flight, then meet the other waves.  The two
+    // waves of a SIMD meet them at different points of a block: the first four behind it, the others
+    // between scores and softmax, so that one wave of every SIMD has the matrix unit while the other
+    // has the vector unit.  (One statement: see cs_load_to_lds_if.)
     constexpr int INFLIGHT = LD * (STAGES - 3);
     const int team = wave / (PW_WAVES / 2);
 #define PW_SYNC(on) \
@@ -736,8 +756,8 @@ __global__ __launch_bounds__(64 * PW_WAVES) void k_paged_wide(cs_pages_dev D, pa
                 const unsigned char* p = sp + V_AT + (a * KS + (mt >> 1)) * 1024 + (mt & 1) * 512 + lane * 8;
                 h[a] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(__attribute__((address_space(3))) unsigned char*)p);
                 if (MASKED) {
-                    // what lies behind the last token, in place of a page or before every window may be anything, and 0 * anything
-                    // must stay 0
+                    // what lies behind the last token, in place of a page or before every window may be
+                    // anything, and 0 * anything must stay 0
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
                         const int t = t0 + 16 * a + 4 * g + j;
@@ -763,22 +783,26 @@ __global__ __launch_bounds__(64 * PW_WAVES) void k_paged_wide(cs_pages_dev D, pa
         __builtin_amdgcn_s_setprio(0);
     };
 
-    // Blocks 0 .. STAGES-3 are requested up front; round i requests block i + STAGES - 2 into the stage of block i - 2, whose values the second
-    // team has read before the meeting behind its scores of block i - 1.  Behind round i's meeting block i + 1 is there.
+    // Blocks 0 .. STAGES-3 are requested up front; round i requests block i + STAGES - 2 into the stage
+    // of block i - 2, whose values the second team has read before the meeting behind its scores of
+    // block i - 1.  Behind round i's meeting block i + 1 is there.
     pages(0);
 #pragma unroll
     for (int j = 0; j < STAGES - 2; ++j) issue(j, j);         // (past the last block: page 0, into a stage that nobody reads)
     PW_SYNC(1);
     int st_cur = 0, st_req = STAGES - 2;
-    // The loop's bound and the position come from a vector register that the compiler cannot see through: around branches it
-    // takes for uniform it splits the live ranges of the accumulators, copies and spills them.
+    // The loop's bound and the position come from a vector register that the compiler cannot see
+    // through: around branches it takes for uniform it splits the live ranges of the accumulators,
+    // copies and spills them.
     int vzero;
     asm volatile("v_mov_b32 %0, 0" : "=v"(vzero));
     const int nblocks_v = nblocks + vzero;
-    // positions that this wave's rows have: blocks outside what they see are not computed, blocks inside need no mask
+    // positions that this wave's rows have: blocks outside what they see are not computed, blocks
+    // inside need no mask
     const int p_lo = T.L + (T.n0 + wave * WROWS) / G + vzero;
     const int p_hi = T.L + min(T.rows - 1, (T.n0 + wave * WROWS + WROWS - 1) / G) + vzero;
-    // tokens below w_lo are seen by no row of the wave, those from w_hi on by every one (as far as a window goes)
+    // tokens below w_lo are seen by no row of the wave, those from w_hi on by every one (as far as a
+    // window goes)
     const int w_lo = A.window ? p_lo - A.window + 1 : 0, w_hi = A.window ? p_hi - A.window + 1 : 0;
     const int p_end = T.n0 + wave * WROWS < T.QR ? p_hi : -1;      // a wave without rows multiplies nothing
     const int p_open = min(p_lo, D.cap - 1);
@@ -837,14 +861,17 @@ __global__ __launch_bounds__(64 * PW_WAVES) void k_paged_wide(cs_pages_dev D, pa
 
 // ---- float32 caches: everything in float32, on the float32 matrix instruction -------------------------
 //   S^T[token][row] = K . Q^T, O^T[feature][row] += V^T . P^T over blocks of 16 tokens, four k per instruction.
-// Lane (c, g) loads 16 bytes of a key row, four steps of the first product; the rows of S^T that it gets are the k of the second
-// one, step j taking token 4g + j, and its 16 bytes of that token's value row are four features 4c + u, one for each
-// of four tiles.  So nothing is moved between lanes, and nothing goes through LDS but the query rows (and, with TOKENS, the
-// waves' results: few rows, where the waves share them and take the token blocks in turn; without it every wave has 16 * NT rows
-// of its own, and what bounds it is the instruction's rate, 157 TFLOP/s, the re-read blocks coming out of the caches).  Two workgroups share a
-// compute unit, and the matrix units are busy 74 % while they do: two streams of 700 and 438 rows behind 3001 and 1876 tokens, 8 heads of
-// 128: 152-168 us = 80-88 TFLOP/s (one workgroup per compute unit: 225 us; 16 rows a wave: 4 to 9 % slower; two key blocks ahead: no change).
-// Few rows are bound by memory: 8 single tokens behind 8000, 8 heads of 128: 95 us = 5.5 TB/s.
+// Lane (c, g) loads 16 bytes of a key row, four steps of the first product; the rows of S^T that it
+// gets are the k of the second one, step j taking token 4g + j, and its 16 bytes of that token's value
+// row are four features 4c + u, one for each of four tiles.  So nothing is moved between lanes, and
+// nothing goes through LDS but the query rows (and, with TOKENS, the waves' results: few rows, where
+// the waves share them and take the token blocks in turn; without it every wave has 16 * NT rows of its
+// own, and what bounds it is the instruction's rate, 157 TFLOP/s, the re-read blocks coming out of the
+// caches).  Two workgroups share a compute unit, and the matrix units are busy 74 % while they do: two
+// streams of 700 and 438 rows behind 3001 and 1876 tokens, 8 heads of 128: 150 to 155 us = 86 to 89
+// TFLOP/s (one workgroup per compute unit: 225 us; 16 rows a wave: 4 to 9 % slower; two key blocks
+// ahead: no change).  Few rows are bound by memory: 8 single tokens behind 8000, 8 heads of 128, 524
+// MB: 90 to 94 us = 5.6 to 5.8 TB/s, 95 us with the merge.
 #define PF_WAVES 4
 template <int HD, int NT, bool TOKENS>
 __global__ __launch_bounds__(64 * PF_WAVES, !TOKENS && HD <= 128 ? 2 : 1) void k_paged_f32(cs_pages_dev D, pa_args A, pa_plan P) {
@@ -1098,9 +1125,11 @@ __global__ __launch_bounds__(64 * PF_WAVES, !TOKENS && HD <= 128 ? 2 : 1) void k
 }
 
 // ---- joining token ranges ---------------------------------------------------------------------
-// out[r][h] = sum_s 2^(m_s - M) O_s / sum_s 2^(m_s - M) l_s.  2^lanes_log2 lanes have a query row's hd features, four each; a lane
-// reads the (max, sum) pairs of every lanes-th range, and the weights go round by shuffles.  The workgroups are those of the kernel
-// before it: the ones that had the ranges of a tile share out its rows (4 ranges of 8 x 44 rows and 8 heads: 6 us, a launch's own 3 among them).
+// out[r][h] = sum_s 2^(m_s - M) O_s / sum_s 2^(m_s - M) l_s.  2^lanes_log2 lanes have a query row's hd
+// features, four each; a lane reads the (max, sum) pairs of every lanes-th range, and the weights go
+// round by shuffles.  The workgroups are those of the kernel before it: the ones that had the ranges of
+// a tile share out its rows (4 ranges of 8 x 44 rows and 8 heads: 6 us, a launch's own 3 among them; 13
+// ranges of 37 float32 tiles and 2 heads, 962 workgroups, 11.6 us).
 #define PM_THREADS 256
 template <typename T_>
 __global__ __launch_bounds__(PM_THREADS) void k_paged_merge(cs_pages_dev D, pa_args A, pa_plan P, int lanes_log2) {
@@ -1128,7 +1157,8 @@ __global__ __launch_bounds__(PM_THREADS) void k_paged_merge(cs_pages_dev D, pa_a
             for (int s = 0; s < ns; s += 4)
 #pragma unroll
                 for (int u = 0; u < 4; ++u) {
-                    // (past the last range: weight 0, its row once more; a range that saw nothing has stored zeros)
+                    // (past the last range: weight 0, its row once more; a range that saw nothing has
+                    // stored zeros)
                     const int from = (threadIdx.x & 63 & ~(lanes - 1)) + min(s + u, ns - 1);
                     const float keep = s + u < ns ? 1.f : 0.f;
                     l += keep * __shfl(wl, from, 64);
@@ -1163,20 +1193,24 @@ struct pa_cut {
 };
 #define PN_MOST 48                // query rows up to which a stream takes the kernel of few rows
 #define PA_MOST_RANGES 256
-// Pairs that there is room for beyond one per tile, in rounds of the chip.  With room for as many as even out the rounds best the
-// partial results, which are the workspace, come to 2.1 GB (3968 rows of 32 heads over a table of 2^20 tokens); with eight rounds they
-// stay under 0.4 GB.  The cut is the same where that was never used (2048 rows of 32 heads behind 129000 tokens, a table of 2^17:
-// 1.1 GB -> 0.3, 3.8 ms); else the rounds are less even, and there is less to join: 11 x 252 float32 rows of 28 heads behind 31225 tokens
-// 9.75 -> 10.2 ms, a float32 block of 1251 rows of 64 heads beside 23 single tokens, all behind 273 to 1090: 1000 -> 784 us.
+// Pairs that there is room for beyond one per tile, in rounds of the chip.  With room for as many as
+// even out the rounds best the partial results, which are the workspace, come to 2.1 GB (3968 rows of
+// 32 heads over a table of 2^20 tokens); with eight rounds they stay under 0.5 GB.  The cut is the same
+// where that was never used (2048 rows of 32 heads behind 129000 tokens, a table of 2^17: 1.1 GB ->
+// 0.3, 3.8 ms); else the rounds are less even, and there is less to join: 11 x 252 float32 rows of 28
+// heads behind 31225 tokens 9.75 -> 10.2 ms, a float32 block of 1251 rows of 64 heads beside 23 single
+// tokens, all behind 273 to 1090: 1000 -> 784 us.
 #define PA_MOST_ROUNDS 8
-// The host's cut prices the ranges as the device does, with every stream as long as the longest; batches of more than 64 streams take it.
-// For the others it says how many (tile, range) pairs there is room for: one round of the chip, or what the host's cut has.
-// (A workgroup without a pair ends at once, but where one fills a compute unit it waits for its turn.)
+// The host's cut prices the ranges as the device does, with every stream as long as the longest;
+// batches of more than 64 streams take it. For the others it says how many (tile, range) pairs there is
+// room for: one round of the chip, or what the host's cut has. (A workgroup without a pair ends at
+// once, but where one fills a compute unit it waits for its turn.)
 static int64_t pa_ranges(pa_part& t, int64_t len, int B, int KVH, int hd, int slots, int start, int join) {
     if (!t.tiles) return 0;
     t.slots = slots, t.start = start, t.join = join;
     const int64_t items = (int64_t)t.tiles * KVH;
-    // (no ranges where the chip is full twice over, or where none would pay for the merge if they all ran at once)
+    // (no ranges where the chip is full twice over, or where none would pay for the merge if they all
+    // ran at once)
     const int ranges = (int)std::max<int64_t>(1, std::min<int64_t>(PA_MOST_RANGES, len / 64));
     bool one = items >= 2 * slots;
     if (items <= slots) {
@@ -1206,8 +1240,9 @@ static pa_cut pa_make_cut(const cs_pages* p, int H, bool has_row0, int R, int ma
     const bool f32 = p->dtype == CS_F32;
     c.hdt = p->head_dim <= 64 ? 64 : p->head_dim <= 128 ? 128 : 256;
     pa_part &N = c.narrow, &W = c.wide;
-    // Streams of up to n_most query rows per KV head go to the kernel of few rows.  Where a batch has longer ones too, that kernel is
-    // made for single tokens: a tile of 48 rows would cost every one of them three tiles' products.
+    // Streams of up to n_most query rows per KV head go to the kernel of few rows.  Where a batch has
+    // longer ones too, that kernel is made for single tokens: a tile of 48 rows would cost every one of
+    // them three tiles' products.
     const int n_most = c.hdt == 256 || qr > PN_MOST ? 16 : PN_MOST;
     if (has_row0 || qr <= n_most) {
         N.nt = (int)std::min<int64_t>(n_most / 16, cs_ceil_div(qr, 16));
@@ -1216,9 +1251,11 @@ static pa_cut pa_make_cut(const cs_pages* p, int H, bool has_row0, int R, int ma
         N.tiles = !has_row0 ? B : (int)(qr <= n_most ? all / N.TR + std::min(B, R) : std::min(B, R));
     }
     if (qr > n_most) {
-        // Tiles of half the rows where whole ones, cut into ranges of 256 tokens of what a row sees on average, leave the chip unfilled: a
-        // block of tokens takes such a tile about half as long, and there are twice as many (6 streams of 985 rows of 4 heads: 60 -> 34 us;
-        // 1000 rows of 32 heads: 56 -> 35; 64 rows behind 4000 tokens: 28 -> 23; but 2 streams of 300 rows behind 1000: 48 -> 52, by the rule whole).
+        // Tiles of half the rows where whole ones, cut into ranges of 256 tokens of what a row sees on
+        // average, leave the chip unfilled: a block of tokens takes such a tile about half as long, and
+        // there are twice as many (6 streams of 985 rows of 4 heads: 60 -> 34 us; 1000 rows of 32
+        // heads: 56 -> 35; 64 rows behind 4000 tokens: 28 -> 23; but 2 streams of 300 rows behind 1000:
+        // 48 -> 52, by the rule whole).
         const bool unfilled = (all / (PW_WAVES * 32) + 1) * KVH * std::max<int64_t>(1, (len - rows / 2) / 256) < 256;
         W.nt = c.hdt == 256 || (!f32 && unfilled) ? 1 : 2;
         W.TR = (f32 ? PF_WAVES : PW_WAVES) * 16 * W.nt;
@@ -1226,12 +1263,20 @@ static pa_cut pa_make_cut(const cs_pages* p, int H, bool has_row0, int R, int ma
         W.qr_hi = 0x7fffffff;
         W.tiles = (int)(has_row0 ? all / W.TR + std::min<int64_t>(B, all / (n_most + 1)) : B * cs_ceil_div(qr, W.TR));
     }
-    // The chip's slots: one workgroup per compute unit, two of the float32 kernel for many rows.  What a workgroup's ends and the merge cost
-    // is in tokens of each kernel's own pace.  That of float32 blocks of few rows goes with the features, and so does what a merge costs in
-    // its tokens: 384 of 64 features, 192 of 128, 96 of 256 (captured calls, one price of 512 for all before: a row each of 4 streams behind
-    // 450, 8 heads of 128: 16.7 -> 12.5 us, behind 1000: 13.0 both; a row behind 565, 8 heads of 256: 30.5 -> 17.1; 11 rows
-    // behind 565, 4 heads of 64: 11.9 -> 9.5, behind 450, where it still does not pay, 11.4 both; called one by one from Python the last of
-    // these is bound by its two launches instead of one, 11.8 -> 12.5).
+    // The chip's slots: one workgroup per compute unit, two of the float32 kernel for many rows.  What
+    // a workgroup's ends and the merge cost is in tokens of each kernel's own pace.  That of float32
+    // blocks of few rows goes with the features, and so does what a merge costs in its tokens: 384 of
+    // 64 features, 192 of 128, 96 of 256 (captured calls, one price of 512 for all before: a row each
+    // of 4 streams behind 450, 8 heads of 128: 16.7 -> 12.5 us, behind 1000: 13.0 both; a row behind
+    // 565, 8 heads of 256: 30.5 -> 17.1; 11 rows behind 565, 4 heads of 64: 11.9 -> 9.5, behind 450,
+    // where it still does not pay, 11.4 both; called one by one from Python the last of these is bound
+    // by its two launches instead of one, 11.8 -> 12.5).  The other three are single figures yet.
+    // Against half and twice both of a kernel's, captured calls: few bfloat16 rows behind 600 to 900
+    // tokens would gain 14 to 38 % from half where a token has 128 or 256 features and lose 6 to 16 %
+    // where it has 64, behind 1000 to 1300 twice costs up to 131 %, and behind 2000 and more neither
+    // changes 3 %; many bfloat16 rows on an empty cache take up to 2.6 times as long with half (2 x 600
+    // rows of 28 heads: 26.6 -> 68 us), and twice changes them by -21 (2 x 600 behind 1000) to +10 %
+    // (1500 rows of 8 heads of 64 behind 300); many float32 rows: -7 to +2 % with half, 3 % with twice.
     c.at_w = f32 ? pa_ranges(N, len, B, KVH, p->head_dim, 256, 128, 384 * 64 / c.hdt) : pa_ranges(N, len, B, KVH, p->head_dim, 256, 256, 768);
     c.bytes = c.at_w + (f32 ? pa_ranges(W, len, B, KVH, p->head_dim, 512, 16, 128) : pa_ranges(W, len, B, KVH, p->head_dim, 256, 128, 192));
     return c;
