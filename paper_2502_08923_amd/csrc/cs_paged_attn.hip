@@ -34,10 +34,13 @@ struct pa_args {
 // costing its tokens and, in the same unit, a workgroup's start and end), and the cheapest is taken of
 // those that there is room for.  Room is what the host's cut needs, which takes every stream to be as
 // long as the longest, or one round of the chip: where single tiles of all streams fill the chip by
-// that count (32 streams of 8 KV heads), a long one among short ones is not cut finer. A batch of more
-// than 64 streams takes the host's cut itself, whatever its lengths are.  (Against the host's cut for
-// all: 2048 rows and 15 single tokens behind 4 to 16 thousand 740 -> 685 us, two ragged float32 prompt
-// blocks 185 -> 152 us, eight equal streams 120 -> 122 us.)
+// that count (32 streams of 8 KV heads), a long one among short ones is not cut finer.  A batch of more
+// than 64 streams takes the host's cut itself, whatever its lengths are, and where it has row offsets
+// every workgroup walks them 64 at a time until its own: that is for hundreds of streams (single tokens
+// behind 100, 8 heads of 128 a KV head: 256 streams 9.2 us against 7.8 without offsets, 1024 38 against
+// 17, 4096 353 against 52).  (Against the host's cut for all: 2048 rows and 15 single tokens behind 4 to
+// 16 thousand 740 -> 685 us, two ragged float32 prompt blocks 185 -> 152 us, eight equal streams 120 ->
+// 122 us.)
 struct pa_tile {
     int b, n0, QR;            // stream, first query row, query rows of the stream
     int row0, rows, L;        // its first row, rows, length
@@ -228,8 +231,8 @@ __device__ __forceinline__ void pa_finish(const cs_pages_dev& D, const pa_args& 
 // last token.  Loads past it, and of pages that do not exist, return zeros and cost no traffic, and
 // none sits behind a branch. Two blocks of keys and two of values per wave are in flight (32 KB a wave
 // at head_dim 128); what bounds it then is memory: 8 streams of 11 rows behind 18431 tokens, head_dim
-// 128, 4 heads a group, 606 MB: 109 to 114 us = 5.3 to 5.6 TB/s; 64 single tokens behind 2 to 8
-// thousand, pages of 16 tokens, 1357 MB: 259 to 265 us = 5.1 to 5.2 TB/s; one stream of 16000: 22 us
+// 128, 4 heads a group, 606 MB: 109 to 115 us = 5.3 to 5.6 TB/s; 64 single tokens behind 2 to 8
+// thousand, pages of 16 tokens, 1357 MB: 259 to 266 us = 5.1 to 5.2 TB/s; one stream of 16000: 22 us
 // with the merge. Workgroups: one per compute unit (twice as many cost 7 %, four times 20 %: their
 // starts, their ends and the merge).
 #define PN_WAVES 4
@@ -539,8 +542,8 @@ __device__ __forceinline__ void cs_load_to_lds_lane(unsigned voff, const void* s
 // median and range: 4096 rows of 32 heads on an empty cache 150 us (146 to 167) = 0.92 PFLOP/s; 2048
 // rows behind 16384 tokens, with the merge, 538 us (531 to 612) = 1.09; 16 streams of 33 rows of 28
 // heads (231 of 256 tile rows) behind 65535 tokens, with the merge, 608 us (600 to 645) = 0.82.  Under
-// the profiler, which spaces the launches, the kernel alone takes 175 to 185, 610 to 640 and 690 to 715
-// us at the median (0.76, 0.94 and 0.71).  Tried against this, same card: no teams +3 %, no wave
+// the profiler, which spaces the launches, the kernel alone takes about 180, 620 and 700 us at the
+// median (0.76, 0.94 and 0.71).  Tried against this, same card: no teams +3 %, no wave
 // priorities +1 to 2.5 %; the products of the next block woven into the softmax by hand +10 %;
 // fragments of a whole block read ahead +3 to 5 %; 64 rows a wave in four waves: spills; two workgroups
 // of four waves per compute unit: the same at 4096 rows, +20 % where one tile's rows had become two's.
@@ -1215,7 +1218,7 @@ static int64_t pa_ranges(pa_part& t, int64_t len, int B, int KVH, int hd, int sl
     bool one = items >= 2 * slots;
     if (items <= slots) {
         bool pays = false;
-        for (int n = 2; n <= ranges; ++n) pays |= cs_round_up(cs_ceil_div(len, n), 32) + join + n < cs_round_up(len, 32);
+        for (int n = 2; n <= ranges && !pays; ++n) pays = cs_round_up(cs_ceil_div(len, n), 32) + join + n < cs_round_up(len, 32);
         one |= !pays;
     }
     const int most = one ? 1 : ranges;
