@@ -504,6 +504,70 @@ int cs_paged_attention(const cs_pages* p, const void* q, int64_t q_row, int64_t 
                        void* stream);
 
 /* ------------------------------------------------------------------------------------
+ * Paged cache held in 4 bits  (Sec. 3.2, App. B.1-B.2, as above: the same step over a smaller cache)
+ *
+ * The pages, tables, lengths and rows of a call are those of cs_pages; what is stored differs.  Keys and
+ * values are quantised as they are written: an element is one of
+ *   0, 1/2, 1, 3/2, 2, 3, 4, 6            (code 0 .. 7, 8 more for a negative one)
+ * times the scale of its group, which is 32 consecutive elements of a head's row.  The scale is a power of
+ * two, the smallest s of 2^-125 .. 2^125 with max|x| <= 7 s (7 rounds to 6, by no more than half the step
+ * that 6 has below it), kept as its exponent + 127 in one byte; above 7 * 2^125 magnitudes become 6 * 2^125.
+ * An element becomes the code nearest to x / s, of two equally near ones the even one.  A group that
+ * holds a NaN or an infinity has scale byte 255, which makes all its values NaN.  This is the e2m1 / e8m0 format
+ * of the OCP microscaling specification 1.0 (whose own rule for the scale is another): 17/32 byte an element.
+ *
+ * Codes: byte j of a row has elements 2j (low half) and 2j + 1.  Scales: byte [group][slot] of a page and
+ * head, the slots of a page contiguous.  A token's bytes are its own: rows that go to different slots never
+ * share one.
+ *
+ * Limits as above, but: head_dim a multiple of 32 up to 256, page_size a power of two in 32..32768; the
+ * strides of codes count bytes and are multiples of 16, k_token and v_token at least head_dim / 2; those of
+ * scales too, ks_group and vs_group at least page_size (where there is more than one to step over).
+ * Keys and values of live tokens must be finite, values that are attended to below 2^90 (a float32 sum holds
+ * 2^30 of them times probabilities of up to 2^8); what may hold anything above may do so here.
+ * There is no backward pass.
+ * ---------------------------------------------------------------------------------- */
+typedef struct cs_pages_fp4 {
+    uint8_t *k, *v;                         /* device pools of codes of one layer */
+    uint8_t *k_scale, *v_scale;             /* device pools of scales */
+    int64_t k_page, k_head, k_token;        /* strides of k, in bytes */
+    int64_t v_page, v_head, v_token;
+    int64_t ks_page, ks_head, ks_group;     /* strides of k_scale, in bytes */
+    int64_t vs_page, vs_head, vs_group;
+    const int32_t* table;                   /* device [batch][table_stride], table_pages entries of a row in use */
+    int64_t table_stride;
+    const int32_t* len;                     /* device [batch] */
+    int32_t batch, table_pages, n_pages, page_size;
+    int32_t n_kv_heads, head_dim;
+    int32_t reserved[2];                    /* 0 */
+} cs_pages_fp4;
+
+/* Quantises R new key and value rows [R][n_kv_heads][head_dim] into the pages of their streams, at positions
+ * L_b + i.  src_dtype CS_F32 or CS_BF16.  Keys come rotated (cs_op_qk_norm_rope).  Where two rows go to the same
+ * slot (a page named twice), either's bytes may stay, code and scale apart.  Asynchronous on `stream`. */
+int cs_paged_fp4_append(const cs_pages_fp4* p, int32_t src_dtype, const void* k, int64_t k_row, int64_t k_head,
+                        const void* v, int64_t v_row, int64_t v_head, const int32_t* d_row0, int32_t R, void* stream);
+
+/* The values of R tokens as rows [R][n_kv_heads][head_dim]: row i of stream b is what the slot of position
+ * first[b] + i holds (first: device [batch]; NULL: the lengths, the rows that an append with the same offsets has
+ * written).  dst_dtype CS_F32 or CS_BF16, exact in both.  A position that is negative or has no page gives
+ * zeros; rows from d_row0[batch] on are left as they were.  Slots beyond len are read like others.  The outputs may
+ * not overlap.  Asynchronous on `stream`. */
+int cs_paged_fp4_read(const cs_pages_fp4* p, int32_t dst_dtype, void* k, int64_t k_row, int64_t k_head, void* v, int64_t v_row,
+                      int64_t v_head, const int32_t* d_row0, const int32_t* first, int32_t R, void* stream);
+
+/* cs_paged_attention over such a cache: same rows, mask, scale, hints, workspace rules and results, k and v being
+ * the values of the codes.  q_dtype CS_F32 or CS_BF16 is the type of q and out.  With CS_BF16 queries the
+ * probabilities are rounded to bfloat16 for the product with V; float32 queries and probabilities go into the
+ * products as three bfloat16 parts, which is all of them. */
+int64_t cs_paged_fp4_attention_workspace(const cs_pages_fp4* p, int32_t q_dtype, int32_t n_heads, int32_t has_row0, int32_t R,
+                                         int32_t max_rows, int64_t max_len);
+int cs_paged_fp4_attention(const cs_pages_fp4* p, int32_t q_dtype, const void* q, int64_t q_row, int64_t q_head, int32_t n_heads,
+                           const int32_t* d_row0, int32_t R, float scale, int32_t window, int32_t max_rows, int64_t max_len,
+                           void* out, int64_t out_row, int64_t out_head, void* workspace, int64_t workspace_bytes,
+                           void* stream);
+
+/* ------------------------------------------------------------------------------------
  * Instrumentation: per-kernel-class device timing with HIP events recorded on the stream
  * the kernels run on.  cs_profile_enable(mask) selects classes (0 = off, the default);
  * cs_profile_read synchronises the device and returns the summed duration and the number

@@ -34,6 +34,7 @@ EXPORTS = [
     "cs_index_reset", "cs_index_find_match_batch_dev", "cs_op_gemm", "cs_op_attention", "cs_op_argmax_accept",
     "cs_set_plain_kernels", "cs_set_prompt_block_rows", "cs_kv_set_len_dev", "cs_profile_enable", "cs_profile_reset",
     "cs_profile_read", "cs_op_qk_norm_rope", "cs_paged_append", "cs_paged_attention", "cs_paged_attention_workspace",
+    "cs_paged_fp4_append", "cs_paged_fp4_read", "cs_paged_fp4_attention", "cs_paged_fp4_attention_workspace",
 ]
 
 CS_PROF = {"scan": 1, "gemm": 2, "attn": 4, "attn_merge": 8, "argmax": 16, "lm_head": 32}
@@ -71,6 +72,15 @@ class cs_pages(C.Structure):
                 + [(n, C.c_int64) for n in ("k_page", "k_head", "k_token", "v_page", "v_head", "v_token")]
                 + [("table", C.c_void_p), ("table_stride", C.c_int64), ("len", C.c_void_p)]
                 + [(n, C.c_int32) for n in ("batch", "table_pages", "n_pages", "page_size", "n_kv_heads", "head_dim", "dtype", "reserved")])
+
+
+class cs_pages_fp4(C.Structure):
+    _fields_ = ([(n, C.c_void_p) for n in ("k", "v", "k_scale", "v_scale")]
+                + [(n, C.c_int64) for n in ("k_page", "k_head", "k_token", "v_page", "v_head", "v_token",
+                                            "ks_page", "ks_head", "ks_group", "vs_page", "vs_head", "vs_group")]
+                + [("table", C.c_void_p), ("table_stride", C.c_int64), ("len", C.c_void_p)]
+                + [(n, C.c_int32) for n in ("batch", "table_pages", "n_pages", "page_size", "n_kv_heads", "head_dim")]
+                + [("reserved", C.c_int32 * 2)])
 
 
 class cs_merged_stats(C.Structure):
@@ -144,6 +154,12 @@ def load_library(path: Optional[str] = None) -> C.CDLL:
     lib.cs_paged_attention_workspace.restype = i64
     lib.cs_paged_attention.argtypes = [C.POINTER(cs_pages), vp, i64, i64, i32, vp, i32, f32, i32, i32, i64, vp, i64, i64,
                                        vp, i64, vp]
+    lib.cs_paged_fp4_append.argtypes = [C.POINTER(cs_pages_fp4), i32, vp, i64, i64, vp, i64, i64, vp, i32, vp]
+    lib.cs_paged_fp4_read.argtypes = [C.POINTER(cs_pages_fp4), i32, vp, i64, i64, vp, i64, i64, vp, vp, i32, vp]
+    lib.cs_paged_fp4_attention_workspace.argtypes = [C.POINTER(cs_pages_fp4), i32, i32, i32, i32, i32, i64]
+    lib.cs_paged_fp4_attention_workspace.restype = i64
+    lib.cs_paged_fp4_attention.argtypes = [C.POINTER(cs_pages_fp4), i32, vp, i64, i64, i32, vp, i32, f32, i32, i32, i64, vp, i64, i64,
+                                           vp, i64, vp]
     lib.cs_profile_enable.argtypes = [i32]
     lib.cs_profile_enable.restype = None
     lib.cs_profile_reset.restype = None
@@ -859,6 +875,134 @@ def cs_paged_attention(pages: Pages, q: torch.Tensor, row0: Optional[torch.Tenso
     _check(lib.cs_paged_attention(pages.ref, *qp, H, r0, R, 1.0 / math.sqrt(hd) if scale is None else scale, window,
                                   max_rows, max_len, *_rows3(out, "out", qs), _ptr(workspace),
                                   0 if workspace is None else workspace.numel() * workspace.element_size(), _stream_of(dev)))
+    return out
+
+
+class PagesFP4:
+    """cs_pages_fp4: the caller's pools, page table and lengths of one layer of a paged cache held in 4 bits.  k and v: uint8 codes
+    [n_pages][n_kv_heads][page_size][head_dim/2], any strides with contiguous rows (a token-major pool is passed transposed);
+    k_scale and v_scale: uint8 [n_pages][n_kv_heads][head_dim/32][page_size], any strides with contiguous slots; table: int32
+    [batch][pages]; length: int32 [batch].  The tensors stay the caller's: tables and lengths may be changed in place between calls."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor, table: torch.Tensor,
+                 length: torch.Tensor):
+        self.device = _device_of((k, v, k_scale, v_scale, table, length))
+        if k.dim() != 4 or k.shape != v.shape or k_scale.dim() != 4 or k_scale.shape != v_scale.shape:
+            raise TypeError("k and v must be [n_pages][n_kv_heads][page_size][head_dim/2], the scales [n_pages][n_kv_heads][head_dim/32][page_size]")
+        if any(t.dtype is not torch.uint8 for t in (k, v, k_scale, v_scale)):
+            raise TypeError("codes and scales must be uint8")
+        if any(t.shape[3] > 1 and t.stride(3) != 1 for t in (k, v, k_scale, v_scale)):
+            raise TypeError("the codes of a row and the scales of a page's slots must be contiguous")
+        n_pages, heads, size, half = k.shape
+        if half % 16 or k_scale.shape != (n_pages, heads, half // 16, size):
+            raise TypeError(f"codes {list(k.shape)} need scales {[n_pages, heads, half // 16, size]} and rows of whole groups of 32 elements")
+        if table.dtype != torch.int32 or table.dim() != 2 or (table.shape[1] > 1 and table.stride(1) != 1):
+            raise TypeError("table must be int32 [batch][pages] with contiguous rows")
+        _vec(length, "length", torch.int32, table.shape[0])
+        _fits(*k.shape, *table.shape)
+        self.k, self.v, self.k_scale, self.v_scale, self.table, self.length = k, v, k_scale, v_scale, table, length
+        st = [t.stride(d) if t.shape[d] > 1 else (0 if d < 2 else t.shape[3]) for t in (k, v, k_scale, v_scale) for d in range(3)]
+        self.c = cs_pages_fp4(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), *st, table.data_ptr(),
+                              table.stride(0) if table.shape[0] > 1 else table.shape[1], length.data_ptr(), table.shape[0],
+                              table.shape[1], n_pages, size, heads, 2 * half)
+        self.ref = C.byref(self.c)
+
+    _row0 = Pages._row0
+
+
+def cs_paged_fp4_append(pages: PagesFP4, k: torch.Tensor, v: torch.Tensor, row0: Optional[torch.Tensor] = None, stream=None):
+    """New rows k, v [R][KVH][hd] (bfloat16 or float32, keys rotated) are quantised into the pages of their streams, at positions
+    length[b] + i.  row0: int32 [batch + 1] offsets of the streams' rows, None: equal shares."""
+    _forward_only(k, v)
+    dev = _device_of((pages.k, k, v, row0))
+    if _elsewhere(dev, stream):
+        with _on(dev, stream):
+            return cs_paged_fp4_append(pages, k, v, row0)
+    R, c = k.shape[0], pages.c
+    _fits(R)
+    want = (R, c.n_kv_heads, c.head_dim)
+    dt = _dtype(k, "k")
+    if v.dtype != k.dtype:
+        raise TypeError("k and v must be of one type")
+    _check(load_library().cs_paged_fp4_append(pages.ref, dt, *_rows3(k, "k", want), *_rows3(v, "v", want), pages._row0(row0), R,
+                                              _stream_of(dev)))
+
+
+def cs_paged_fp4_read(pages: PagesFP4, first: Optional[torch.Tensor] = None, R: Optional[int] = None, row0: Optional[torch.Tensor] = None,
+                      dtype: Optional[torch.dtype] = None, out=None, stream=None):
+    """The values of R tokens as rows (k, v) [R][KVH][hd]: row i of stream b is what the cache holds at position first[b] + i (int32
+    [batch]; None: the lengths).  row0: int32 [batch + 1] offsets of the streams' rows, None: equal shares.  In new tensors of
+    `dtype` (bfloat16 by default; both types hold the values exactly), or in out = (k_out, v_out), where R is their rows.  Rows
+    without a page are zeros, rows behind the last stream are left as they were."""
+    ko, vo = out if out is not None else (None, None)
+    _forward_only(ko, vo)
+    dev = _device_of((pages.k, first, row0, ko, vo))
+    if _elsewhere(dev, stream):
+        with _on(dev, stream):
+            return cs_paged_fp4_read(pages, first, R, row0, dtype, out)
+    c = pages.c
+    if out is None:
+        if R is None:
+            raise ValueError("R says how many rows are read, where there is no out")
+        want = (R, c.n_kv_heads, c.head_dim)
+        ko, vo = (torch.zeros if row0 is not None else torch.empty)((2, *want), dtype=dtype or torch.bfloat16, device=pages.device).unbind()
+    else:
+        if ko is None or vo is None or ko.dtype != vo.dtype or (dtype is not None and ko.dtype != dtype):
+            raise TypeError("out must be (k_out, v_out) of one type, dtype if that is given")
+        if R is not None and R != ko.shape[0]:
+            raise ValueError("R is the number of rows of out")
+        want = (ko.shape[0], c.n_kv_heads, c.head_dim)
+    _fits(want[0])
+    _check(load_library().cs_paged_fp4_read(pages.ref, _dtype(ko, "k_out"), *_rows3(ko, "k_out", want), *_rows3(vo, "v_out", want),
+                                            pages._row0(row0), _vec(first, "first", torch.int32, c.batch), want[0], _stream_of(dev)))
+    return ko, vo
+
+
+def cs_paged_fp4_attention_workspace(pages: PagesFP4, n_heads: int, R: int, row0: bool = False, max_rows: int = 0, max_len: int = 0,
+                                     dtype: torch.dtype = torch.bfloat16) -> int:
+    """Bytes that cs_paged_fp4_attention needs for these arguments (row0: whether it is given offsets; dtype: of the queries)."""
+    _fits(n_heads, R, max_rows)
+    if dtype not in _DTYPES:
+        raise TypeError("queries must be float32 or bfloat16")
+    need = load_library().cs_paged_fp4_attention_workspace(pages.ref, _DTYPES[dtype], n_heads, 1 if row0 else 0, R, max_rows, max_len)
+    if need < 0:
+        _check(need)
+    return need
+
+
+def cs_paged_fp4_attention(pages: PagesFP4, q: torch.Tensor, row0: Optional[torch.Tensor] = None, scale: Optional[float] = None,
+                           window: int = 0, max_rows: int = 0, max_len: int = 0, out: Optional[torch.Tensor] = None,
+                           workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """q [R][H][hd], bfloat16 or float32, rotated.  Returns [R][H][hd] of that type (in `out` if given, which may be q; rows behind
+    the last stream are left as they were).  The other arguments are those of cs_paged_attention; a workspace of its own is as
+    large as cs_paged_fp4_attention_workspace says."""
+    _forward_only(q, out)
+    dev = _device_of((pages.k, q, row0, out, workspace))
+    if _elsewhere(dev, stream):
+        with _on(dev, stream):
+            return cs_paged_fp4_attention(pages, q, row0, scale, window, max_rows, max_len, out, workspace)
+    qs, c = q.shape, pages.c
+    dt, qp = _dtype(q, "q"), _rows3(q, "q", qs)
+    R, H, hd = qs
+    _fits(R, H, window, max_rows)
+    if hd != c.head_dim:
+        raise ValueError(f"q must have the cache's head_dim, {c.head_dim}")
+    if out is None:
+        out = q.new_empty(qs)
+    elif out.dtype != q.dtype:
+        raise TypeError("out must have the type of q")
+    lib, r0 = load_library(), pages._row0(row0)
+    if workspace is None:
+        need = lib.cs_paged_fp4_attention_workspace(pages.ref, dt, H, 1 if r0 else 0, R, max_rows, max_len)
+        if need > 0:
+            workspace = q.new_empty(need, dtype=torch.uint8)
+        elif need < 0:
+            _check(need)
+    elif not workspace.is_contiguous():
+        raise ValueError("workspace must be contiguous")
+    _check(lib.cs_paged_fp4_attention(pages.ref, dt, *qp, H, r0, R, 1.0 / math.sqrt(hd) if scale is None else scale, window,
+                                      max_rows, max_len, *_rows3(out, "out", qs), _ptr(workspace),
+                                      0 if workspace is None else workspace.numel() * workspace.element_size(), _stream_of(dev)))
     return out
 
 

@@ -11,7 +11,7 @@ CSRC = os.path.join(HERE, "csrc")
 BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libcopyspec.so")
 SOURCES = ["cs_api.hip", "cs_scan.hip", "cs_index.hip", "cs_elem.hip", "cs_gemm.hip", "cs_attn.hip",
-           "cs_paged.hip", "cs_paged_attn.hip"]
+           "cs_paged.hip", "cs_paged_attn.hip", "cs_paged_fp4.hip", "cs_paged_fp4_attn.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fno-gpu-rdc",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
@@ -22,7 +22,8 @@ FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fno-gpu-rdc",
 # maximum is guarded before it is subtracted), so the maxima of their softmax need no
 # canonicalising copy of every operand: 18 fewer vector instructions per 32-token block.
 # (Keys and values of live tokens are finite by contract; dead ones are masked before a maximum sees them.)
-EXTRA_FLAGS = {"cs_attn.hip": ["-fno-honor-nans"], "cs_paged_attn.hip": ["-fno-honor-nans"]}
+EXTRA_FLAGS = {"cs_attn.hip": ["-fno-honor-nans"], "cs_paged_attn.hip": ["-fno-honor-nans"],
+               "cs_paged_fp4_attn.hip": ["-fno-honor-nans"]}
 
 
 def _compile(src: str) -> str:

@@ -1,0 +1,315 @@
+// What goes into a paged cache of 4-bit elements and what comes out of it again: the append quantises new
+// key and value rows into the pages of their streams (Sec. 3.2: the block is appended to the context; App.
+// B.1-B.2: the per-layer K, V), the read gives the values back.
+//
+//   s = 2^e, the smallest with max|x| <= 7 s over a group of 32;   code = e2m1(x / s);   value = e2m1(code) s
+//
+// Both are streams of memory: a lane has eight consecutive elements of a head's row (16 bytes of a
+// bfloat16 row, one dword of codes), four neighbours have a group.  With x = 2^e' m, 1 <= m < 2, the scale's
+// exponent is e' - 2, one more where m > 7/4: an addition to the bits of max|x| that carries into the exponent
+// there, so scale and codes are exact integer and power-of-two arithmetic and one rounding.
+#include <algorithm>
+
+#include "cs_paged_fp4.h"
+
+// ---- argument checks -------------------------------------------------------------------
+#define CS_MAX_BSTRIDE ((int64_t)1 << 40)
+
+static int check_pool(const char* who, const char* name, const void* base, int64_t page, int64_t head, int64_t inner, int64_t least,
+                      int64_t steps, int64_t width) {
+    CS_TRY(cs_check_rows(who, name, base, page, head, 1));
+    CS_REQUIRE(steps < 2 || inner >= least, CS_E_ARG, "%s: an inner stride of %s is less than %lld bytes", who, name, (long long)least);
+    CS_REQUIRE(inner >= 0 && inner <= CS_MAX_BSTRIDE && inner % 16 == 0, CS_E_ARG, "%s: an inner stride of %s is no multiple of 16 bytes", who, name);
+    CS_REQUIRE((steps - 1) * inner + width < (int64_t)1 << 31, CS_E_UNSUPPORTED, "%s: a page of %s spans 2^31 bytes or more", who, name);
+    return CS_OK;
+}
+
+int cs_fp4_check(const char* who, const cs_pages_fp4* p) {
+    CS_REQUIRE(p, CS_E_ARG, "%s: NULL pages", who);
+    CS_REQUIRE(p->reserved[0] == 0 && p->reserved[1] == 0, CS_E_ARG, "%s: a reserved field is not 0", who);
+    CS_REQUIRE(p->batch >= 0 && p->n_pages >= 1 && p->n_kv_heads >= 1 && p->table_pages >= 1, CS_E_ARG,
+               "%s: a size of the pages is out of range", who);
+    CS_REQUIRE(p->batch == 0 || (p->table && p->len), CS_E_ARG, "%s: NULL table or lengths", who);
+    CS_REQUIRE(p->table_stride >= p->table_pages, CS_E_ARG, "%s: table_stride is less than table_pages", who);
+    CS_REQUIRE(p->head_dim >= 32 && p->head_dim <= 256 && p->head_dim % 32 == 0, CS_E_UNSUPPORTED,
+               "%s: head_dim must be a multiple of 32 in 32..256", who);
+    CS_REQUIRE(p->page_size >= 32 && p->page_size <= 32768 && (p->page_size & (p->page_size - 1)) == 0, CS_E_UNSUPPORTED,
+               "%s: page_size must be a power of two in 32..32768", who);
+    CS_REQUIRE((int64_t)p->table_pages * p->page_size <= (int64_t)1 << 30, CS_E_UNSUPPORTED,
+               "%s: table_pages * page_size exceeds 2^30", who);
+    CS_REQUIRE(p->batch <= 65536 && p->n_kv_heads <= 4096, CS_E_UNSUPPORTED, "%s: too many streams or heads", who);
+    const int hd = p->head_dim, P = p->page_size;
+    CS_TRY(check_pool(who, "k", p->k, p->k_page, p->k_head, p->k_token, hd / 2, P, hd / 2));
+    CS_TRY(check_pool(who, "v", p->v, p->v_page, p->v_head, p->v_token, hd / 2, P, hd / 2));
+    CS_TRY(check_pool(who, "k_scale", p->k_scale, p->ks_page, p->ks_head, p->ks_group, P, hd / CS_FP4_GROUP, P));
+    CS_TRY(check_pool(who, "v_scale", p->v_scale, p->vs_page, p->vs_head, p->vs_group, P, hd / CS_FP4_GROUP, P));
+    return CS_OK;
+}
+
+int cs_fp4_view(const char* who, const cs_pages_fp4* p, const int32_t* d_row0, int32_t R, cs_fp4_dev* d) {
+    cs_pages q = {};
+    q.table = p->table, q.table_stride = p->table_stride, q.len = p->len;
+    q.batch = p->batch, q.table_pages = p->table_pages, q.n_pages = p->n_pages, q.page_size = p->page_size;
+    q.n_kv_heads = p->n_kv_heads, q.head_dim = p->head_dim, q.dtype = CS_BF16;
+    CS_TRY(cs_pages_view(who, &q, d_row0, R, &d->d));
+    d->k = p->k, d->v = p->v, d->ks = p->k_scale, d->vs = p->v_scale;
+    d->k_page = p->k_page, d->k_head = p->k_head, d->k_token = p->k_token;
+    d->v_page = p->v_page, d->v_head = p->v_head, d->v_token = p->v_token;
+    d->ks_page = p->ks_page, d->ks_head = p->ks_head, d->ks_group = p->ks_group;
+    d->vs_page = p->vs_page, d->vs_head = p->vs_head, d->vs_group = p->vs_group;
+    return CS_OK;
+}
+
+// ---- rows and their places --------------------------------------------------------------
+#define F4_THREADS 256
+#define F4_ROWS 64            // most rows of a workgroup: a lane each for their places
+
+struct f4_side {
+    void* rows;
+    int64_t row, head;
+};
+struct f4_args {
+    f4_side s[2];             // keys, values
+    const int32_t* first;     // position of row 0 of every stream, or NULL: its length
+    int rpw, lanes_log2, segs;
+};
+
+// (page, position) of row r0 + lane, for the nr lanes of a wave that have one; page -1: nowhere, -2: nobody's row
+// (first: position of every stream's row 0, or NULL: its length)
+__device__ __forceinline__ int2 f4_place(const cs_pages_dev& D, const int32_t* first, int r0, int nr, int lane) {
+    const int B = D.p.batch, r = r0 + lane;
+    int b = B;
+    if (!D.row0) b = r / D.rows;
+    else if (B <= 64) {
+        // as many streams end at or before a row: one load, and a count over the wave for every row
+        const int end = lane < B ? D.row0[lane + 1] : 0x7fffffff;
+        for (int i = 0; i < nr; ++i) {
+            const int n = __popcll(__ballot(end <= r0 + i));
+            b = lane == i ? n : b;
+        }
+    } else {
+        int lo = 0, hi = B;                                      // the first stream that ends behind the row
+        while (lo < hi) {
+            const int mid = (lo + hi) >> 1;
+            const bool ended = D.row0[mid + 1] <= r;
+            lo = ended ? mid + 1 : lo;
+            hi = ended ? hi : mid;
+        }
+        b = lo;
+    }
+    if (lane >= nr || b >= B) return make_int2(-2, 0);
+    const int2 sr = cs_stream_rows(D, b);
+    if (r < sr.x || r - sr.x >= sr.y) return make_int2(-2, 0);
+    const int64_t at = (int64_t)(first ? first[b] : cs_stream_len(D, b)) + (r - sr.x);
+    if (at < 0 || at >= D.cap) return make_int2(-1, 0);
+    const int page = D.p.table[b * D.p.table_stride + (at >> D.page_log2)];
+    return make_int2(page < 0 || page >= D.p.n_pages ? -1 : page, (int)at);
+}
+
+// (row, head) pairs of a workgroup, keys' heads before values': a lane's pairs lie `per` apart
+struct f4_tasks {
+    int heads, dr, dh;
+    __device__ __forceinline__ f4_tasks(int per, int heads) : heads(heads), dr(per / heads), dh(per % heads) {}
+    __device__ __forceinline__ int2 at(int i) const { return make_int2(i / heads, i % heads); }
+    __device__ __forceinline__ int2 next(int2 t) const {
+        const int h = t.y + dh, over = h >= heads;
+        return make_int2(t.x + dr + over, over ? h - heads : h);
+    }
+};
+
+template <typename T>
+struct f4_raw;
+template <>
+struct f4_raw<bf16_t> { u32x4 x; };
+template <>
+struct f4_raw<float> { f32x4 x[2]; };
+__device__ __forceinline__ void f4_load(f4_raw<bf16_t>& o, const bf16_t* p) { o.x = *reinterpret_cast<const u32x4*>(p); }
+__device__ __forceinline__ void f4_load(f4_raw<float>& o, const float* p) {
+    o.x[0] = *reinterpret_cast<const f32x4*>(p);
+    o.x[1] = *reinterpret_cast<const f32x4*>(p + 4);
+}
+__device__ __forceinline__ void f4_floats(const f4_raw<bf16_t>& r, float* o) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        o[2 * j] = __uint_as_float(r.x[j] << 16);
+        o[2 * j + 1] = __uint_as_float(r.x[j] & 0xffff0000u);
+    }
+}
+__device__ __forceinline__ void f4_floats(const f4_raw<float>& r, float* o) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) o[j] = r.x[j >> 2][j & 3];
+}
+
+// the largest of the four lanes of a quad
+__device__ __forceinline__ unsigned f4_quad_max(unsigned v) {
+    v = max(v, (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, 0xb1, 0xf, 0xf, true));       // lanes 1 0 3 2
+    return max(v, (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, 0x4e, 0xf, 0xf, true));    // lanes 2 3 0 1
+}
+
+// ---- append -----------------------------------------------------------------------------
+
+template <typename TI>
+__global__ __launch_bounds__(F4_THREADS) void k_paged_fp4_append(cs_fp4_dev F, f4_args A) {
+    __shared__ int2 dest[F4_ROWS];
+    const cs_pages_dev& D = F.d;
+    const int tid = threadIdx.x, KVH = D.p.n_kv_heads, heads = 2 * KVH;
+    const int r0 = (int)cs_paged_wg() * A.rpw, nr = min(A.rpw, D.R - r0);
+    const int seg = tid & ((1 << A.lanes_log2) - 1), per = F4_THREADS >> A.lanes_log2;
+    const bool on = seg < A.segs;
+    const f4_tasks T(per, heads);
+    int2 t = T.at(tid >> A.lanes_log2);
+    auto request = [&](int2 t, f4_raw<TI>& x) {
+        const f4_side& s = A.s[t.y >= KVH];
+        f4_load(x, (const TI*)s.rows + (int64_t)(r0 + t.x) * s.row + (int64_t)(t.y >= KVH ? t.y - KVH : t.y) * s.head + seg * 8);
+    };
+    f4_raw<TI> cur, nxt;
+    // rows behind the last stream are not read; the others are in flight while their places are looked up
+    const int live = D.row0 ? min(nr, D.row0[D.p.batch] - r0) : nr;
+    if (t.x < live && on) request(t, cur);
+    if (tid < CS_WAVE) {
+        const int2 at = f4_place(D, nullptr, r0, nr, tid);
+        if (tid < nr) dest[tid] = at;
+    }
+    __syncthreads();
+    while (t.x < live) {
+        const int2 n = T.next(t);
+        if (n.x < live && on) request(n, nxt);
+        float x[8];
+        f4_floats(cur, x);
+        unsigned top = 0;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) top = max(top, __float_as_uint(x[j]) & 0x7fffffffu);
+        top = f4_quad_max(top);                                // (of integers: a NaN counts as more than an infinity)
+        const int e = (int)((top + 0x1fffffu) >> 23) - 2;
+        const unsigned scale = top >= 0x7f800000u ? 255u : (unsigned)min(max(e, CS_FP4_SCALE_MIN), CS_FP4_SCALE_MAX);
+        const float s = __uint_as_float(scale << 23);
+        unsigned codes = 0;
+        codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, x[0], x[1], s, 0);
+        codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, x[2], x[3], s, 1);
+        codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, x[4], x[5], s, 2);
+        codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, x[6], x[7], s, 3);
+        const int2 at = dest[t.x];
+        if (at.x >= 0 && on) {
+            const bool is_v = t.y >= KVH;
+            const int g = is_v ? t.y - KVH : t.y, slot = at.y & (D.p.page_size - 1);
+            uint8_t* c = is_v ? F.v + at.x * F.v_page + g * F.v_head + slot * F.v_token : F.k + at.x * F.k_page + g * F.k_head + slot * F.k_token;
+            *reinterpret_cast<unsigned*>(c + seg * 4) = codes;
+            uint8_t* f = is_v ? F.vs + at.x * F.vs_page + g * F.vs_head + (seg >> 2) * F.vs_group : F.ks + at.x * F.ks_page + g * F.ks_head + (seg >> 2) * F.ks_group;
+            if ((seg & 3) == 0) f[slot] = (uint8_t)scale;
+        }
+        cur = nxt;
+        t = n;
+    }
+}
+
+// ---- read -------------------------------------------------------------------------------
+__device__ __forceinline__ void f4_store(bf16_t* p, bf16x8 v) { *reinterpret_cast<bf16x8*>(p) = v; }
+__device__ __forceinline__ void f4_store(float* p, bf16x8 v) {
+#pragma unroll
+    for (int u = 0; u < 8; u += 4) *reinterpret_cast<f32x4*>(p + u) = (f32x4){(float)v[u], (float)v[u + 1], (float)v[u + 2], (float)v[u + 3]};
+}
+
+template <typename TO>
+__global__ __launch_bounds__(F4_THREADS) void k_paged_fp4_read(cs_fp4_dev F, f4_args A) {
+    __shared__ int2 from[F4_ROWS];
+    const cs_pages_dev& D = F.d;
+    const int tid = threadIdx.x, KVH = D.p.n_kv_heads, heads = 2 * KVH;
+    const int r0 = (int)cs_paged_wg() * A.rpw, nr = min(A.rpw, D.R - r0);
+    const int seg = tid & ((1 << A.lanes_log2) - 1), per = F4_THREADS >> A.lanes_log2;
+    if (tid < CS_WAVE) {
+        const int2 at = f4_place(D, A.first, r0, nr, tid);
+        if (tid < nr) from[tid] = at;
+    }
+    __syncthreads();
+    if (seg >= A.segs) return;
+    const f4_tasks T(per, heads);
+    int2 t = T.at(tid >> A.lanes_log2);
+    auto request = [&](int2 t, unsigned& codes, unsigned& scale) {
+        const int2 at = from[t.x];
+        codes = scale = 0;
+        if (at.x < 0) return;
+        const bool is_v = t.y >= KVH;
+        const int g = is_v ? t.y - KVH : t.y, slot = at.y & (D.p.page_size - 1);
+        const uint8_t* c = is_v ? F.v + at.x * F.v_page + g * F.v_head + slot * F.v_token : F.k + at.x * F.k_page + g * F.k_head + slot * F.k_token;
+        const uint8_t* f = is_v ? F.vs + at.x * F.vs_page + g * F.vs_head + (seg >> 2) * F.vs_group : F.ks + at.x * F.ks_page + g * F.ks_head + (seg >> 2) * F.ks_group;
+        codes = *reinterpret_cast<const unsigned*>(c + seg * 4);
+        scale = f[slot];
+    };
+    unsigned codes, scale, codes_n = 0, scale_n = 0;
+    if (t.x < nr) request(t, codes, scale);
+    while (t.x < nr) {
+        const int2 n = T.next(t);
+        if (n.x < nr) request(n, codes_n, scale_n);
+        if (from[t.x].x != -2) {
+            const f4_side& s = A.s[t.y >= KVH];
+            f4_store((TO*)s.rows + (int64_t)(r0 + t.x) * s.row + (int64_t)(t.y >= KVH ? t.y - KVH : t.y) * s.head + seg * 8,
+                     cs_fp4_decode(codes, scale << 23));
+        }
+        codes = codes_n;
+        scale = scale_n;
+        t = n;
+    }
+}
+
+// ---- entry points -----------------------------------------------------------------------
+// what both have of their arguments; rows per workgroup: see the calls
+static int f4_prepare(const char* who, const cs_pages_fp4* p, int32_t dtype, const void* k, int64_t k_row, int64_t k_head, const void* v,
+                      int64_t v_row, int64_t v_head, const int32_t* d_row0, int32_t R, cs_fp4_dev* F, f4_args* A) {
+    CS_TRY(cs_fp4_check(who, p));
+    CS_REQUIRE(dtype == CS_F32 || dtype == CS_BF16, CS_E_ARG, "%s: rows of unknown type %d", who, dtype);
+    CS_TRY(cs_fp4_view(who, p, d_row0, R, F));
+    if (R == 0 || p->batch == 0) return CS_OK;
+    const size_t esz = dtype == CS_BF16 ? 2 : 4;
+    CS_TRY(cs_check_rows(who, "k rows", k, k_row, k_head, esz));
+    CS_TRY(cs_check_rows(who, "v rows", v, v_row, v_head, esz));
+    A->s[0] = {(void*)k, k_row, k_head};
+    A->s[1] = {(void*)v, v_row, v_head};
+    A->segs = p->head_dim / 8;
+    A->lanes_log2 = 2;
+    while (1 << A->lanes_log2 < A->segs) ++A->lanes_log2;
+    return CS_OK;
+}
+static int f4_rows_of(const f4_args& A, const cs_pages_fp4* p, int R) {
+    // a workgroup passes some times over its (row, head) pairs, so that the look-up of the places is shared, while there are
+    // more than enough of them for the chip
+    const int per = F4_THREADS >> A.lanes_log2, rows = (8 * per + 2 * p->n_kv_heads - 1) / (2 * p->n_kv_heads);
+    return std::max(1, std::min(std::min(rows, F4_ROWS), R / 1024));
+}
+
+extern "C" int cs_paged_fp4_append(const cs_pages_fp4* p, int32_t src_dtype, const void* k, int64_t k_row, int64_t k_head, const void* v,
+                                   int64_t v_row, int64_t v_head, const int32_t* d_row0, int32_t R, void* stream) {
+    const char* who = "cs_paged_fp4_append";
+    cs_fp4_dev F;
+    f4_args A = {};
+    CS_TRY(f4_prepare(who, p, src_dtype, k, k_row, k_head, v, v_row, v_head, d_row0, R, &F, &A));
+    if (R == 0 || p->batch == 0) return CS_OK;
+    const int half = p->head_dim / 2, P = p->page_size;
+    CS_TRY(cs_check_apart(who, "k", p->k_page, p->n_pages, p->k_head, p->n_kv_heads, half));
+    CS_TRY(cs_check_apart(who, "v", p->v_page, p->n_pages, p->v_head, p->n_kv_heads, half));
+    CS_TRY(cs_check_apart(who, "k_scale", p->ks_page, p->n_pages, p->ks_head, p->n_kv_heads, P));
+    CS_TRY(cs_check_apart(who, "v_scale", p->vs_page, p->n_pages, p->vs_head, p->n_kv_heads, P));
+    A.rpw = f4_rows_of(A, p, R);
+    const dim3 grid = cs_paged_grid(cs_ceil_div(R, A.rpw));
+    hipStream_t s = (hipStream_t)stream;
+    if (src_dtype == CS_BF16) k_paged_fp4_append<bf16_t><<<grid, F4_THREADS, 0, s>>>(F, A);
+    else k_paged_fp4_append<float><<<grid, F4_THREADS, 0, s>>>(F, A);
+    return cs_launch_ok("k_paged_fp4_append");
+}
+
+extern "C" int cs_paged_fp4_read(const cs_pages_fp4* p, int32_t dst_dtype, void* k, int64_t k_row, int64_t k_head, void* v, int64_t v_row,
+                                 int64_t v_head, const int32_t* d_row0, const int32_t* first, int32_t R, void* stream) {
+    const char* who = "cs_paged_fp4_read";
+    cs_fp4_dev F;
+    f4_args A = {};
+    CS_TRY(f4_prepare(who, p, dst_dtype, k, k_row, k_head, v, v_row, v_head, d_row0, R, &F, &A));
+    if (R == 0 || p->batch == 0) return CS_OK;
+    CS_TRY(cs_check_apart(who, "k rows", k_row, R, k_head, p->n_kv_heads, p->head_dim));
+    CS_TRY(cs_check_apart(who, "v rows", v_row, R, v_head, p->n_kv_heads, p->head_dim));
+    A.first = first;
+    A.rpw = f4_rows_of(A, p, R);
+    const dim3 grid = cs_paged_grid(cs_ceil_div(R, A.rpw));
+    hipStream_t s = (hipStream_t)stream;
+    if (dst_dtype == CS_BF16) k_paged_fp4_read<bf16_t><<<grid, F4_THREADS, 0, s>>>(F, A);
+    else k_paged_fp4_read<float><<<grid, F4_THREADS, 0, s>>>(F, A);
+    return cs_launch_ok("k_paged_fp4_read");
+}

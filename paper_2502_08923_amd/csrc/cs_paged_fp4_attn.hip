@@ -1,0 +1,780 @@
+// Attention of a chunk of new rows per stream over the pages of a cache held in 4 bits (Sec. 3.2: the draft
+// is appended to the context and evaluated in one pass; App. B.2: per-layer K, V).
+//
+//   out[r][h] = sum_t p_t v[t] / sum_t p_t,   p_t = exp(scale * q[r][h] . k[t] - max),   t <= L_b + i, t > L_b + i - window
+//
+// One pass over the tokens with the running maximum and sum of the softmax in float32, as over the wider
+// caches, and cut as there (cs_paged_split.h).  Codes become bfloat16 in registers, two an instruction, with
+// the scale applied and nothing rounded, and the products are those of the bfloat16 matrix instruction, K as
+// the A operand.  Queries and probabilities are NP bfloat16 parts each: one for bfloat16 queries (the
+// probabilities are rounded to V's type in the product, half a step of 2^-8), three for float32 queries, which
+// hold all 24 bits.  Every sum has one order, given by the cut.
+#include <algorithm>
+#include <cmath>
+#include <type_traits>
+
+#include "cs_paged_fp4.h"
+#include "cs_paged_split.h"
+
+template <int NP>
+using f4_qtype = std::conditional_t<NP == 1, bf16_t, float>;
+
+// eight elements at p -> NP parts whose sum they are
+__device__ __forceinline__ void f4_split(const bf16_t* p, bf16x8 (&o)[1]) { o[0] = *reinterpret_cast<const bf16x8*>(p); }
+__device__ __forceinline__ void f4_split8(const float* x, bf16x8 (&o)[3]) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const bf16_t a = (bf16_t)x[j];
+        const float r = x[j] - (float)a;
+        const bf16_t b = (bf16_t)r;
+        o[0][j] = a;
+        o[1][j] = b;
+        o[2][j] = (bf16_t)(r - (float)b);
+    }
+}
+__device__ __forceinline__ void f4_split8(const float* x, bf16x8 (&o)[1]) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) o[0][j] = (bf16_t)x[j];
+}
+__device__ __forceinline__ void f4_split(const float* p, bf16x8 (&o)[3]) {
+    float x[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] = p[j];
+    f4_split8(x, o);
+}
+
+// ---- few query rows: the stream of codes is the bound ---------------------------------------------------
+// Four waves share a tile of up to 48 query rows and take the 32-token blocks of a token range in turn; codes,
+// scores and outputs stay in registers:
+//   S^T[token][row] = K . Q^T           A = 16 key rows, B = query rows
+//   O^T[feature][row] += V^T . P^T      A = 16 features of 32 tokens, B = the probabilities as S^T left them
+// Which token is which row of A, and which feature which k of the first product, is free as long as both
+// operands agree.  Lane (c, g) takes the features g * HD / 4 .. of its key rows, which is 16 bytes of codes
+// under one scale at HD = 128, and row c of half a is token 8 (c / 4) + 4 a + c % 4 of the block, so that the
+// rows of S^T that the lane gets, and the value rows it needs, are the tokens 8g .. 8g + 7: their scales are
+// eight bytes of the page.  Of those value rows a lane loads HD / 16 features each, makes them bfloat16 and
+// turns pairs of tokens with byte permutes into the A fragments: fragment u has feature c * HD / 16 + u in row
+// c.  A page holds whole blocks, so every load has one page and a uniform base: a buffer that ends with the
+// last token.  Loads past it, and of pages that do not exist, return zeros and cost no traffic.
+#define F4N_WAVES 4
+template <int HD>
+struct f4_keys { u32x4 k[2][HD == 256 ? 2 : 1]; u32x2 s[HD == 256 ? 2 : 1]; };
+template <int HD>
+struct f4_values { unsigned v[8][HD == 256 ? 2 : 1]; u32x2 s; };
+
+template <int HD, int NT, int NP>
+__global__ __launch_bounds__(64 * F4N_WAVES, 2) void k_paged_fp4_narrow(cs_fp4_dev F, pa_args A, pa_plan P) {
+    typedef f4_qtype<NP> T_;
+    constexpr int KS = HD / 32, MT = HD / 16, VF = HD / 16;
+    constexpr int KB = HD == 256 ? 2 : 1;                       // 32-feature pieces of a lane's key row (HD 64: half of one)
+    constexpr int VW = HD == 256 ? 2 : 1;                       // dwords of a lane's value row (HD 64: half of one)
+    constexpr int AHEAD = HD == 256 || NT > 1 || NP > 1 ? 2 : 4;         // blocks in flight
+    constexpr int ROWS = 16 * NT, QROW = HD * 2 + 16, QPLANE = ROWS * QROW;
+    constexpr int SLOT = NT * (MT * 1024 + 512);                // a wave's (O, maximum, sum)
+    constexpr int LDS_BYTES = 2 * SLOT > NP * QPLANE ? 2 * SLOT : NP * QPLANE;
+    __shared__ __attribute__((aligned(16))) unsigned char smem[LDS_BYTES];
+    const cs_pages_dev& D = F.d;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int c = lane & 15, g = lane >> 4;
+    const unsigned wg = cs_paged_wg();
+    const int KVH = D.p.n_kv_heads, kvh = wg % KVH;
+    pa_work K;
+    if (!pa_find(D, A.G, A.window, P, wg / KVH, kvh, K)) return;
+    const pa_tile& T = K.T;
+    const int hd = D.p.head_dim;
+    const int n_rows = min(ROWS, T.QR - T.n0);          // live query rows of the tile
+    const int i_lo = T.n0 / A.G, i_hi = (T.n0 + n_rows - 1) / A.G;
+    const int n_tok = min(T.L + i_hi + 1, D.cap);       // tokens that the tile's last row sees
+    const int base = A.window ? max(0, T.L + i_lo - A.window + 1) & ~31 : 0;
+    const int w_begin = (int)min((int64_t)base + (int64_t)K.split * K.chunk, (int64_t)n_tok);
+    const int t_end = K.split == K.nsplit - 1 ? n_tok : (int)min((int64_t)w_begin + K.chunk, (int64_t)n_tok);
+    // blocks between these need no mask
+    const int open_lo = A.window ? T.L + i_hi - A.window + 1 : 0, open_hi = min(T.L + i_lo + 1, D.cap);
+    const int w_first = A.window ? T.L + i_lo - A.window + 1 : 0;       // tokens before it are seen by no row of the tile
+
+    // query rows into LDS
+    for (int idx = tid; idx < ROWS * (HD / 8); idx += 64 * F4N_WAVES) {
+        const int n = idx / (HD / 8), seg = idx % (HD / 8);
+        bf16x8 v[NP];
+#pragma unroll
+        for (int p = 0; p < NP; ++p) v[p] = (bf16x8){0, 0, 0, 0, 0, 0, 0, 0};
+        if (n < n_rows && seg * 8 < hd) {
+            const int i = (T.n0 + n) / A.G, h = kvh * A.G + T.n0 + n - i * A.G;
+            f4_split((const T_*)A.q + (T.row0 + i) * A.q_row + h * A.q_head + seg * 8, v);
+        }
+#pragma unroll
+        for (int p = 0; p < NP; ++p) *reinterpret_cast<bf16x8*>(smem + p * QPLANE + n * QROW + seg * 16) = v[p];
+    }
+    int q_last[NT], q_first[NT];                        // tokens that the lane's query rows see
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+        const int n = nt * 16 + c, i = (T.n0 + n) / A.G;
+        q_last[nt] = n < n_rows ? T.L + i : -1;
+        q_first[nt] = A.window ? T.L + i - A.window + 1 : 0;
+    }
+
+    const uint8_t *Kh = F.k + kvh * F.k_head, *Vh = F.v + kvh * F.v_head, *KSh = F.ks + kvh * F.ks_head, *VSh = F.vs + kvh * F.vs_head;
+    const int32_t* tab = D.p.table + T.b * D.p.table_stride;
+    constexpr unsigned NOWHERE = 0x80000000u;
+    const unsigned kts = (unsigned)F.k_token, vts = (unsigned)F.v_token, kgs = (unsigned)F.ks_group, vgs = (unsigned)F.vs_group;
+    const unsigned row_bytes = hd / 2, n_groups = hd / CS_FP4_GROUP;
+    unsigned koff[2][KB], ksoff[KB], voff[8], vsoff;
+#pragma unroll
+    for (int h = 0; h < KB; ++h) {
+        const int f = g * (HD / 4) + h * 32;
+        const bool there = f < hd;
+#pragma unroll
+        for (int a = 0; a < 2; ++a) koff[a][h] = there ? (8 * (c >> 2) + 4 * a + (c & 3)) * kts + f / 2 : NOWHERE;
+        ksoff[h] = there ? f / CS_FP4_GROUP * kgs + 8 * (c >> 2) : NOWHERE;
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) voff[e] = c * VF < hd ? (8 * g + e) * vts + c * VF / 2 : NOWHERE;
+    vsoff = c * VF < hd ? c * VF / CS_FP4_GROUP * vgs + 8 * g : NOWHERE;
+
+    f32x4 oacc[MT][NT], lacc[NT];
+    float m_run[NT];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+        m_run[nt] = -INFINITY;
+        lacc[nt] = (f32x4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) oacc[mt][nt] = (f32x4){0.f, 0.f, 0.f, 0.f};
+    }
+    const bf16_t one = (bf16_t)1.0f;
+    const bf16x8 ones = (bf16x8){one, one, one, one, one, one, one, one};
+    const float scale2 = A.scale2;
+    const int kshift = 8 * (c & 3);
+    __syncthreads();
+
+    constexpr int STEP = 32 * F4N_WAVES;
+    // a lane holds the page of one of the wave's next 64 blocks
+    for (int seg0 = w_begin; seg0 < t_end; seg0 += 64 * STEP) {
+        const int t_begin = seg0 + 32 * wave;
+        const int n_all = t_begin < t_end ? min(64, (t_end - t_begin + STEP - 1) / STEP) : 0;
+        int page_l = -1;
+        {
+            const int64_t tb = (int64_t)t_begin + (int64_t)lane * STEP;
+            if (tb < t_end) page_l = tab[tb >> D.page_log2];
+            page_l = (unsigned)page_l < (unsigned)D.p.n_pages ? page_l : -1;
+        }
+        auto at = [&](int i) { return t_begin + i * STEP; };
+        auto page_of = [&](int i) { return __builtin_amdgcn_readlane(page_l, i); };
+        auto codes = [&](const uint8_t* head, int64_t page_stride, unsigned ts, int i) {
+            const int t = at(i), page = i < n_all ? page_of(i) : -1, live = min(32, n_tok - t);
+            const unsigned bytes = page >= 0 && live > 0 ? (live - 1) * ts + row_bytes : 0;
+            return cs_rsrc(head + (page >= 0 ? page : 0) * page_stride + (int64_t)(t & (D.p.page_size - 1)) * ts, bytes);
+        };
+        auto scales = [&](const uint8_t* head, int64_t page_stride, unsigned gs, int i) {
+            const int t = at(i), page = i < n_all ? page_of(i) : -1;
+            return cs_rsrc(head + (page >= 0 ? page : 0) * page_stride + (t & (D.p.page_size - 1)), page >= 0 ? (n_groups - 1) * gs + 32 : 0);
+        };
+        auto ldk = [&](f4_keys<HD>& b, int i) {
+            const auto rs = codes(Kh, F.k_page, kts, i);
+#pragma unroll
+            for (int a = 0; a < 2; ++a)
+#pragma unroll
+                for (int h = 0; h < KB; ++h) {
+                    if constexpr (HD == 64) {
+                        const auto x = __builtin_amdgcn_raw_buffer_load_b64(rs, koff[a][h], 0, 0);
+                        b.k[a][h][0] = x[0];
+                        b.k[a][h][1] = x[1];
+                    } else b.k[a][h] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rs, koff[a][h], 0, 0));
+                }
+            const auto ss = scales(KSh, F.ks_page, kgs, i);
+#pragma unroll
+            for (int h = 0; h < KB; ++h) b.s[h] = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(ss, ksoff[h], 0, 0));
+        };
+        auto ldv = [&](f4_values<HD>& b, int i) {
+            const auto rs = codes(Vh, F.v_page, vts, i);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                if constexpr (HD == 64) b.v[e][0] = __builtin_amdgcn_raw_buffer_load_b16(rs, voff[e], 0, 0);
+                else if constexpr (HD == 128) b.v[e][0] = __builtin_amdgcn_raw_buffer_load_b32(rs, voff[e], 0, 0);
+                else {
+                    const auto x = __builtin_amdgcn_raw_buffer_load_b64(rs, voff[e], 0, 0);
+                    b.v[e][0] = x[0];
+                    b.v[e][VW - 1] = x[1];
+                }
+            }
+            b.s = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(scales(VSh, F.vs_page, vgs, i), vsoff, 0, 0));
+        };
+        auto block = [&](f4_keys<HD>& kb, f4_values<HD>& vb, int i) {
+            f32x4 sacc[2][NT];
+#pragma unroll
+            for (int a = 0; a < 2; ++a)
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) sacc[a][nt] = (f32x4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int s = 0; s < KS; ++s) {
+                const int h = s / 4, d = s % 4;
+                bf16x8 kf[2];
+#pragma unroll
+                for (int a = 0; a < 2; ++a) kf[a] = cs_fp4_decode(kb.k[a][h][d], kb.s[h][a] >> kshift << 23);
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int p = 0; p < NP; ++p) {
+                        const bf16x8 qb = *reinterpret_cast<const bf16x8*>(smem + p * QPLANE + (nt * 16 + c) * QROW + g * (HD / 2) + s * 16);
+                        sacc[0][nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[0], qb, sacc[0][nt], 0, 0, 0);
+                        sacc[1][nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[1], qb, sacc[1][nt], 0, 0, 0);
+                    }
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            ldk(kb, i + AHEAD);
+            __builtin_amdgcn_sched_barrier(0);
+            const int t0 = at(i), page = page_of(i);
+            if (t0 < open_lo || t0 + 32 > open_hi || page < 0) {
+                const int t = t0 + 8 * g;
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const bool sees = t + e <= q_last[nt] && t + e >= q_first[nt] && t + e < D.cap && page >= 0;
+                        sacc[e >> 2][nt][e & 3] = sees ? sacc[e >> 2][nt][e & 3] : -INFINITY;
+                    }
+                // codes behind the last token have come as zeros, but scales and what has left every window may be
+                // anything, and 0 * anything must stay 0: with scale byte 0 every code is finite
+                const int e0 = min(max(w_first - t, 0), 8), e1 = min(max(n_tok - t, 0), 8);
+                const uint64_t from = e0 < 8 ? ~(uint64_t)0 << 8 * e0 : 0, to = e1 < 8 ? ~(~(uint64_t)0 << 8 * e1) : ~(uint64_t)0;
+                vb.s[0] &= (unsigned)(from & to);
+                vb.s[1] &= (unsigned)((from & to) >> 32);
+            }
+            bool moved = false;
+            float alpha[NT];
+            bf16x8 pb[NT][NP];
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                float sv[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) sv[e] = sacc[e >> 2][nt][e & 3];
+                float mx = fmaxf(fmaxf(sv[0], sv[1]), sv[2]);
+                mx = fmaxf(fmaxf(mx, sv[3]), sv[4]);
+                mx = fmaxf(fmaxf(mx, sv[5]), fmaxf(sv[6], sv[7]));
+                mx = fa_row4_max(mx) * scale2;
+                // the reference maximum follows the true one only when it is left behind by 2^8
+                const bool up = mx > m_run[nt] + FA_RESCALE_LOG2;
+                const float m_new = up ? mx : m_run[nt];
+                const float m_safe = m_new == -INFINITY ? 0.f : m_new;
+                alpha[nt] = up ? __builtin_amdgcn_exp2f(m_run[nt] - m_safe) : 1.0f;
+                moved |= up;
+                m_run[nt] = m_new;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) sv[e] = __builtin_amdgcn_exp2f(fmaf(sv[e], scale2, -m_safe));
+                f4_split8(sv, pb[nt]);
+            }
+            if (__any(moved)) {
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+                    lacc[nt] *= alpha[nt];
+#pragma unroll
+                    for (int mt = 0; mt < MT; ++mt) oacc[mt][nt] *= alpha[nt];
+                }
+            }
+            // (the row sum is that of the rounded probabilities)
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int p = 0; p < NP; ++p) lacc[nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pb[nt][p], lacc[nt], 0, 0, 0);
+            // two features of the lane at a time: byte d of its eight value rows
+#pragma unroll
+            for (int d = 0; d < VF / 2; ++d) {
+                unsigned w[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const unsigned x = vb.v[e][d / 4];
+                    const float s = __uint_as_float(vb.s[e >> 2] >> 8 * (e & 3) << 23);
+                    bf16x2 r;
+                    if (d % 4 == 0) r = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x, s, 0);
+                    else if (d % 4 == 1) r = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x, s, 1);
+                    else if (d % 4 == 2) r = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x, s, 2);
+                    else r = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x, s, 3);
+                    w[e] = __builtin_bit_cast(unsigned, r);
+                }
+                u32x4 lo, hi;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    lo[r] = __builtin_amdgcn_perm(w[2 * r + 1], w[2 * r], 0x05040100u);
+                    hi[r] = __builtin_amdgcn_perm(w[2 * r + 1], w[2 * r], 0x07060302u);
+                }
+                const bf16x8 fl = __builtin_bit_cast(bf16x8, lo), fh = __builtin_bit_cast(bf16x8, hi);
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int p = 0; p < NP; ++p) {
+                        oacc[2 * d][nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fl, pb[nt][p], oacc[2 * d][nt], 0, 0, 0);
+                        oacc[2 * d + 1][nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fh, pb[nt][p], oacc[2 * d + 1][nt], 0, 0, 0);
+                    }
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            ldv(vb, i + AHEAD);
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        f4_keys<HD> kb[AHEAD];
+        f4_values<HD> vb[AHEAD];
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j) {
+            __builtin_amdgcn_sched_barrier(0);
+            ldk(kb[j], j);
+            __builtin_amdgcn_sched_barrier(0);
+            ldv(vb[j], j);
+        }
+        int i = 0;
+        for (; i + AHEAD <= n_all; i += AHEAD) {
+#pragma unroll
+            for (int j = 0; j < AHEAD; ++j) block(kb[j], vb[j], i + j);
+        }
+#pragma unroll
+        for (int j = 0; j < AHEAD - 1; ++j)
+            if (i + j < n_all) block(kb[j], vb[j], i + j);
+    }
+
+    // the waves' (maximum, sum, O) joined in two steps, a lane each time with the same lane of another wave;
+    // oacc[u][nt][j]: query row nt*16 + c, feature (4g + j) * VF + u
+    float l_run[NT];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) l_run[nt] = lacc[nt][0];
+#pragma unroll
+    for (int step = F4N_WAVES / 2; step > 0; step >>= 1) {
+        __syncthreads();             // (first: every wave is done with the query rows)
+        if (wave >= step && wave < 2 * step) {
+            unsigned char* to = smem + (wave - step) * SLOT;
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt) *reinterpret_cast<f32x4*>(to + ((nt * MT + mt) * 64 + lane) * 16) = oacc[mt][nt];
+                *reinterpret_cast<float2*>(to + NT * MT * 1024 + (nt * 64 + lane) * 8) = make_float2(m_run[nt], l_run[nt]);
+            }
+        }
+        __syncthreads();
+        if (wave < step) {
+            const unsigned char* from = smem + wave * SLOT;
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                const float2 ml = *reinterpret_cast<const float2*>(from + NT * MT * 1024 + (nt * 64 + lane) * 8);
+                const float M = fmaxf(m_run[nt], ml.x), Ms = M == -INFINITY ? 0.f : M;
+                const float f0 = __builtin_amdgcn_exp2f(m_run[nt] - Ms), f1 = __builtin_amdgcn_exp2f(ml.x - Ms);
+                m_run[nt] = M;
+                l_run[nt] = f0 * l_run[nt] + f1 * ml.y;
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt)
+                    oacc[mt][nt] = f0 * oacc[mt][nt] + f1 * *reinterpret_cast<const f32x4*>(from + ((nt * MT + mt) * 64 + lane) * 16);
+            }
+        }
+    }
+    if (wave) return;
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+        const int n = nt * 16 + c;
+        if (n >= n_rows) continue;
+        const int i = (T.n0 + n) / A.G, h = kvh * A.G + T.n0 + n - i * A.G;
+        const int64_t r = T.row0 + i, row = ((int64_t)K.entry * KVH + kvh) * P.TR + n;
+        const bool whole = K.nsplit == 1;
+        const float inv = l_run[nt] > 0.f ? 1.0f / l_run[nt] : 0.f;           // a row that sees nothing: 0
+        if (g == 0 && !whole) P.pml[row] = make_float2(m_run[nt], l_run[nt]);
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int u = 0; u < VF; u += 4) {
+                const int d = (4 * g + j) * VF + u;
+                const f32x4 o = (f32x4){oacc[u][nt][j], oacc[u + 1][nt][j], oacc[u + 2][nt][j], oacc[u + 3][nt][j]};
+                if (d >= hd) continue;
+                if (whole) pa_store4((T_*)A.out + r * A.out_row + h * A.out_head + d, o * inv);
+                else pa_store4(P.po + row * hd + d, o);
+            }
+    }
+}
+
+// ---- many query rows: the matrix cores and the vector unit are the bound --------------------------------
+// Eight waves have 16 * NT query rows each and walk the tokens together, 64 at a time.  Codes are made
+// bfloat16 once for all of them: every wave takes eight of the next 64 tokens' key and value rows from registers,
+// where their codes have arrived meanwhile, and lays them down in the other half of LDS while the waves
+// multiply out of this one.
+//   keys: 16 tokens x 32 features in fragment order, a lane's 16 bytes are what it multiplies
+//   values: 16 tokens x 32 features as two 16 x 16 squares of 32-byte rows for the transposing LDS read
+// What is dead or behind every window is laid down as zeros, so only the scores have a mask.
+#define F4W_WAVES 8
+template <int HD, int NT, int NP>
+__global__ __launch_bounds__(64 * F4W_WAVES) void k_paged_fp4_wide(cs_fp4_dev F, pa_args A, pa_plan P) {
+    typedef f4_qtype<NP> T_;
+    constexpr int KS = HD / 32, MT = HD / 16;
+    constexpr int WROWS = 16 * NT, TR = F4W_WAVES * WROWS;
+    constexpr int DW = HD / 64;                                 // dwords of codes of a lane's piece of a row
+    constexpr int HALF = 2 * KS * 1024, V_AT = 2 * HALF, STAGE_BYTES = 2 * V_AT;         // keys of a block; of a stage
+    __shared__ __attribute__((aligned(16))) unsigned char stage[2][STAGE_BYTES];
+    const cs_pages_dev& D = F.d;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int c = lane & 15, g = lane >> 4;
+    const int KVH = D.p.n_kv_heads;
+    const unsigned wg = cs_paged_wg();
+    const int kvh = wg % KVH;
+    pa_work K;
+    if (!pa_find(D, A.G, A.window, P, wg / KVH, kvh, K)) return;
+    const pa_tile& T = K.T;
+    const int hd = D.p.head_dim, G = A.G;
+    const int n_rows = min(TR, T.QR - T.n0);
+    const int i_lo = T.n0 / G, i_hi = (T.n0 + n_rows - 1) / G;
+    const int n_lim = min(T.L + i_hi + 1, D.cap);              // tokens that the tile's last row sees
+    const int w_first = A.window ? T.L + i_lo - A.window + 1 : 0;       // tokens before it are seen by no row of the tile
+    const int base = A.window ? max(0, w_first) & ~31 : 0;
+    const int w_begin = (int)min((int64_t)base + (int64_t)K.split * K.chunk, (int64_t)n_lim);
+    const int t_end = K.split == K.nsplit - 1 ? n_lim : (int)min((int64_t)w_begin + K.chunk, (int64_t)n_lim);
+    const int n_stages = (t_end - w_begin + 63) / 64;
+
+    const int n0 = T.n0 + wave * WROWS + c;
+    bf16x8 qreg[NT][KS][NP];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+        const int n = n0 + nt * 16, i = n / G;
+        const T_* qp = (const T_*)A.q + (T.row0 + i) * A.q_row + (kvh * G + n - i * G) * A.q_head + g * 8;
+#pragma unroll
+        for (int s = 0; s < KS; ++s) {
+#pragma unroll
+            for (int p = 0; p < NP; ++p) qreg[nt][s][p] = (bf16x8){0, 0, 0, 0, 0, 0, 0, 0};
+            if (n < T.QR && s * 32 < hd) f4_split(qp + s * 32, qreg[nt][s]);
+        }
+    }
+
+    // a lane's piece of the 64 tokens: features (lane / 8) * HD / 8 .. of token 8 * wave + lane % 8
+    const int tok = 8 * wave + (lane & 7), f0 = (lane >> 3) * (HD / 8);
+    const bool there = f0 < hd;
+    constexpr unsigned NOWHERE = 0x80000000u;
+    const unsigned kts = (unsigned)F.k_token, vts = (unsigned)F.v_token, kgs = (unsigned)F.ks_group, vgs = (unsigned)F.vs_group;
+    const unsigned koff = there ? (tok & 31) * kts + f0 / 2 : NOWHERE, ksoff = there ? f0 / CS_FP4_GROUP * kgs + (tok & 31) : NOWHERE;
+    const unsigned voff = there ? (tok & 31) * vts + f0 / 2 : NOWHERE, vsoff = there ? f0 / CS_FP4_GROUP * vgs + (tok & 31) : NOWHERE;
+    const uint8_t *Kh = F.k + kvh * F.k_head, *Vh = F.v + kvh * F.v_head, *KSh = F.ks + kvh * F.ks_head, *VSh = F.vs + kvh * F.vs_head;
+    const int32_t* tab = D.p.table + T.b * D.p.table_stride;
+
+    // A lane has the page of one of the next 64 blocks of 32 tokens.
+    int page_l = -1;
+    unsigned long long okay = 0, old = 0;                      // blocks that exist, of these and of the 64 before
+    auto pages = [&](int blk0) {
+        const int64_t t = (int64_t)w_begin + 32 * ((int64_t)blk0 + lane);
+        page_l = t < t_end ? tab[t >> D.page_log2] : -1;
+        const bool ok = (unsigned)page_l < (unsigned)D.p.n_pages;
+        old = okay;
+        okay = __ballot(ok);
+        page_l = ok ? page_l : -1;
+    };
+    unsigned kc[DW], vc[DW], ksc, vsc;
+    auto request = [&](int i) {
+        if ((2 * i & 63) == 0) pages(2 * i);
+        const int t0 = w_begin + 64 * i + 32 * (wave >> 2);
+        const int page = __builtin_amdgcn_readlane(page_l, (2 * i + (wave >> 2)) & 63), slot = t0 & (D.p.page_size - 1);
+        const int64_t pg = page >= 0 ? page : 0;
+        const int live = min(32, n_lim - t0);
+        const bool some = page >= 0 && live > 0;
+        const auto rk = cs_rsrc(Kh + pg * F.k_page + (int64_t)slot * kts, some ? (live - 1) * kts + hd / 2 : 0);
+        const auto rv = cs_rsrc(Vh + pg * F.v_page + (int64_t)slot * vts, some ? (live - 1) * vts + hd / 2 : 0);
+        const auto rks = cs_rsrc(KSh + pg * F.ks_page + slot, some ? (hd / CS_FP4_GROUP - 1) * kgs + 32 : 0);
+        const auto rvs = cs_rsrc(VSh + pg * F.vs_page + slot, some ? (hd / CS_FP4_GROUP - 1) * vgs + 32 : 0);
+        const int t = t0 + (tok & 31);
+        const bool mine = t < n_lim && t >= w_first;           // (dead scales may be anything)
+        if constexpr (DW == 1) {
+            kc[0] = __builtin_amdgcn_raw_buffer_load_b32(rk, koff, 0, 0);
+            vc[0] = __builtin_amdgcn_raw_buffer_load_b32(rv, voff, 0, 0);
+        } else if constexpr (DW == 2) {
+            const auto x = __builtin_amdgcn_raw_buffer_load_b64(rk, koff, 0, 0), y = __builtin_amdgcn_raw_buffer_load_b64(rv, voff, 0, 0);
+#pragma unroll
+            for (int d = 0; d < DW; ++d) kc[d] = x[d], vc[d] = y[d];
+        } else {
+            const auto x = __builtin_amdgcn_raw_buffer_load_b128(rk, koff, 0, 0), y = __builtin_amdgcn_raw_buffer_load_b128(rv, voff, 0, 0);
+#pragma unroll
+            for (int d = 0; d < DW; ++d) kc[d] = x[d], vc[d] = y[d];
+        }
+        ksc = __builtin_amdgcn_raw_buffer_load_b8(rks, mine ? ksoff : NOWHERE, 0, 0);
+        vsc = __builtin_amdgcn_raw_buffer_load_b8(rvs, mine ? vsoff : NOWHERE, 0, 0);
+    };
+    // where they go: block (wave / 4), half, token of the half
+    unsigned char* const put = &stage[0][0] + (wave >> 2) * HALF + (wave >> 1 & 1) * KS * 1024;
+    const int row = tok & 15;
+    auto lay_down = [&](int buf) {
+        unsigned char* p = put + buf * STAGE_BYTES;
+#pragma unroll
+        for (int d = 0; d < DW; ++d) {
+            const int f = f0 + 8 * d;
+            *reinterpret_cast<bf16x8*>(p + (f >> 5) * 1024 + (row + 16 * (f >> 3 & 3)) * 16) = cs_fp4_decode(kc[d], ksc << 23);
+            *reinterpret_cast<bf16x8*>(p + V_AT + (f >> 5) * 1024 + (f >> 4 & 1) * 512 + row * 32 + (f >> 3 & 1) * 16) = cs_fp4_decode(vc[d], vsc << 23);
+        }
+    };
+
+    f32x4 oacc[MT][NT], lacc[NT];
+    float m_run[NT], thr[NT];
+    int q_last[NT];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+        const int i = (n0 + nt * 16) / G;
+        q_last[nt] = T.L + i;
+        m_run[nt] = thr[nt] = -INFINITY;
+        lacc[nt] = (f32x4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) oacc[mt][nt] = (f32x4){0.f, 0.f, 0.f, 0.f};
+    }
+    const float scale2 = A.scale2, inv_scale2 = 1.0f / A.scale2;
+    const bf16_t one = (bf16_t)1.0f;
+    const bf16x8 ones = (bf16x8){one, one, one, one, one, one, one, one};
+
+    auto scores = [&](const unsigned char* sp, f32x4 (&sacc)[2][NT]) {
+        __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+        for (int s = 0; s < KS; ++s) {
+            const bf16x8 k0 = *reinterpret_cast<const bf16x8*>(sp + (s * 64 + lane) * 16);
+            const bf16x8 k1 = *reinterpret_cast<const bf16x8*>(sp + ((KS + s) * 64 + lane) * 16);
+            const f32x4 zero4 = (f32x4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int p = 0; p < NP; ++p) {
+                    sacc[0][nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k0, qreg[nt][s][p], s + p == 0 ? zero4 : sacc[0][nt], 0, 0, 0);
+                    sacc[1][nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k1, qreg[nt][s][p], s + p == 0 ? zero4 : sacc[1][nt], 0, 0, 0);
+                }
+        }
+        __builtin_amdgcn_s_setprio(0);
+    };
+    // the running maximum of the tile rows moves (and O is rescaled) only when it is left behind by 2^8
+    auto reference = [&](const f32x4 (&sacc)[2][NT], bool masked) {
+        if (!masked) {
+            bool over = false;
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                const float lm = fmaxf(fmaxf(fmaxf(sacc[0][nt][0], sacc[0][nt][1]), fmaxf(sacc[0][nt][2], sacc[0][nt][3])),
+                                       fmaxf(fmaxf(sacc[1][nt][0], sacc[1][nt][1]), fmaxf(sacc[1][nt][2], sacc[1][nt][3])));
+                over |= !(lm <= thr[nt]);
+            }
+            if (!__any(over)) return;
+        }
+        bool moved = false;
+        float alpha[NT];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            float mx = fmaxf(fmaxf(sacc[0][nt][0], sacc[0][nt][1]), sacc[0][nt][2]);
+            mx = fmaxf(fmaxf(mx, sacc[0][nt][3]), sacc[1][nt][0]);
+            mx = fmaxf(fmaxf(mx, sacc[1][nt][1]), fmaxf(sacc[1][nt][2], sacc[1][nt][3]));
+            mx = fa_row4_max(mx) * scale2;
+            const bool up = mx > m_run[nt] + FA_RESCALE_LOG2;
+            const float m_new = up ? mx : m_run[nt];
+            alpha[nt] = up ? __builtin_amdgcn_exp2f(m_run[nt] - (m_new == -INFINITY ? 0.f : m_new)) : 1.0f;
+            moved |= up;
+            m_run[nt] = m_new;
+            thr[nt] = m_new == -INFINITY ? -INFINITY : (m_new + FA_RESCALE_LOG2) * inv_scale2;
+        }
+        if (__any(moved)) {
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                lacc[nt] *= alpha[nt];
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt) oacc[mt][nt] *= alpha[nt];
+            }
+        }
+    };
+    typedef short s16x4 __attribute__((ext_vector_type(4)));
+    typedef short s16x8 __attribute__((ext_vector_type(8)));
+    auto finish = [&](f32x4 (&sacc)[2][NT], const unsigned char* sp, int t0, bool masked, bool ok) {
+        if (masked) {
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int a = 0; a < 2; ++a)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const int t = t0 + 16 * a + 4 * g + j;
+                        const bool sees = t <= q_last[nt] && (A.window == 0 || t > q_last[nt] - A.window) && t < n_lim && ok;
+                        sacc[a][nt][j] = sees ? sacc[a][nt][j] : -INFINITY;
+                    }
+        }
+        reference(sacc, masked);
+        bf16x8 pb[NT][NP];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            const float m_safe = m_run[nt] == -INFINITY ? 0.f : m_run[nt];
+            float x[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = __builtin_amdgcn_exp2f(fmaf(sacc[e >> 2][nt][e & 3], scale2, -m_safe));
+            f4_split8(x, pb[nt]);
+        }
+        __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
+            s16x4 h[2];
+#pragma unroll
+            for (int a = 0; a < 2; ++a) {
+                const unsigned char* p = sp + V_AT + (a * KS + (mt >> 1)) * 1024 + (mt & 1) * 512 + lane * 8;
+                h[a] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(__attribute__((address_space(3))) unsigned char*)p);
+            }
+            const bf16x8 vf = __builtin_bit_cast(bf16x8, (s16x8){h[0][0], h[0][1], h[0][2], h[0][3], h[1][0], h[1][1], h[1][2], h[1][3]});
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int p = 0; p < NP; ++p) oacc[mt][nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pb[nt][p], oacc[mt][nt], 0, 0, 0);
+        }
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int p = 0; p < NP; ++p) lacc[nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pb[nt][p], lacc[nt], 0, 0, 0);
+        __builtin_amdgcn_s_setprio(0);
+    };
+
+    // positions that this wave's rows have: blocks outside what they see are not computed, blocks inside need no mask
+    const int p_lo = T.L + (T.n0 + wave * WROWS) / G, p_hi = T.L + min(T.rows - 1, (T.n0 + wave * WROWS + WROWS - 1) / G);
+    const int w_lo = A.window ? p_lo - A.window + 1 : 0, w_hi = A.window ? p_hi - A.window + 1 : 0;
+    const int p_end = T.n0 + wave * WROWS < T.QR ? min(p_hi, t_end - 1) : -1;       // a wave without rows multiplies nothing
+    const int p_open = min(p_lo, D.cap - 1);
+    f32x4 sa[2][NT];
+    if (n_stages > 0) {
+        request(0);
+        lay_down(0);
+        request(1);
+    }
+    __syncthreads();
+    for (int i = 0; i < n_stages; ++i) {
+        if (i + 1 < n_stages) lay_down((i + 1) & 1);
+        request(i + 2);
+        const unsigned long long there_are = (i + 2) >> 5 == i >> 5 ? okay : old;
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+            const int t0 = w_begin + 64 * i + 32 * b;
+            if (t0 > p_end || t0 + 31 < w_lo) continue;
+            const unsigned char* sp = stage[i & 1] + b * HALF;
+            const bool ok = there_are >> ((2 * i + b) & 63) & 1;
+            scores(sp, sa);
+            finish(sa, sp, t0, t0 + 31 > p_open || t0 < w_hi || !ok, ok);
+        }
+        __syncthreads();
+    }
+
+    // oacc[mt][nt][j]: query row nt*16 + c, feature mt*16 + 4g + j
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+        const int n = n0 + nt * 16;
+        if (n >= T.QR) continue;
+        const int i = n / G, h = kvh * G + n - i * G;
+        const int64_t r = T.row0 + i, row = ((int64_t)K.entry * KVH + kvh) * P.TR + n - T.n0;
+        const float l = lacc[nt][0], inv = l > 0.f ? 1.0f / l : 0.f;
+        const bool whole = K.nsplit == 1;
+        if (g == 0 && !whole) P.pml[row] = make_float2(m_run[nt], l);
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
+            const int d = mt * 16 + 4 * g;
+            if (d >= hd) continue;
+            if (whole) pa_store4((T_*)A.out + r * A.out_row + h * A.out_head + d, oacc[mt][nt] * inv);
+            else pa_store4(P.po + row * hd + d, oacc[mt][nt]);
+        }
+    }
+}
+
+// ---- entry points --------------------------------------------------------------------------
+static int check_shape(const char* who, const cs_pages_fp4* p, int32_t q_dtype, int32_t n_heads, int32_t R, int32_t max_rows, int64_t max_len) {
+    CS_TRY(cs_fp4_check(who, p));
+    CS_REQUIRE(q_dtype == CS_F32 || q_dtype == CS_BF16, CS_E_ARG, "%s: queries of unknown type %d", who, q_dtype);
+    CS_REQUIRE(n_heads >= 1 && n_heads <= 4096 && n_heads % p->n_kv_heads == 0, CS_E_ARG,
+               "%s: n_heads must be a multiple of n_kv_heads, up to 4096", who);
+    CS_REQUIRE(R >= 0 && R <= 1 << 26, CS_E_ARG, "%s: R out of range", who);
+    CS_REQUIRE((int64_t)R * n_heads <= 1 << 30, CS_E_UNSUPPORTED, "%s: R * n_heads exceeds 2^30", who);
+    CS_REQUIRE(max_rows >= 0 && max_len >= 0, CS_E_ARG, "%s: negative max_rows or max_len", who);
+    return CS_OK;
+}
+
+// How a call is cut: the same for the workspace and the launches.
+struct f4_cut {
+    int hdt;
+    pa_part narrow, wide;
+    int64_t at_w, bytes;                      // where the second launch's partial results start; bytes in all
+};
+#define F4N_MOST 48               // query rows up to which a stream takes the kernel of few rows
+static f4_cut f4_make_cut(const cs_pages_fp4* p, bool f32, int H, bool has_row0, int R, int max_rows, int64_t max_len) {
+    f4_cut c = {};
+    const int KVH = p->n_kv_heads, G = H / KVH, B = p->batch, cap = p->table_pages * p->page_size;
+    const int rows = has_row0 ? (max_rows ? std::min(max_rows, R) : R) : R / B;
+    const int64_t qr = (int64_t)rows * G, all = (int64_t)R * G, len = max_len && max_len < cap ? max_len : cap;
+    c.hdt = p->head_dim <= 64 ? 64 : p->head_dim <= 128 ? 128 : 256;
+    pa_part &N = c.narrow, &W = c.wide;
+    // Streams of up to n_most query rows per KV head go to the kernel of few rows.  Where a batch has
+    // longer ones too, that kernel is made for single tokens: a tile of 48 rows would cost every one of
+    // them three tiles' products.
+    const int n_most = c.hdt == 256 || qr > F4N_MOST ? 16 : F4N_MOST;
+    if (has_row0 || qr <= n_most) {
+        N.nt = (int)std::min<int64_t>(n_most / 16, cs_ceil_div(qr, 16));
+        N.TR = 16 * N.nt;
+        N.qr_hi = qr <= n_most ? 0x7fffffff : n_most;
+        N.tiles = !has_row0 ? B : (int)(qr <= n_most ? all / N.TR + std::min(B, R) : std::min(B, R));
+    }
+    if (qr > n_most) {
+        // Tiles of half the rows where whole ones, cut into ranges of 256 tokens of what a row sees on
+        // average, leave the chip unfilled
+        const bool unfilled = (all / (F4W_WAVES * 32) + 1) * KVH * std::max<int64_t>(1, (len - rows / 2) / 256) < 256;
+        W.nt = c.hdt == 256 || f32 || unfilled ? 1 : 2;
+        W.TR = F4W_WAVES * 16 * W.nt;
+        W.qr_lo = has_row0 ? n_most : 0;
+        W.qr_hi = 0x7fffffff;
+        W.tiles = (int)(has_row0 ? all / W.TR + std::min<int64_t>(B, all / (n_most + 1)) : B * cs_ceil_div(qr, W.TR));
+    }
+    c.at_w = pa_ranges(N, len, B, KVH, p->head_dim, 512, 256, 512);
+    c.bytes = c.at_w + pa_ranges(W, len, B, KVH, p->head_dim, 256, 128, 192);
+    return c;
+}
+
+extern "C" int64_t cs_paged_fp4_attention_workspace(const cs_pages_fp4* p, int32_t q_dtype, int32_t n_heads, int32_t has_row0, int32_t R,
+                                                    int32_t max_rows, int64_t max_len) {
+    const char* who = "cs_paged_fp4_attention_workspace";
+    CS_TRY(check_shape(who, p, q_dtype, n_heads, R, max_rows, max_len));
+    CS_REQUIRE(has_row0 || p->batch == 0 || R % p->batch == 0, CS_E_ARG, "%s: R rows cannot be shared out among %d streams without d_row0",
+               who, p->batch);
+    if (R == 0 || p->batch == 0) return 0;
+    return f4_make_cut(p, q_dtype == CS_F32, n_heads, has_row0 != 0, R, max_rows, max_len).bytes;
+}
+
+template <int HD, int NT, int NP>
+static int f4n_launch(const cs_fp4_dev& F, const pa_args& A, const pa_plan& P, dim3 grid, hipStream_t s) {
+    k_paged_fp4_narrow<HD, NT, NP><<<grid, 64 * F4N_WAVES, 0, s>>>(F, A, P);
+    return cs_launch_ok("k_paged_fp4_narrow");
+}
+template <int HD, int NT, int NP>
+static int f4w_launch(const cs_fp4_dev& F, const pa_args& A, const pa_plan& P, dim3 grid, hipStream_t s) {
+    k_paged_fp4_wide<HD, NT, NP><<<grid, 64 * F4W_WAVES, 0, s>>>(F, A, P);
+    return cs_launch_ok("k_paged_fp4_wide");
+}
+
+extern "C" int cs_paged_fp4_attention(const cs_pages_fp4* p, int32_t q_dtype, const void* q, int64_t q_row, int64_t q_head, int32_t n_heads,
+                                      const int32_t* d_row0, int32_t R, float scale, int32_t window, int32_t max_rows, int64_t max_len,
+                                      void* out, int64_t out_row, int64_t out_head, void* workspace, int64_t workspace_bytes, void* stream) {
+    const char* who = "cs_paged_fp4_attention";
+    CS_TRY(check_shape(who, p, q_dtype, n_heads, R, max_rows, max_len));
+    CS_REQUIRE(scale > 0.f && std::isfinite(scale), CS_E_ARG, "%s: scale must be positive and finite", who);
+    CS_REQUIRE(window >= 0, CS_E_ARG, "%s: negative window", who);
+    cs_fp4_dev F;
+    CS_TRY(cs_fp4_view(who, p, d_row0, R, &F));
+    if (R == 0 || p->batch == 0) return CS_OK;
+    const bool f32 = q_dtype == CS_F32;
+    const size_t esz = f32 ? 4 : 2;
+    CS_TRY(cs_check_rows(who, "q", q, q_row, q_head, esz));
+    CS_TRY(cs_check_rows(who, "out", out, out_row, out_head, esz));
+    CS_TRY(cs_check_apart(who, "out", out_row, R, out_head, n_heads, p->head_dim));
+    F.d.p.dtype = q_dtype;                                      // (the merge's outputs)
+    const pa_args A = {q, q_row, q_head, out, out_row, out_head, n_heads, n_heads / p->n_kv_heads, window, scale * 1.4426950408889634f};
+    hipStream_t s = (hipStream_t)stream;
+    const f4_cut c = f4_make_cut(p, f32, n_heads, d_row0 != nullptr, R, max_rows, max_len);
+    CS_REQUIRE(c.bytes <= 0 || (workspace && workspace_bytes >= c.bytes), CS_E_CAPACITY, "%s: the workspace has %lld bytes, %lld are needed",
+               who, (long long)(workspace ? workspace_bytes : 0), (long long)c.bytes);
+    CS_REQUIRE(((uintptr_t)workspace & 15) == 0, CS_E_ARG, "%s: the workspace is not aligned to 16 bytes", who);
+    const int64_t grid_n = (int64_t)c.narrow.entries * p->n_kv_heads, grid_w = (int64_t)c.wide.entries * p->n_kv_heads;
+    CS_REQUIRE(grid_n <= 0x7fffffff && grid_w <= 0x7fffffff, CS_E_UNSUPPORTED, "%s: too many tiles", who);
+    int rc = CS_E_UNSUPPORTED;
+    if (grid_w) {
+        const pa_plan P = pa_plan_of(c.wide, (char*)workspace + c.at_w, p->n_kv_heads, p->head_dim);
+        const dim3 n = cs_paged_grid(grid_w);
+#define FW(HD_, NT_) if (c.hdt == HD_ && c.wide.nt == NT_) rc = NT_ == 1 && f32 ? f4w_launch<HD_, 1, 3>(F, A, P, n, s) : f4w_launch<HD_, NT_, 1>(F, A, P, n, s)
+        FW(64, 1); FW(64, 2); FW(128, 1); FW(128, 2); FW(256, 1);
+#undef FW
+        CS_TRY(rc);
+        CS_TRY(pm_launch(F.d, A, P, n, s));
+    }
+    if (grid_n) {
+        const pa_plan P = pa_plan_of(c.narrow, (char*)workspace, p->n_kv_heads, p->head_dim);
+        const dim3 n = cs_paged_grid(grid_n);
+#define FN(HD_, NT_) if (c.hdt == HD_ && c.narrow.nt == NT_) rc = f32 ? f4n_launch<HD_, NT_, 3>(F, A, P, n, s) : f4n_launch<HD_, NT_, 1>(F, A, P, n, s)
+        FN(64, 1); FN(64, 2); FN(64, 3); FN(128, 1); FN(128, 2); FN(128, 3); FN(256, 1);
+#undef FN
+        CS_TRY(rc);
+        CS_TRY(pm_launch(F.d, A, P, n, s));
+    }
+    return CS_OK;
+}

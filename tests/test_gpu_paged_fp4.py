@@ -1,0 +1,840 @@
+"""The operators of a paged cache held in 4 bits against their definitions: quantising append, read, attention.
+
+Quantising and reading are exact: every code and scale is compared as it is.  Attention is compared with float64 over the values
+that codes and scales stand for.  u = 2^-24 is half a step of float32; a value rounded to bfloat16 is off by at most 2^-8 of
+itself; sums of n products in float32 are off by at most n * u of the sum of their magnitudes, whatever their order."""
+import math
+
+import pytest
+import torch
+
+from paper_2502_08923_amd import binding as cs
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+U = 2.0 ** -24
+BF, F32 = torch.bfloat16, torch.float32
+HALF = {BF: 2.0 ** -8, F32: 2.0 ** -24}
+E2M1 = [0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0]
+
+
+def gen(seed):
+    g = torch.Generator(device=DEV)
+    g.manual_seed(seed)
+    return g
+
+
+def randn(shape, g, dtype, spread=1.0):
+    return (torch.randn(shape, generator=g, device=DEV) * spread).to(dtype)
+
+
+def power(n):
+    """2^n in float64, exactly"""
+    return ((n.long() + 1023) << 52).view(torch.float64)
+
+
+def decode(codes, scales):
+    """Codes uint8 [..., hd/2] and scales uint8 [..., hd/32] -> float64 [..., hd]"""
+    table = torch.tensor(E2M1 + [-x for x in E2M1], dtype=torch.float64, device=codes.device)
+    each = torch.stack([codes & 15, codes >> 4], dim=-1).flatten(-2)
+    s = torch.where(scales == 255, torch.full(scales.shape, math.nan, dtype=torch.float64, device=scales.device), power(scales.long() - 127))
+    return table[each.long()] * s.repeat_interleave(32, dim=-1)
+
+
+def quantise(x):
+    """[..., hd] -> codes uint8 [..., hd/2], scales uint8 [..., hd/32], by distance to every value"""
+    y = x.double().unflatten(-1, (-1, 32))
+    top = y.abs().amax(-1)
+    bad = ~torch.isfinite(y).all(-1)
+    e = torch.full(top.shape, 2, dtype=torch.long, device=x.device)                      # the smallest with top <= 7 * 2^(e - 127)
+    for n in range(2, 252):
+        e += top > 7 * 2.0 ** (n - 127)
+    a = torch.nan_to_num(y.abs() / power(e - 127).unsqueeze(-1), nan=0.0, posinf=0.0).clamp(max=7)
+    far = (a.unsqueeze(-1) - torch.tensor(E2M1, dtype=torch.float64, device=x.device)).abs()
+    least = far.amin(-1, keepdim=True)
+    near = far == least
+    low = near.int().argmax(-1)                                                          # of two equally near the even one
+    code = torch.where((near.sum(-1) > 1) & (low % 2 == 1), low + 1, low) + 8 * torch.signbit(x.float()).unflatten(-1, (-1, 32)).long()
+    code = torch.where(bad.unsqueeze(-1), torch.zeros_like(code), code).flatten(-2)
+    return (code[..., 0::2] + 16 * code[..., 1::2]).to(torch.uint8), torch.where(bad, torch.full_like(e, 255), e).to(torch.uint8)
+
+
+class Cache:
+    """Pools, table and lengths of ragged streams.  What no live token owns has scale byte 255 and random codes, and table entries
+    behind a stream's last page are out of range."""
+
+    def __init__(self, lens, rows, KVH, hd, P, dtype=BF, seed=1, order="head", pad=0, holes=(), spare=2, shared=0, grown=None):
+        g = gen(seed)
+        B = len(lens)
+        self.lens, self.rows, self.P, self.pad, self.dtype, self.KVH, self.hd = list(lens), list(rows), P, pad, dtype, KVH, hd
+        need = [-(-(n + (grown or rows)[b]) // P) for b, n in enumerate(lens)]
+        total = sum(need) + spare
+        if order == "both":                              # codes of a token's key and value side by side, wider strides everywhere
+            pool = torch.randint(0, 256, (total, KVH, P, 2, 16 * (-(-hd // 32) + 1)), generator=g, dtype=torch.uint8, device=DEV)
+            self.k, self.v = pool[..., 0, :hd // 2], pool[..., 1, :hd // 2]
+            f = torch.full((total, KVH, 2, hd // 32 + 1, P + 16), 255, dtype=torch.uint8, device=DEV)
+            self.ks, self.vs = f[:, :, 0, :hd // 32, :P], f[:, :, 1, :hd // 32, :P]
+        else:
+            shape = (total, KVH, P, hd // 2) if order == "head" else (total, P, KVH, hd // 2)
+            self.k, self.v = (torch.randint(0, 256, shape, generator=g, dtype=torch.uint8, device=DEV) for _ in range(2))
+            if order == "token":
+                self.k, self.v = self.k.transpose(1, 2), self.v.transpose(1, 2)
+            self.ks, self.vs = (torch.full((total, KVH, hd // 32, P), 255, dtype=torch.uint8, device=DEV) for _ in range(2))
+        names = torch.randperm(total, generator=g, device=DEV).tolist()
+        width = max(need + [1]) + 1
+        table = [[(-1, 1 << 30, -2 ** 31)[j % 3] for j in range(width)] for _ in range(B)]
+        for b in range(B):
+            for j in range(need[b]):
+                table[b][j] = table[0][j] if b and j < shared else names.pop()
+        self.k_tok, self.v_tok = [], []                  # [KVH][n][hd] of every stream, float64
+        for b in range(B):
+            n = lens[b] + rows[b]
+            both = []
+            for i, (codes, scales) in enumerate(((self.k, self.ks), (self.v, self.vs))):
+                c = torch.randint(0, 256, (KVH, n, hd // 2), generator=g, dtype=torch.uint8, device=DEV)
+                s = torch.randint(123, 128, (KVH, hd // 32, n), generator=g, dtype=torch.uint8, device=DEV)
+                if b and shared:
+                    m = min(n, shared * P)
+                    c[:, :m], s[:, :, :m] = first[i][0][:, :m], first[i][1][:, :, :m]
+                both.append((c, s))
+                for j in range(-(-n // P)):
+                    a, e = j * P, min(n, (j + 1) * P)
+                    codes[table[b][j], :, :e - a] = c[:, a:e]
+                    scales[table[b][j], :, :, :e - a] = s[:, :, a:e]
+            if b == 0:
+                first = both
+            self.k_tok.append(decode(both[0][0], both[0][1].transpose(1, 2)))
+            self.v_tok.append(decode(both[1][0], both[1][1].transpose(1, 2)))
+        self.gone = [set() for _ in range(B)]
+        for b, j in holes:                               # evicted pages: poisoned, the table names nothing
+            self.ks[table[b][j]] = 255
+            self.vs[table[b][j]] = 255
+            table[b][j] = (-1, total, 2 ** 31 - 1)[j % 3]
+            self.gone[b].add(j)
+        self.table = torch.tensor(table, dtype=torch.int32, device=DEV).view(B, width)
+        self.length = torch.tensor(lens, dtype=torch.int32, device=DEV)
+        self.ends = [0]
+        for r in rows:
+            self.ends.append(self.ends[-1] + r)
+        self.R = self.ends[-1] + pad
+        self.row0 = torch.tensor(self.ends, dtype=torch.int32, device=DEV)
+        self.pages = self.handle()
+
+    def handle(self, **kw):
+        d = dict(k=self.k, v=self.v, k_scale=self.ks, v_scale=self.vs, table=self.table, length=self.length)
+        d.update(kw)
+        return cs.PagesFP4(**d)
+
+    def state(self):
+        return [t.clone() for t in (self.k, self.v, self.ks, self.vs)]
+
+    def queries(self, H, seed=3, spread=2.0, R=None):
+        return randn((self.R if R is None else R, H, self.hd), gen(seed), self.dtype, spread)
+
+    def reference(self, q, scale, window=0):
+        """(out, sum of p|v|, bound on the size of a score's terms) in float64, rows behind the last stream 0"""
+        KVH, hd = self.KVH, self.hd
+        H = q.shape[1]
+        G = H // KVH
+        out = torch.zeros(q.shape, dtype=torch.float64, device=DEV)
+        mag, delta = torch.zeros_like(out), torch.zeros(q.shape[:2] + (1,), dtype=torch.float64, device=DEV)
+        for b, (L, r) in enumerate(zip(self.lens, self.rows)):
+            if r == 0:
+                continue
+            k, v = self.k_tok[b], self.v_tok[b]
+            t = torch.arange(L + r, device=DEV)
+            at = L + torch.arange(r, device=DEV)
+            sees = t[None] <= at[:, None]
+            if window:
+                sees &= t[None] > at[:, None] - window
+            for j in self.gone[b]:
+                sees[:, j * self.P:(j + 1) * self.P] = False
+            for g in range(KVH):
+                for u in range(G):
+                    x = q[self.ends[b]:self.ends[b] + r, g * G + u].double()
+                    s = (x @ k[g].T.contiguous()) * scale
+                    d = (x.abs() @ k[g].abs().T.contiguous()) * scale
+                    d = torch.where(sees, d, torch.zeros_like(d)).amax(1)
+                    s = s.masked_fill(~sees, -math.inf)
+                    m = s.amax(1, keepdim=True)
+                    p = torch.where(sees, torch.exp(s - torch.where(m.isinf(), torch.zeros_like(m), m)), torch.zeros_like(s))
+                    l = p.sum(1, keepdim=True)
+                    p = torch.where(l > 0, p / l, p)
+                    rows = slice(self.ends[b], self.ends[b] + r)
+                    out[rows, g * G + u] = p @ v[g]
+                    mag[rows, g * G + u] = p @ v[g].abs()
+                    delta[rows, g * G + u, 0] = d
+        return out, mag, delta
+
+    def check(self, H, window=0, scale=None, seed=3, spread=2.0, **call):
+        q = self.queries(H, seed, spread)
+        want, mag, delta = self.reference(q, 1 / math.sqrt(self.hd) if scale is None else scale, window)
+        if self.pad:
+            q[self.ends[-1]:] = math.nan
+        out = torch.full_like(q, 123.0)
+        got = cs.cs_paged_fp4_attention(self.pages, q, row0=self.row0, window=window, scale=scale, out=out, **call)
+        assert got is out
+        live = self.ends[-1]
+        assert bool((got[live:] == 123.0).all()), "rows behind the last stream were written"
+        self.close(got[:live], want[:live], mag[:live], delta[:live])
+        return q, got
+
+    def close(self, got, want, mag, delta):
+        """Keys and values are exact.  A score is off by (N hd + 4) * u of sum |q_d k_d| * scale (products and sums, the scale and
+        the exponent's subtraction; N = 3 parts of a float32 query, else 1) and exp2 by 2 u more; a probability by as much, relatively,
+        and the result by twice that of sum p|v| (numerator and denominator).  Sums over N n tokens and the joins: (N n + 16) u.
+        bfloat16: the probabilities are rounded, numerator and denominator alike, 2 * 2^-8 together, and the result once."""
+        n, parts = max(a + b for a, b in zip(self.lens, self.rows)), 1 if got.dtype == BF else 3
+        rel = 2 * ((parts * self.hd + 4) * delta + 2) * U + 2 * (parts * n + 16) * U
+        if got.dtype == BF:
+            rel = rel + 2 * HALF[BF]
+        tol = mag * rel + want.abs() * HALF[got.dtype] + 1e-30
+        err = (got.double() - want).abs()
+        assert bool((err <= tol).all()), (float((err - tol).max()), int((~(err <= tol)).sum()), err.shape)
+
+
+class Guarded:
+    """Tensors inside larger ones that hold a pattern; the surroundings must keep it."""
+
+    def __init__(self):
+        self.all = []
+
+    def like(self, shape, dtype, fill=None):
+        n = math.prod(shape) * torch.tensor([], dtype=dtype).element_size()
+        raw = torch.full((n + 8192,), 0xA5, dtype=torch.uint8, device=DEV)
+        self.all.append((raw, n))
+        t = raw[4096:4096 + n].view(dtype).view(shape)
+        if fill is not None:
+            t.fill_(fill)
+        return t
+
+    def check(self):
+        for raw, n in self.all:
+            assert bool((raw[:4096] == 0xA5).all()) and bool((raw[4096 + n:] == 0xA5).all()), "written outside the tensor"
+
+
+def same(a, b):
+    """Equal, NaN where NaN"""
+    return torch.equal(torch.nan_to_num(a.double(), nan=1e300), torch.nan_to_num(b.double(), nan=1e300))
+
+
+# ------------------------------------------------------------------------------------------------------
+# append and read
+# ------------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_read_gives_every_code_under_every_scale(dtype):
+    """Scales 0 .. 252 and 255; above 252 the largest codes are past the largest bfloat16."""
+    P, hd = 256, 512 // 2
+    codes = torch.arange(256, device=DEV, dtype=torch.uint8).view(1, 1, 1, 256)[..., :128].expand(1, 1, P, 128).contiguous()
+    codes[0, 0, 1::2] += 128
+    scales = torch.arange(256, device=DEV, dtype=torch.uint8).view(1, 1, 1, P).expand(1, 1, 8, P).clone()
+    scales[scales == 253], scales[scales == 254] = 127, 255
+    for shift in (0, 1):                                   # every half of the codes under every scale
+        codes = codes.roll(shift, 2)
+        pages = cs.PagesFP4(codes, codes.flip(3).contiguous(), scales, scales, torch.zeros((1, 1), dtype=torch.int32, device=DEV),
+                            torch.zeros(1, dtype=torch.int32, device=DEV))
+        k, v = cs.cs_paged_fp4_read(pages, R=P, dtype=dtype)
+        assert k.shape == (P, 1, hd) and k.dtype == dtype
+        f = scales[0, 0].T.contiguous()
+        assert same(k[:, 0], decode(codes[0, 0], f)) and same(v[:, 0], decode(codes.flip(3)[0, 0], f))
+
+
+def test_append_of_every_bfloat16():
+    """All 65536 patterns, beside smaller ones and beside the largest: scales and codes bit for bit, NaN and infinities included."""
+    bits = torch.arange(65536, device=DEV, dtype=torch.int32).to(torch.int16).view(BF)
+    g = gen(5)
+    near = bits.view(-1, 32)                                                # 32 patterns of one exponent and sign
+    mixed = bits[torch.randperm(65536, generator=g, device=DEV)].view(-1, 32)
+    own = torch.zeros((65536, 32), dtype=BF, device=DEV)                    # each alone decides on its scale
+    own[:, 7] = bits
+    own[:, 8] = -0.24 * torch.nan_to_num(bits, nan=0.0, posinf=0.0, neginf=0.0)
+    rows = torch.cat([near, mixed, own]).view(-1, 1, 32)
+    # the same with magnitudes around each border of the codes
+    t = torch.cat([near.float(), own[:4096].float()])
+    t = torch.cat([t, torch.nextafter(t, torch.full_like(t, math.inf)), torch.nextafter(t, torch.zeros_like(t))]).view(-1, 1, 32)
+    for x in (rows, t):
+        R = x.shape[0]
+        P = 1024
+        c = Cache([0], [R], 1, 32, P)
+        cs.cs_paged_fp4_append(c.pages, x, -x)
+        for y, codes, scales in ((x, c.k, c.ks), (-x, c.v, c.vs)):
+            want_c, want_s = quantise(y[:, 0])
+            order = c.table[0, :-1].long()
+            got_c = codes[order, 0].reshape(-1, 16)[:R]
+            got_s = scales[order, 0, 0].reshape(-1, 1)[:R]
+            assert torch.equal(got_s, want_s)
+            fine = want_s[:, 0] != 255
+            assert torch.equal(got_c[fine], want_c[fine])
+            assert int((~fine).sum()) >= 8 and int(fine.sum()) > 1000            # (the eight groups of exponent 255 among them)
+
+
+SIZES = [(8, 128, 64, "head"), (1, 32, 32, "token"), (3, 96, 32, "both"), (4, 64, 256, "token"), (2, 256, 32, "head"), (5, 160, 64, "both"), (1, 224, 128, "head")]
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("KVH,hd,P,order", SIZES)
+def test_append_and_read_of_ragged_rows(KVH, hd, P, order, dtype):
+    """Every byte of the pools: the rows' own are theirs, all others are as before.  Then the rows are read back."""
+    lens, rows = [0, 1, P - 1, P, 2 * P + 5, 70, 3], [1, P + 3, 2, 0, 17, 2 * P, 11]
+    c = Cache(lens, rows, KVH, hd, P, order=order, pad=3, seed=hd, holes=[(4, 2), (5, 70 // P + 1)])
+    before = c.state()
+    k, v = randn((c.R, KVH, hd), gen(1), dtype), randn((c.R, KVH, hd), gen(2), dtype, 30.0)
+    k[c.ends[-1]:], v[c.ends[-1]:] = math.nan, math.nan
+    cs.cs_paged_fp4_append(c.pages, k, v, row0=c.row0)
+    table, n_pages = c.table.tolist(), c.k.shape[0]
+    want_k, want_v = (torch.zeros((c.R, KVH, hd), dtype=torch.float64, device=DEV) for _ in range(2))
+    for x, want, codes, scales in ((k, want_k, before[0], before[2]), (v, want_v, before[1], before[3])):
+        qc, qs = quantise(x)
+        for b, (n, r) in enumerate(zip(lens, rows)):
+            for i in range(r):
+                page, slot, at = table[b][(n + i) // P], (n + i) % P, c.ends[b] + i
+                if 0 <= page < n_pages:
+                    codes[page, :, slot], scales[page, :, :, slot] = qc[at], qs[at]
+                    want[at] = decode(qc[at], qs[at])
+    for got, want in zip((c.k, c.v, c.ks, c.vs), before):
+        assert torch.equal(got, want)
+    for out_type in (BF, F32):
+        out = torch.full((2, c.R, KVH, hd), 9.0, dtype=out_type, device=DEV)
+        cs.cs_paged_fp4_read(c.pages, row0=c.row0, out=(out[0], out[1]))
+        for got, want in zip(out, (want_k, want_v)):
+            assert torch.equal(got[:c.ends[-1]].double(), want[:c.ends[-1]])           # (rows of evicted pages: zeros)
+            assert bool((got[c.ends[-1]:] == 9.0).all())
+    # what is written differs from the rows by at most half a step of the largest code, 1 of 7
+    amax = k[:c.ends[0] + 1].double().unflatten(-1, (-1, 32)).abs().amax(-1, keepdim=True)
+    err = (want_k[:1] - k[:1].double()).unflatten(-1, (-1, 32)).abs()
+    assert bool((err <= amax / 3.5).all())
+
+
+@pytest.mark.parametrize("B", [63, 64, 65, 200])
+def test_append_and_read_of_many_streams(B):
+    """On either side of as many streams as a wave has lanes, some without rows; equal shares; a row each."""
+    lens, rows = [(7 * b) % 40 for b in range(B)], [(b * 5) % 4 for b in range(B)]
+    c = Cache(lens, rows, 1, 64, 32, pad=2, seed=B)
+    k = randn((c.R, 1, 64), gen(2), BF)
+    cs.cs_paged_fp4_append(c.pages, k, -k, row0=c.row0)
+    got_k, got_v = cs.cs_paged_fp4_read(c.pages, R=c.R, row0=c.row0)
+    want = decode(*quantise(k))
+    live = c.ends[-1]
+    assert torch.equal(got_k[:live].double(), want[:live]) and torch.equal(got_v[:live].double(), -want[:live])
+    assert bool((got_k[live:] == 0).all())
+    for each in (1, 3):
+        c = Cache(lens, [each] * B, 1, 64, 32, seed=B)
+        k = randn((c.R, 1, 64), gen(each), BF)
+        cs.cs_paged_fp4_append(c.pages, k, -k)
+        for row0 in (None, c.row0):
+            got_k, got_v = cs.cs_paged_fp4_read(c.pages, R=c.R, row0=row0)
+            assert torch.equal(got_k.double(), decode(*quantise(k))) and torch.equal(got_v, -got_k)
+
+
+def test_append_and_read_of_many_rows():
+    """Enough rows that a workgroup has several, of one small head and of many; offsets at every place in a workgroup's rows."""
+    for KVH, hd, rows in ((1, 32, [5000, 1, 3000, 0, 77]), (8, 128, [2047, 1500, 1, 511]), (40, 64, [1100, 0, 1001])):
+        c = Cache([3] * len(rows), rows, KVH, hd, 64, pad=5, seed=hd)
+        k, v = randn((c.R, KVH, hd), gen(1), F32), randn((c.R, KVH, hd), gen(2), F32)
+        cs.cs_paged_fp4_append(c.pages, k, v, row0=c.row0)
+        got_k, got_v = cs.cs_paged_fp4_read(c.pages, R=c.R, row0=c.row0, dtype=F32)
+        live = c.ends[-1]
+        assert torch.equal(got_k[:live].double(), decode(*quantise(k[:live]))) and torch.equal(got_v[:live].double(), decode(*quantise(v[:live])))
+
+
+def test_read_of_whole_streams_and_of_places_that_do_not_exist():
+    lens = [100, 0, 33, 64]
+    c = Cache(lens, [0] * 4, 2, 64, 32, holes=[(0, 1)], seed=3)
+    row0 = torch.tensor([0, 100, 100, 133, 197], dtype=torch.int32, device=DEV)
+    k, v = cs.cs_paged_fp4_read(c.pages, torch.zeros(4, dtype=torch.int32, device=DEV), R=200, row0=row0, dtype=F32)
+    want_k = torch.cat([t.transpose(0, 1) for t in c.k_tok])
+    want_v = torch.cat([t.transpose(0, 1) for t in c.v_tok])
+    want_k[32:64], want_v[32:64] = 0, 0
+    assert torch.equal(k[:197].double(), want_k) and torch.equal(v[:197].double(), want_v) and bool((k[197:] == 0).all())
+    # before the first token, across it, behind the table, behind 2^31
+    first = torch.tensor([-7, -2 ** 31, 2 ** 31 - 3, 62], dtype=torch.int32, device=DEV)
+    k, _ = cs.cs_paged_fp4_read(c.pages, first, R=40, dtype=F32)
+    assert bool((k[:7] == 0).all()) and torch.equal(k[7:10].double(), c.k_tok[0][:, :3].transpose(0, 1))
+    assert bool((k[10:30] == 0).all()) and torch.equal(k[30:32].double(), c.k_tok[3][:, 62:64].transpose(0, 1)) and bool((k[32:] == 0).all())
+
+
+def test_append_past_the_table_and_at_negative_lengths():
+    """A negative length is 0; positions that the table has no column for are not written."""
+    c = Cache([5, 60, 0], [4, 4, 4], 1, 64, 32, seed=2)
+    short = c.handle(table=c.table[:, :2].contiguous())
+    c.length.copy_(torch.tensor([-9, 62, 2 ** 31 - 2]))
+    before = c.state()
+    k = randn((12, 1, 64), gen(1), BF)
+    cs.cs_paged_fp4_append(short, k, k)
+    qc, qs = quantise(k)
+    table = c.table.tolist()
+    for r, (b, at) in {0: (0, 0), 1: (0, 1), 2: (0, 2), 3: (0, 3), 4: (1, 62), 5: (1, 63)}.items():
+        page, slot = table[b][at // 32], at % 32
+        for j in (0, 1):
+            before[j][page, :, slot], before[2 + j][page, :, :, slot] = qc[r], qs[r]
+    for got, want in zip((c.k, c.v, c.ks, c.vs), before):
+        assert torch.equal(got, want)
+    got, _ = cs.cs_paged_fp4_read(short, R=12)
+    assert torch.equal(got[:6].double(), decode(qc[:6], qs[:6])) and bool((got[6:] == 0).all())
+
+
+# ------------------------------------------------------------------------------------------------------
+# attention
+# ------------------------------------------------------------------------------------------------------
+
+SHAPES = [(4, 4, 64), (8, 2, 128), (7, 1, 128), (3, 3, 32), (6, 2, 96), (16, 1, 256), (5, 5, 160), (4, 1, 192), (12, 4, 224)]
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("H,KVH,hd", SHAPES)
+@pytest.mark.parametrize("P", [32, 64])
+def test_attention_shapes(H, KVH, hd, P, dtype):
+    lens, rows = [0, 1, 15, 31, 32, 33, 200, 129], [1, 1, 3, 1, 0, 2, 11, 5]
+    Cache(lens, rows, KVH, hd, P, dtype, seed=hd, order="token" if P == 32 else "head", pad=3).check(H)
+    lens, rows = [0, 100, 31, 257], [150, 70, 1, 33]
+    Cache(lens, rows, KVH, hd, P, dtype, seed=hd, order="both", pad=3).check(H)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("P", [32, 128, 1024])
+@pytest.mark.parametrize("rows", [1, 4, 11, 12, 13, 33, 70, 150, 300])
+def test_attention_equal_rows(rows, P, dtype):
+    """With offsets and without, with right hints, none and too small ones, into guarded outputs with guarded workspaces."""
+    c = Cache([0, 31, 257, 1100], [rows] * 4, 2, 128, P, dtype, seed=rows)
+    c.check(8)
+    q = c.queries(8)
+    want = c.reference(q, 1 / math.sqrt(128))
+    guard = Guarded()
+    for call in (dict(max_rows=rows, max_len=1100 + rows), {}, dict(max_rows=1, max_len=16)):
+        need = cs.cs_paged_fp4_attention_workspace(c.pages, 8, 4 * rows, dtype=dtype, **call)
+        ws, out = guard.like((need,), torch.uint8) if need else None, guard.like(q.shape, dtype, 7.0)
+        c.close(cs.cs_paged_fp4_attention(c.pages, q, out=out, workspace=ws, **call), *want)
+    guard.check()
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("window", [1, 2, 16, 33, 100, 5000])
+@pytest.mark.parametrize("rows", [1, 9, 130])
+def test_attention_window(rows, window, dtype):
+    """What has left the window of a stream's first new row is poisoned."""
+    for hd, P, KVH, H in ((64, 32, 2, 4), (128, 64, 1, 3), (256, 32, 1, 2)):
+        c = Cache([0, 40, 700, 1500], [rows, rows, 0, rows], KVH, hd, P, dtype, seed=window)
+        table = c.table.cpu()
+        for b, n in enumerate(c.lens):
+            for j in range(max(0, n - window + 1)):
+                c.ks[int(table[b][j // P]), :, :, j % P] = 255
+                c.vs[int(table[b][j // P]), :, :, j % P] = 255
+        c.check(H, window=window)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("rows", [1, 6, 100])
+@pytest.mark.parametrize("P", [32, 64])
+def test_attention_evicted_pages(P, rows, dtype):
+    """Pages that the table no longer names are not attended to, whatever lies in them; a row that sees nothing else is 0."""
+    lens = [3 * P, 10 * P + 5, P - 1]
+    holes = [(0, 0), (0, 2), (1, 1), (1, 5), (1, 6), (1, 7)]
+    Cache(lens, [rows] * 3, 2, 64, P, dtype, seed=P, holes=holes).check(4)
+    Cache(lens, [rows] * 3, 1, 128, P, dtype, seed=P, holes=holes).check(4)
+    if rows == 1:
+        c = Cache([P - 1, 2 * P], [1, 1], 2, 64, P, dtype, seed=P, holes=[(0, 0)])
+        _, got = c.check(4)
+        assert bool((got[0] == 0).all())
+        c = Cache([4 * P - 1], [1], 2, 64, P, dtype, seed=P, holes=[(0, 3)])
+        _, got = c.check(4, window=P // 2)
+        assert bool((got[0] == 0).all())
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_attention_shared_prefix(dtype):
+    Cache([150, 200, 133], [4, 1, 40], 2, 64, 32, dtype, order="both", shared=4).check(8)
+    Cache([150, 200, 133], [4, 1, 2], 2, 128, 32, dtype, shared=4).check(2)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_attention_mixed_batch(dtype):
+    """A prompt block next to single tokens, streams without rows at both ends, hints that are right, absent and wrong."""
+    lens, rows = [5, 900, 0, 3000, 64, 700, 0], [0, 1, 513, 1, 1, 2, 0]
+    c = Cache(lens, rows, 2, 128, 32, dtype, pad=5, seed=9)
+    for hints in ({}, dict(max_rows=513, max_len=3001), dict(max_rows=1, max_len=16), dict(max_rows=4096, max_len=100000)):
+        c.check(8, **hints)
+
+
+@pytest.mark.parametrize("dtype,rows,lens", [(BF, 1, [30000, 77]), (BF, 11, [9000, 20011]), (BF, 40, [12345]), (F32, 1, [20000]),
+                                             (F32, 7, [6000, 100]), (BF, 513, [4000]), (BF, 1025, [0])])
+def test_attention_long_contexts(dtype, rows, lens):
+    c = Cache(lens, [rows] * len(lens), 2, 128, 64, dtype, seed=rows)
+    c.check(8)
+    c.check(8, max_rows=rows, max_len=max(lens) + rows)
+
+
+@pytest.mark.parametrize("hd,H,KVH", [(128, 8, 2), (64, 4, 4), (256, 4, 2), (96, 6, 1)])
+@pytest.mark.parametrize("lens,rows", [([0], [985]), ([0, 300], [130, 700]), ([2000, 0, 70], [200, 49, 1]), ([8000], [90])])
+def test_attention_prompt_blocks(lens, rows, hd, H, KVH):
+    """Prompt blocks on empty and on filled caches, alone and ragged: tiles of 128 and of 256 query rows."""
+    c = Cache(lens, rows, KVH, hd, 32, BF, seed=hd, pad=2)
+    c.check(H)
+    c.check(H, max_rows=max(rows), max_len=max(a + b for a, b in zip(lens, rows)))
+    c.check(H, window=100)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("rows,lens,window", [(1, [30000, 50], 0), (40, [9000], 0), (70, [9000, 9], 0), (300, [7001], 0), (2, [20000], 9000),
+                                              (90, [12000], 5000)])
+def test_attention_one_range_over_a_long_context(rows, lens, window, dtype):
+    """A hint of short contexts leaves one workgroup a whole one: more blocks than its lanes hold page numbers for."""
+    holes = [(0, j) for j in (0, 31, 32, 33, 63, 64, 65, 127, 128, 200)]
+    Cache(lens, [rows] * len(lens), 1, 64, 32, dtype, seed=rows, holes=holes).check(2, max_rows=rows, max_len=16, window=window)
+    Cache(lens, [rows] * len(lens), 1, 128, 32, dtype, seed=rows).check(3, max_rows=rows, max_len=16, window=window)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("B", [2, 63, 64, 65, 130])
+def test_attention_many_ragged_streams(B, dtype):
+    """Lengths and rows of every size, on either side of what a wave's lanes can cut; two streams carry most of the tokens."""
+    lens = [(37 * b * b) % 90 for b in range(B)]
+    lens[0], lens[B // 2 if B > 2 else 1] = 5000, 2500
+    rows = [(b * 7) % 5 for b in range(B)]
+    rows[0] = 3
+    Cache(lens, rows, 1, 64, 32, dtype, seed=B, pad=2).check(4)
+    rows[B - 1] = 140                                     # one prompt block among them
+    Cache(lens, rows, 1, 64, 32, dtype, seed=B, pad=2).check(4, max_rows=140, max_len=5003)
+    for each in (2, 30):                                  # equal shares without offsets, one range and several
+        c = Cache(lens, [each] * B, 1, 64, 32, dtype, seed=B)
+        q = c.queries(4)
+        want = c.reference(q, 0.125)
+        for hint in (16, 5003):
+            c.close(cs.cs_paged_fp4_attention(c.pages, q, max_len=hint), *want)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_attention_scale_and_peaked_scores(dtype):
+    c = Cache([300, 1], [5, 2], 2, 64, 32, dtype)
+    c.check(4, scale=0.01)
+    c.check(4, spread=30.0)
+    c = Cache([300, 1], [90, 70], 2, 128, 32, dtype)
+    c.check(4, spread=30.0)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("rows", [1, 100])
+def test_attention_of_small_and_large_scales(rows, dtype):
+    """Groups whose scales lie far apart: what a key contributes goes with its own.  (Up to 6 * 2^86: a sum of 2^30 values, each times a
+    probability of up to 2^8 before it is divided by their sum, is finite in float32 below 2^90; 6 * 2^125 times 2^8 is not.)"""
+    c = Cache([200], [rows], 1, 64, 32, dtype)
+    table = c.table[0].tolist()
+    n = 200 + rows
+    for scales, codes, tok in ((c.ks, c.k, c.k_tok), (c.vs, c.v, c.v_tok)):
+        s = torch.randint(100, 130, (2, n), generator=gen(rows), device=DEV, dtype=torch.uint8)
+        s[0, 3::7], s[1, 5::7] = 2, 213 if scales is c.vs else 2
+        for j in range(-(-n // 32)):
+            a, e = j * 32, min(n, j * 32 + 32)
+            scales[table[j], 0, :, :e - a] = s[:, a:e]
+            tok[0][0, a:e] = decode(codes[table[j], 0, :e - a], s[:, a:e].T.contiguous())
+    c.check(2)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_attention_lengths_outside_the_table(dtype):
+    """Negative lengths count as 0; tokens that the table has no column for do not exist."""
+    for rows in (1, 60):
+        c = Cache([20, 70], [rows, rows], 2, 64, 32, dtype, grown=[100, 100])
+        c.ks.fill_(127), c.vs.fill_(127)
+        q = c.queries(4)
+        short = c.handle(table=c.table[:, :2].contiguous())
+        c.length.copy_(torch.tensor([-7, 2 ** 31 - 1]))
+        got = cs.cs_paged_fp4_attention(short, q)
+        c.length.copy_(torch.tensor([0, 64]))
+        assert torch.equal(got, cs.cs_paged_fp4_attention(short, q))
+        last = cs.cs_paged_fp4_attention(short, q)[rows:]
+        c.length.copy_(torch.tensor([0, 63]))                              # (its first row sees all 64 there)
+        assert torch.equal(cs.cs_paged_fp4_attention(short, q)[rows:], last)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_attention_strided_rows_and_in_place(dtype):
+    for rows in (5, 40):
+        c = Cache([100, 3], [rows, rows], 2, 64, 32, dtype)
+        R = 2 * rows
+        q = c.queries(4)
+        want = cs.cs_paged_fp4_attention(c.pages, q)
+        wide = torch.full((R, 3, 8, 72), 9.0, dtype=dtype, device=DEV)
+        src, dst = wide[:, 0, :4, :64], wide[:, 2, 4:, :64]
+        src.copy_(q)
+        cs.cs_paged_fp4_attention(c.pages, src, out=dst)
+        assert torch.equal(dst, want)
+        assert bool((wide[:, 1] == 9.0).all()) and bool((wide[..., 64:] == 9.0).all()) and torch.equal(src, q)
+        cs.cs_paged_fp4_attention(c.pages, src, out=src)
+        assert torch.equal(src, want)
+        turned = q.permute(1, 0, 2).contiguous().permute(1, 0, 2)         # head-major rows
+        assert torch.equal(cs.cs_paged_fp4_attention(c.pages, turned), want)
+
+
+@pytest.mark.parametrize("hd,H,KVH", [(128, 8, 2), (64, 7, 1), (256, 4, 2)])
+@pytest.mark.parametrize("P,L,rows", [(1024, 683, 336), (2048, 1501, 543), (1024, 1, 1021)])
+def test_attention_pool_of_one_page(P, L, rows, hd, H, KVH):
+    """A pool that ends with its only page, cut into ranges of which the early tiles have nothing."""
+    c = Cache([L], [rows], KVH, hd, P, BF, seed=hd, spare=0)
+    assert c.k.shape[0] == 1
+    q = c.queries(H)
+    want = c.reference(q, 1 / math.sqrt(hd))
+    for call in (dict(max_len=L + rows), dict(row0=c.row0), dict(row0=c.row0, max_rows=rows, max_len=L + rows)):
+        c.close(cs.cs_paged_fp4_attention(c.pages, q, **call), *want)
+
+
+# ------------------------------------------------------------------------------------------------------
+# together, on streams, in graphs; what a caller may get wrong
+# ------------------------------------------------------------------------------------------------------
+
+def _layer(c, qkv, H, KVH, f, pos, **call):
+    q, k = cs.cs_op_qk_norm_rope(qkv[:, :H], qkv[:, H:H + KVH], pos, f, **call)
+    cs.cs_paged_fp4_append(c.pages, k, qkv[:, H + KVH:], row0=c.row0, **call)
+    return cs.cs_paged_fp4_attention(c.pages, q, row0=c.row0, **call)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_steps_of_a_layer(dtype):
+    """Rotation, append, read and attention as a serving loop runs them: a prompt in two chunks, then blocks of copied tokens of
+    which some are dropped again, against attention over the plain concatenation of the quantised rows."""
+    H, KVH, hd, P = 8, 2, 64, 32
+    c = Cache([0, 0], [0, 0], KVH, hd, P, dtype, grown=[400, 400])
+    g = gen(11)
+    f = torch.tensor([10000.0 ** (-2.0 * j / hd) for j in range(hd // 2)], dtype=torch.float64, device=DEV)
+    keys = [torch.zeros((0, KVH, hd), dtype=torch.float64, device=DEV) for _ in range(2)]
+    vals = [k.clone() for k in keys]
+    for rows, kept in (((70, 3), (70, 3)), ((33, 120), (33, 120)), ((11, 11), (4, 11)), ((1, 11), (1, 1)), ((6, 0), (2, 0)), ((1, 1), (1, 1))):
+        lens = [k.shape[0] for k in keys]
+        c.lens, c.rows, c.ends = lens, list(rows), [0, rows[0], sum(rows)]
+        c.row0.copy_(torch.tensor(c.ends))
+        c.length.copy_(torch.tensor(lens))
+        qkv = randn((sum(rows), H + 2 * KVH, hd), g, dtype)
+        pos = torch.cat([torch.arange(n, n + r, device=DEV, dtype=torch.int32) for n, r in zip(lens, rows)])
+        got = _layer(c, qkv, H, KVH, f, pos)
+        q, k = cs.cs_op_qk_norm_rope(qkv[:, :H], qkv[:, H:H + KVH], pos, f)
+        new_k, new_v = decode(*quantise(k)), decode(*quantise(qkv[:, H + KVH:]))
+        read_k, read_v = cs.cs_paged_fp4_read(c.pages, R=sum(rows), row0=c.row0)
+        assert torch.equal(read_k.double(), new_k) and torch.equal(read_v.double(), new_v)
+        c.k_tok = [torch.cat([keys[b], new_k[c.ends[b]:c.ends[b + 1]]]).transpose(0, 1).contiguous() for b in range(2)]
+        c.v_tok = [torch.cat([vals[b], new_v[c.ends[b]:c.ends[b + 1]]]).transpose(0, 1).contiguous() for b in range(2)]
+        c.close(got, *c.reference(q, 1 / math.sqrt(hd)))
+        for b in range(2):
+            n = lens[b] + kept[b]
+            keys[b], vals[b] = c.k_tok[b].transpose(0, 1)[:n], c.v_tok[b].transpose(0, 1)[:n]
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("rows", [[1, 1, 1], [11, 3, 0], [200, 1, 1]])
+def test_captured_layer_follows_the_lengths(rows, dtype):
+    """A captured step replayed while the lengths in device memory grow, between eager steps on another cache."""
+    H, KVH, hd, P = 8, 2, 128, 32
+    lens = [40, 7, 5000]
+    c, e = (Cache(lens, rows, KVH, hd, P, dtype, seed=6, grown=[r + 400 for r in rows]) for _ in range(2))
+    f = torch.tensor([10000.0 ** (-2.0 * j / hd) for j in range(hd // 2)], dtype=torch.float64, device=DEV)
+    R = sum(rows)
+    qkv = randn((R, H + 2 * KVH, hd), gen(12), dtype)
+    pos = torch.zeros(R, dtype=torch.int32, device=DEV)
+    step = torch.ones(3, dtype=torch.int32, device=DEV)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        _layer(c, qkv, H, KVH, f, pos)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = _layer(c, qkv, H, KVH, f, pos)
+        back = cs.cs_paged_fp4_read(c.pages, R=R)[0] if R % 3 == 0 else None
+        c.length.add_(step)
+    for i in range(4):
+        qkv.copy_(randn(qkv.shape, gen(100 + i), dtype))
+        pos.copy_(torch.cat([torch.arange(n + i, n + i + r, device=DEV, dtype=torch.int32) for n, r in zip(lens, rows)]))
+        want = _layer(e, qkv, H, KVH, f, pos)
+        want_back = cs.cs_paged_fp4_read(e.pages, R=R)[0] if R % 3 == 0 else None
+        e.length.add_(step)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want) and (back is None or same(back, want_back)), i
+
+
+def test_two_streams_at_once():
+    """Calls on two streams with a workspace each give what they give alone."""
+    a = Cache([9000, 20011], [11, 11], 2, 128, 64, BF, seed=1)
+    b = Cache([4000, 100], [1, 1], 2, 128, 32, BF, seed=2)
+    qa, qb = a.queries(8), b.queries(8)
+    wa, wb = cs.cs_paged_fp4_attention(a.pages, qa), cs.cs_paged_fp4_attention(b.pages, qb)
+    torch.cuda.synchronize()
+    s1, s2 = torch.cuda.Stream(), torch.cuda.Stream()
+    got = []
+    for _ in range(5):
+        got.append((cs.cs_paged_fp4_attention(a.pages, qa, stream=s1), cs.cs_paged_fp4_attention(b.pages, qb, stream=s2.cuda_stream)))
+        got.append((cs.cs_paged_fp4_attention(a.pages, qa, stream=0), cs.cs_paged_fp4_attention(b.pages, qb, stream=torch.cuda.default_stream())))
+    torch.cuda.synchronize()
+    for x, y in got:
+        assert torch.equal(x, wa) and torch.equal(y, wb)
+    row = randn((2, 2, 128), gen(5), BF)
+    cs.cs_paged_fp4_append(b.pages, row, -row, stream=s1)
+    k, v = cs.cs_paged_fp4_read(b.pages, R=2, stream=s1)
+    s1.synchronize()
+    assert torch.equal(k.double(), decode(*quantise(row))) and torch.equal(v, -k)
+
+
+def test_workspace_of_the_callers():
+    c = Cache([9000, 20011], [11, 11], 2, 128, 64, BF)
+    q = c.queries(8)
+    want = cs.cs_paged_fp4_attention(c.pages, q, max_rows=11, max_len=20022)
+    need = cs.cs_paged_fp4_attention_workspace(c.pages, 8, 22, max_rows=11, max_len=20022)
+    assert need > 0
+    ws = torch.full((need + 64,), 0xA5, dtype=torch.uint8, device=DEV)
+    assert torch.equal(cs.cs_paged_fp4_attention(c.pages, q, max_rows=11, max_len=20022, workspace=ws[:need]), want)
+    assert bool((ws[need:] == 0xA5).all())
+    with pytest.raises(cs.CopySpecError):
+        cs.cs_paged_fp4_attention(c.pages, q, max_rows=11, max_len=20022, workspace=ws[:need - 16])
+
+
+def test_pools_beyond_two_to_the_32_bytes():
+    """Pages whose byte offset needs 33 bits and more, of codes and, by their stride, of scales."""
+    P, KVH, hd, n_pages = 256, 8, 128, 40000                          # 5.2 GB a pool
+    names = [0, 39999, 16383, 32767, 32768, 36000]
+    c = Cache([6 * P - 8], [8], KVH, hd, P, BF)
+    k, v = (torch.empty((n_pages, KVH, P, hd // 2), dtype=torch.uint8, device=DEV) for _ in range(2))
+    ks, vs = (torch.empty((n_pages, KVH, 16, P), dtype=torch.uint8, device=DEV)[:, :, 3:7] for _ in range(2))
+    order = c.table[0, :6].long()
+    for big, small in ((k, c.k), (v, c.v), (ks, c.ks), (vs, c.vs)):
+        big[torch.tensor(names, device=DEV)] = small[order]
+    c.k, c.v, c.ks, c.vs = k, v, ks, vs
+    c.table = torch.tensor([names], dtype=torch.int32, device=DEV)
+    c.pages = c.handle()
+    c.check(32)
+    row = randn((8, KVH, hd), gen(3), BF)
+    cs.cs_paged_fp4_append(c.pages, row, -row)
+    qc, qs = quantise(row)
+    assert torch.equal(k[36000, :, P - 8:].transpose(0, 1), qc) and torch.equal(ks[36000, :, :, P - 8:].permute(2, 0, 1), qs)
+    got, neg = cs.cs_paged_fp4_read(c.pages, R=8)
+    assert torch.equal(got.double(), decode(qc, qs)) and torch.equal(neg, -got)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_results_repeat_bit_for_bit(dtype):
+    """Nothing depends on the order in which workgroups finish."""
+    c = Cache([3000, 17, 900], [40, 1, 5], 2, 128, 32, dtype, pad=1)
+    q, got = c.check(8)
+    for _ in range(5):
+        assert torch.equal(cs.cs_paged_fp4_attention(c.pages, q, row0=c.row0)[:46], got[:46])
+
+
+def test_no_rows_and_no_streams():
+    c = Cache([20], [1], 2, 64, 32, BF)
+    empty = torch.empty((0, 4, 64), dtype=BF, device=DEV)
+    assert cs.cs_paged_fp4_attention(c.pages, empty).shape == (0, 4, 64)
+    cs.cs_paged_fp4_append(c.pages, empty[:, :2], empty[:, :2])
+    assert cs.cs_paged_fp4_read(c.pages, R=0)[0].shape == (0, 2, 64)
+    none = c.handle(table=c.table[:0], length=c.length[:0])
+    q = torch.full((2, 4, 64), 3.0, dtype=BF, device=DEV)
+    out = q.clone()
+    cs.cs_paged_fp4_attention(none, q, out=out)
+    cs.cs_paged_fp4_append(none, q[:, :2], q[:, :2])
+    assert torch.equal(out, q)
+    # rows of which no stream has any
+    nobody = torch.zeros(2, dtype=torch.int32, device=DEV)
+    before = c.state()
+    cs.cs_paged_fp4_attention(c.pages, q, row0=nobody, out=out)
+    cs.cs_paged_fp4_append(c.pages, q[:, :2], q[:, :2], row0=nobody)
+    assert torch.equal(out, q) and all(torch.equal(x, y) for x, y in zip(before, c.state()))
+
+
+NO_SENSE = {3: ([0, 100, 3, 6], [-50, 2, 2000000000, 6], [6, 4, 2, 0], [0, -1, -2, -3], [2 ** 31 - 1] * 4, [0, 6, 0, 6]),
+            73: ([0, 146] * 37, [146 - 2 * b for b in range(74)], [0] * 73 + [146], [(b * 97) % 300 - 50 for b in range(74)])}
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("B,hint", [(3, 0), (3, 2), (3, 200), (73, 0), (73, 2), (73, 100)])
+def test_row_offsets_that_make_no_sense_stay_inside(B, hint, dtype):
+    """Offsets outside 0..R or decreasing: nothing around the outputs, the workspace (of exactly the size asked for) and the pools is
+    written, and rows that no stream has are left as they were."""
+    c = Cache([3000, 40, 1000] + [9] * (B - 3), [2] * B, 2, 64, 32, dtype)
+    R = 2 * B
+    guard = Guarded()
+    pools = [guard.like(t.shape, torch.uint8) for t in (c.k, c.v, c.ks, c.vs)]
+    q = c.queries(4)
+    for bad in NO_SENSE[B]:
+        for t, x in zip(pools, (c.k, c.v, c.ks, c.vs)):
+            t.copy_(x)
+        pages = c.handle(k=pools[0], v=pools[1], k_scale=pools[2], v_scale=pools[3])
+        row0 = torch.tensor(bad, dtype=torch.int32, device=DEV)
+        call = dict(max_rows=hint, max_len=3002 if hint else 0)
+        need = cs.cs_paged_fp4_attention_workspace(pages, 4, R, row0=True, dtype=dtype, **call)
+        ws, out = guard.like((need,), torch.uint8) if need else None, guard.like((R, 4, 64), dtype, 5.0)
+        cs.cs_paged_fp4_attention(pages, q, row0=row0, out=out, workspace=ws, **call)
+        back = guard.like((2, R, 2, 64), dtype, 5.0)
+        cs.cs_paged_fp4_read(pages, row0=row0, out=(back[0], back[1]))
+        claimed = set()
+        for a, e in zip(bad, bad[1:]):
+            claimed |= set(range(min(max(a, 0), R), min(max(e, 0), R)))
+        for r in range(R):
+            if r not in claimed:
+                assert bool((out[r] == 5.0).all()) and bool((back[:, r] == 5.0).all()), (bad, r)
+        assert all(torch.equal(t, x) for t, x in zip(pools, (c.k, c.v, c.ks, c.vs)))
+        # appended rows lie in the slots that the streams' lengths and the offsets name, and nowhere else
+        cs.cs_paged_fp4_append(pages, q[:, :2], q[:, :2], row0=row0)
+        slots = torch.zeros((c.k.shape[0], 32), dtype=torch.bool)
+        table = c.table.cpu()
+        for b, (a, e) in enumerate(zip(bad, bad[1:])):
+            for i in range(min(max(e, 0), R) - min(max(a, 0), R)):
+                at = c.lens[b] + i
+                if at < 32 * table.shape[1] and 0 <= int(table[b][at // 32]) < c.k.shape[0]:
+                    slots[int(table[b][at // 32]), at % 32] = True
+        rest = ~slots.to(DEV)
+        for new, old in zip(pools[:2], (c.k, c.v)):
+            assert torch.equal(new.permute(0, 2, 1, 3)[rest], old.permute(0, 2, 1, 3)[rest]), bad
+        for new, old in zip(pools[2:], (c.ks, c.vs)):
+            assert torch.equal(new.permute(0, 3, 1, 2)[rest], old.permute(0, 3, 1, 2)[rest]), bad
+        guard.check()
+
+
+def test_broadcast_inputs_and_outputs_that_would_overlap():
+    """One row for all, one KV head's pool for all; what is written may not overlap itself."""
+    c = Cache([40, 3], [2, 2], 1, 64, 32, BF)
+    q = randn((1, 4, 64), gen(1), BF)
+    wide = cs.PagesFP4(*(t.expand(-1, 2, -1, -1) for t in (c.k, c.v, c.ks, c.vs)), c.table, c.length)
+    want = cs.cs_paged_fp4_attention(c.pages, q.expand(4, 4, 64).contiguous())
+    c.close(want, *c.reference(q.expand(4, 4, 64).contiguous(), 0.125))
+    assert torch.equal(cs.cs_paged_fp4_attention(wide, q.expand(4, 4, 64)), want)
+    row = q[:, :1]
+    cs.cs_paged_fp4_append(c.pages, row.expand(4, 1, 64), row.expand(4, 1, 64))
+    got, _ = cs.cs_paged_fp4_read(c.pages, R=4)
+    assert torch.equal(got.double(), decode(*quantise(row)).expand(4, 1, 64))
+    for call in (lambda: cs.cs_paged_fp4_attention(c.pages, q.expand(4, 4, 64), out=q.expand(4, 4, 64)),
+                 lambda: cs.cs_paged_fp4_append(wide, want[:, :2], want[:, :2]),
+                 lambda: cs.cs_paged_fp4_read(c.pages, out=(row.expand(4, 1, 64), row.expand(4, 1, 64)))):
+        with pytest.raises(cs.CopySpecError, match="overlap"):
+            call()
+
+
+def test_sizes_that_need_more_than_32_bits_are_refused():
+    c = Cache([40, 3], [2, 2], 2, 64, 32, BF)
+    q = c.queries(4)
+    big = (1 << 32) + 5
+    many = q[:1, :2].expand((1 << 32) + 1, 2, 64)                               # (a view: one row)
+    for call in (lambda: cs.cs_paged_fp4_attention(c.pages, q, window=big), lambda: cs.cs_paged_fp4_attention(c.pages, q, max_rows=big),
+                 lambda: cs.cs_paged_fp4_attention(c.pages, many, out=many), lambda: cs.cs_paged_fp4_append(c.pages, many, many),
+                 lambda: cs.cs_paged_fp4_read(c.pages, out=(many, many)), lambda: cs.cs_paged_fp4_attention_workspace(c.pages, 4, big)):
+        with pytest.raises(ValueError, match="32 bits"):
+            call()
+    assert torch.equal(cs.cs_paged_fp4_attention(c.pages, q, window=(1 << 31) - 1), cs.cs_paged_fp4_attention(c.pages, q))
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_attention_of_the_most_workgroups(dtype):
+    """65536 streams of 64 KV heads, one token each: 2^22 workgroups, which stand along two dimensions of the grid.  All streams have
+    the same page."""
+    B, H, hd, P, L = 65536, 64, 32, 32, 3
+    c = Cache([L], [1], H, hd, P, dtype, spare=0)
+    pages = c.handle(table=torch.zeros((B, 1), dtype=torch.int32, device=DEV), length=torch.full((B,), L, dtype=torch.int32, device=DEV))
+    q = randn((B, H, hd), gen(4), dtype)
+    out = cs.cs_paged_fp4_attention(pages, q, max_rows=1, max_len=P)
+    x = q.double()
+    k, v = c.k_tok[0], c.v_tok[0]
+    s = torch.stack([(x * k[:, t]).sum(-1) for t in range(L + 1)]) / math.sqrt(hd)
+    d = torch.stack([(x * k[:, t]).abs().sum(-1) for t in range(L + 1)]).amax(0) / math.sqrt(hd)
+    p = torch.softmax(s, 0)
+    want, mag = torch.zeros_like(x), torch.zeros_like(x)
+    for t in range(L + 1):
+        want += p[t][..., None] * v[:, t]
+        mag += p[t][..., None] * v[:, t].abs()
+    c.close(out, want, mag, d[..., None])
