@@ -43,6 +43,174 @@ __device__ __forceinline__ void f4_split(const float* p, bf16x8 (&o)[3]) {
     f4_split8(x, o);
 }
 
+// ---- which tiles and tokens a workgroup of the kernel of few rows has ----------------------------------------
+// The G * rows query rows of a stream's KV head (row n: block row n / G, head n % G of the group) are cut into
+// tiles of TR; streams with qr_lo < G * rows <= qr_hi take part.  W workgroups per KV head are as many as run at
+// once, and all tokens are cut among them on the device, from the lengths, by every workgroup for itself:
+//   pieces: a workgroup has one piece of one tile, at most `piece` blocks of 32 tokens, the smallest size with no more
+//           than W pieces; each lane tries another one;
+//   shares: the blocks of all tiles are laid end to end and each workgroup takes as many of them: the end of one tile,
+//           whole ones, the beginning of another.  For streams of different lengths, where pieces are uneven, and
+//           for more tiles than workgroups.
+// What a workgroup has of a tile that it does not have alone is a partial result, at most two of them, which a merge
+// joins.  (W 0: a workgroup each tile, no partial results.)
+struct f4_shares {
+    int TR, qr_lo, qr_hi;
+    int W, least;             // workgroups per KV head; fewest blocks of a piece or a share
+    int step;                 // distance of the numbers of pieces tried
+    int near;                 // neighbouring KV heads that run on one die
+    float* po;                // [2 W][KVH][TR][hd] partial outputs; 2w: of a tile that an earlier workgroup has begun, 2w + 1: of one that w begins
+    float2* pml;              // [2 W][KVH][TR] their (maximum, sum)
+    int4* who;                // [2 W] (first row, first query row, query rows, number | workgroups of the tile << 16) for the merge; 0: nothing
+};
+struct f4_call {
+    cs_fp4_dev F;
+    pa_args A;
+    f4_shares S;
+};
+struct f4_segment {
+    int b, n0;                // stream, first query row
+    int off, n;               // first block of the tile's, blocks (W 0: all of them)
+    bool first, whole;        // the tile's first blocks, all of its blocks
+    int row0, rows, len;      // of the stream
+    int number, of;           // of the workgroups that have a part of the tile
+};
+
+// A segment costs its start and its end beside its blocks, in blocks of 32 tokens.
+#define F4_SEGMENT 10
+
+// tiles of a stream and the blocks that one of them walks (W 0: 1)
+__device__ __forceinline__ int2 f4_extent(const cs_pages_dev& D, int G, int window, const f4_shares& S, int rows, int len) {
+    const int64_t qr = (int64_t)rows * G;
+    if (qr <= S.qr_lo || qr > S.qr_hi) return make_int2(0, 0);
+    int span = min(len + rows, D.cap);
+    if (window) span = (int)min((int64_t)span, (int64_t)window + min(rows, S.TR / G + 1) + 32);
+    return make_int2((int)((qr + S.TR - 1) / S.TR), S.W ? max((span + 31) >> 5, 1) : 1);
+}
+
+// Positions count units: blocks of all tiles (shares) or pieces; a lane looks at one of 64 streams.  (The host makes
+// sure that they fit 31 bits.)
+struct f4_walk {
+    int p, end;               // position and end of the workgroup's share
+    int share;                // units of a share (pieces: 1)
+    int piece;                // blocks of a unit (shares: 1)
+    int start;                // units that stand for the start of a tile, before its blocks (pieces: 0)
+    int b0, before;           // the streams that are looked at, units before them
+    int2 e, rows;             // a lane's: tiles, blocks of each; first row and rows
+    int len;                  // its length
+    int units, upto;          // a lane's: units of a tile; of these streams up to and with its own
+    bool have;
+};
+__device__ __forceinline__ void f4_look_at(const cs_pages_dev& D, int G, int window, const f4_shares& S, f4_walk& k, int lane) {
+    k.e = k.rows = make_int2(0, 0), k.len = 0;
+    if (k.b0 + lane < D.p.batch) {
+        k.rows = cs_stream_rows(D, k.b0 + lane);
+        k.len = cs_stream_len(D, k.b0 + lane);
+        k.e = f4_extent(D, G, window, S, k.rows.y, k.len);
+    }
+    k.units = (k.e.y + k.start + k.piece - 1) / k.piece;
+    k.upto = pa_wave_scan(k.e.x * k.units);
+    k.have = true;
+}
+__device__ __forceinline__ f4_walk f4_start(const cs_pages_dev& D, int G, int window, const f4_shares& S, int w, int lane) {
+    f4_walk k;
+    k.p = w, k.end = w + 1, k.share = k.piece = 1, k.start = k.b0 = k.before = 0, k.have = false;
+    k.e = k.rows = make_int2(0, 0), k.len = k.units = k.upto = 0;
+    const int B = D.p.batch;
+    if (!S.W) {
+        if (!D.row0) {                                          // equal rows: the stream is known
+            const int tiles = f4_extent(D, G, window, S, D.rows, 0).x;
+            const int b = __builtin_amdgcn_readfirstlane(w / max(tiles, 1));
+            k.b0 = b & ~63;
+            k.before = k.b0 * tiles;
+            if (b >= B) k.end = k.p;
+        }
+        return k;
+    }
+    int all = 0, tiles = 0;
+    k.start = F4_SEGMENT;
+    for (; k.b0 < B; k.b0 += 64) {
+        f4_look_at(D, G, window, S, k, lane);
+        all += __builtin_amdgcn_readlane(k.upto, 63);
+        if (B <= 64) {
+            tiles = __builtin_amdgcn_readlane(pa_wave_scan(k.e.x), 63);
+            break;
+        }
+    }
+    k.share = max((all + S.W - 1) / S.W, S.least);
+    if (B <= 64 && tiles <= S.W) {
+        const int longest = __builtin_amdgcn_readlane(pa_wave_reduce(k.e.y, 0, [](int a, int b) { return max(a, b); }), 63);
+        const int n = 1 + lane * S.step, cut = max((longest + n - 1) / n, S.least);
+        const float inv = 1.0f / (float)cut;
+        int count = 0;
+        for (int i = 0; i < B; ++i) {
+            const int blocks = __builtin_amdgcn_readlane(k.e.y, i), q = (int)((float)blocks * inv), r = blocks - q * cut;
+            count += __builtin_amdgcn_readlane(k.e.x, i) * (q + (r > 0) + (r > cut));             // (q is off by one at most)
+        }
+        const int best = __builtin_amdgcn_readlane(pa_wave_reduce(count <= S.W ? cut : 0x7fffffff, 0x7fffffff, [](int a, int b) { return min(a, b); }), 63);
+        if (best <= k.share + F4_SEGMENT) {
+            k.piece = best;
+            k.share = 1;
+            k.start = 0;
+            k.units = (k.e.y + best - 1) / best;
+            k.upto = pa_wave_scan(k.e.x * k.units);
+            all = __builtin_amdgcn_readlane(k.upto, 63);
+        }
+    }
+    k.b0 = 0;
+    k.have = B <= 64;
+    k.p = (int)min((int64_t)k.share * w, (int64_t)all);
+    k.end = min(k.p + k.share, all);
+    return k;
+}
+__device__ __forceinline__ bool f4_next(const cs_pages_dev& D, int G, int window, const f4_shares& S, int w, f4_walk& k, int lane, f4_segment& o) {
+    if (k.p >= k.end) return false;
+    for (;;) {
+        if (!k.have) f4_look_at(D, G, window, S, k, lane);
+        const int all = __builtin_amdgcn_readlane(k.upto, 63);
+        if (k.p < k.before + all) break;
+        k.before += all;
+        k.b0 += 64;
+        k.have = false;
+        if (k.b0 >= D.p.batch) return false;                    // (more workgroups than tiles)
+    }
+    const int l = __ffsll(__ballot(k.before + k.upto > k.p)) - 1;
+    const int tiles = __builtin_amdgcn_readlane(k.e.x, l), blocks = __builtin_amdgcn_readlane(k.e.y, l), units = __builtin_amdgcn_readlane(k.units, l);
+    o.row0 = __builtin_amdgcn_readlane(k.rows.x, l), o.rows = __builtin_amdgcn_readlane(k.rows.y, l), o.len = __builtin_amdgcn_readlane(k.len, l);
+    const unsigned at = k.p - (k.before + __builtin_amdgcn_readlane(k.upto, l) - tiles * units);
+    const int tile = __builtin_amdgcn_readfirstlane(tiles == 1 ? 0 : at / (unsigned)units), off = at - tile * units;
+    const int n = min(units - off, k.end - k.p);
+    o.b = k.b0 + l;
+    o.n0 = tile * S.TR;
+    o.off = max(off * k.piece - k.start, 0);
+    o.n = max((off + n) * k.piece - k.start, 0) - o.off;
+    o.first = off == 0;
+    o.whole = n == units;
+    o.number = 0, o.of = 1;
+    if (!o.whole) {
+        const int first = __builtin_amdgcn_readfirstlane((unsigned)(k.p - off) / (unsigned)k.share);
+        o.number = w - first;
+        o.of = __builtin_amdgcn_readfirstlane((unsigned)(k.p - off + units - 1) / (unsigned)k.share) - first + 1;
+    }
+    k.p += n;
+    return true;
+}
+// Workgroup -> (w, KV head).  Dies take workgroups in turn, eight of them, each with a cache of its own: `near` heads whose
+// rows share cache lines (a token-major pool has 64 bytes of codes of a head of 128 features next to its neighbour's)
+// are eight workgroups apart.
+__device__ __forceinline__ int2 f4_whose(unsigned wg, int KVH, int W_all, int near) {
+    const int groups = KVH / near, whole = W_all * groups >> 3;              // (w, head group) pairs, in eights
+    const int i = wg >> 3, x = wg & 7, turn = i / near;
+    int u, j;
+    if (turn < whole) u = turn * 8 + x, j = i - turn * near;
+    else {
+        const int r = wg - whole * 8 * near;
+        u = whole * 8 + r / near, j = r % near;
+    }
+    const int w = u / groups;
+    return make_int2(w, (u - w * groups) * near + j);
+}
+
 // ---- few query rows: the stream of codes is the bound ---------------------------------------------------
 // Four waves share a tile of up to 48 query rows and take the 32-token blocks of a token range in turn; codes,
 // scores and outputs stay in registers:
@@ -54,8 +222,7 @@ __device__ __forceinline__ void f4_split(const float* p, bf16x8 (&o)[3]) {
 // rows of S^T that the lane gets, and the value rows it needs, are the tokens 8g .. 8g + 7: their scales are
 // eight bytes of the page.  Of those value rows a lane loads HD / 16 features each, makes them bfloat16 and
 // turns pairs of tokens with byte permutes into the A fragments: fragment u has feature c * HD / 16 + u in row
-// c.  A page holds whole blocks, so every load has one page and a uniform base: a buffer that ends with the
-// last token.  Loads past it, and of pages that do not exist, return zeros and cost no traffic.
+// c.  A page holds whole blocks, so every load has one page, a uniform base, and nothing to check.
 #define F4N_WAVES 4
 template <int HD>
 struct f4_keys { u32x4 k[2][HD == 256 ? 2 : 1]; u32x2 s[HD == 256 ? 2 : 1]; };
@@ -63,35 +230,73 @@ template <int HD>
 struct f4_values { unsigned v[8][HD == 256 ? 2 : 1]; u32x2 s; };
 
 template <int HD, int NT, int NP>
-__global__ __launch_bounds__(64 * F4N_WAVES, 2) void k_paged_fp4_narrow(cs_fp4_dev F, pa_args A, pa_plan P) {
+__global__ __launch_bounds__(64 * F4N_WAVES, 2) void k_paged_fp4_narrow(f4_call C) {
     typedef f4_qtype<NP> T_;
     constexpr int KS = HD / 32, MT = HD / 16, VF = HD / 16;
     constexpr int KB = HD == 256 ? 2 : 1;                       // 32-feature pieces of a lane's key row (HD 64: half of one)
     constexpr int VW = HD == 256 ? 2 : 1;                       // dwords of a lane's value row (HD 64: half of one)
+    constexpr bool QREG = NT == 1 && NP == 1;                   // the query fragments stay in registers, else they are read from LDS
     constexpr int AHEAD = HD == 256 || NT > 1 || NP > 1 ? 2 : 4;         // blocks in flight
     constexpr int ROWS = 16 * NT, QROW = HD * 2 + 16, QPLANE = ROWS * QROW;
     constexpr int SLOT = NT * (MT * 1024 + 512);                // a wave's (O, maximum, sum)
     constexpr int LDS_BYTES = 2 * SLOT > NP * QPLANE ? 2 * SLOT : NP * QPLANE;
     __shared__ __attribute__((aligned(16))) unsigned char smem[LDS_BYTES];
-    const cs_pages_dev& D = F.d;
+    // The arguments fill the scalar registers several times over.  Read anew for every segment and behind its loop, they
+    // are not carried through it.
+    typedef const __attribute__((address_space(4))) f4_call* call_ptr;
+    auto call = [&]() -> const f4_call& {
+        call_ptr p = (call_ptr)__builtin_amdgcn_kernarg_segment_ptr();
+        asm volatile("" : "+s"(p));
+        return *(const f4_call*)p;
+    };
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int c = lane & 15, g = lane >> 4;
-    const unsigned wg = cs_paged_wg();
-    const int KVH = D.p.n_kv_heads, kvh = wg % KVH;
-    pa_work K;
-    if (!pa_find(D, A.G, A.window, P, wg / KVH, kvh, K)) return;
-    const pa_tile& T = K.T;
-    const int hd = D.p.head_dim;
+    int w, kvh;
+    f4_walk walk;
+    {
+        const f4_call& C0 = call();
+        const int2 o = f4_whose(cs_paged_wg(), C0.F.d.p.n_kv_heads, C0.S.W ? C0.S.W : C0.S.step, C0.S.near);
+        w = __builtin_amdgcn_readfirstlane(o.x), kvh = __builtin_amdgcn_readfirstlane(o.y);
+        walk = f4_start(C0.F.d, C0.A.G, C0.A.window, C0.S, w, lane);
+        if (C0.S.W && kvh == 0 && tid == 0) C0.S.who[2 * w] = C0.S.who[2 * w + 1] = make_int4(0, 0, 0, 0);
+    }
+    f4_segment K;
+    for (;;) {
+    const f4_call& C1 = call();
+    const cs_fp4_dev& F = C1.F;
+    const cs_pages_dev& D = F.d;
+    const pa_args& A = C1.A;
+    if (!f4_next(D, A.G, A.window, C1.S, w, walk, lane, K)) return;
+    if (NT > 1 || HD == 256) walk.have = false;         // (registers: the streams are looked at again)
+    const int hd = D.p.head_dim, cap = D.cap;
+    pa_tile T;
+    T.b = K.b;
+    T.n0 = K.n0;
+    T.row0 = K.row0;
+    T.rows = K.rows;
+    T.QR = T.rows * A.G;
+    T.L = K.len;
+    if (!QREG) __syncthreads();                         // every wave is done with the segment before
     const int n_rows = min(ROWS, T.QR - T.n0);          // live query rows of the tile
     const int i_lo = T.n0 / A.G, i_hi = (T.n0 + n_rows - 1) / A.G;
     const int n_tok = min(T.L + i_hi + 1, D.cap);       // tokens that the tile's last row sees
     const int base = A.window ? max(0, T.L + i_lo - A.window + 1) & ~31 : 0;
-    const int w_begin = (int)min((int64_t)base + (int64_t)K.split * K.chunk, (int64_t)n_tok);
-    const int t_end = K.split == K.nsplit - 1 ? n_tok : (int)min((int64_t)w_begin + K.chunk, (int64_t)n_tok);
+    const int w_begin = (int)min((int64_t)base + (int64_t)K.off * 32, (int64_t)n_tok);
+    const int t_end = K.number == K.of - 1 ? n_tok : (int)min((int64_t)base + ((int64_t)K.off + K.n) * 32, (int64_t)n_tok);
     // blocks between these need no mask
     const int open_lo = A.window ? T.L + i_hi - A.window + 1 : 0, open_hi = min(T.L + i_lo + 1, D.cap);
     const int w_first = A.window ? T.L + i_lo - A.window + 1 : 0;       // tokens before it are seen by no row of the tile
 
+    bf16x8 qreg[KS];
+    if constexpr (QREG) {
+        const int i = (T.n0 + c) / A.G, h = kvh * A.G + T.n0 + c - i * A.G;
+        const bf16_t* qp = (const bf16_t*)A.q + (T.row0 + i) * A.q_row + h * A.q_head + g * (HD / 4);
+#pragma unroll
+        for (int s = 0; s < KS; ++s) {
+            qreg[s] = (bf16x8){0, 0, 0, 0, 0, 0, 0, 0};
+            if (c < n_rows && g * (HD / 4) + s * 8 < hd) qreg[s] = *reinterpret_cast<const bf16x8*>(qp + s * 8);
+        }
+    } else
     // query rows into LDS
     for (int idx = tid; idx < ROWS * (HD / 8); idx += 64 * F4N_WAVES) {
         const int n = idx / (HD / 8), seg = idx % (HD / 8);
@@ -105,31 +310,30 @@ __global__ __launch_bounds__(64 * F4N_WAVES, 2) void k_paged_fp4_narrow(cs_fp4_d
 #pragma unroll
         for (int p = 0; p < NP; ++p) *reinterpret_cast<bf16x8*>(smem + p * QPLANE + n * QROW + seg * 16) = v[p];
     }
-    int q_last[NT], q_first[NT];                        // tokens that the lane's query rows see
+    int q_last[NT];                                     // the last token that the lane's query rows see, and how many before it
+    const int back = A.window ? A.window - 1 : 0x3fffffff;
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
-        const int n = nt * 16 + c, i = (T.n0 + n) / A.G;
-        q_last[nt] = n < n_rows ? T.L + i : -1;
-        q_first[nt] = A.window ? T.L + i - A.window + 1 : 0;
+        const int n = nt * 16 + c;
+        q_last[nt] = n < n_rows ? T.L + (T.n0 + n) / A.G : -1;
     }
 
     const uint8_t *Kh = F.k + kvh * F.k_head, *Vh = F.v + kvh * F.v_head, *KSh = F.ks + kvh * F.ks_head, *VSh = F.vs + kvh * F.vs_head;
     const int32_t* tab = D.p.table + T.b * D.p.table_stride;
-    constexpr unsigned NOWHERE = 0x80000000u;
-    const unsigned kts = (unsigned)F.k_token, vts = (unsigned)F.v_token, kgs = (unsigned)F.ks_group, vgs = (unsigned)F.vs_group;
-    const unsigned row_bytes = hd / 2, n_groups = hd / CS_FP4_GROUP;
-    unsigned koff[2][KB], ksoff[KB], voff[8], vsoff;
+    // (features that the head does not have are read at feature 0: their query elements are 0, their outputs are not stored)
+    unsigned koff[KB], ksoff[KB], voff, vsoff;
+    const unsigned kts = (unsigned)F.k_token, vts = (unsigned)F.v_token;
+    {
 #pragma unroll
-    for (int h = 0; h < KB; ++h) {
-        const int f = g * (HD / 4) + h * 32;
-        const bool there = f < hd;
-#pragma unroll
-        for (int a = 0; a < 2; ++a) koff[a][h] = there ? (8 * (c >> 2) + 4 * a + (c & 3)) * kts + f / 2 : NOWHERE;
-        ksoff[h] = there ? f / CS_FP4_GROUP * kgs + 8 * (c >> 2) : NOWHERE;
+        for (int h = 0; h < KB; ++h) {
+            const int f = g * (HD / 4) + h * 32 < hd ? g * (HD / 4) + h * 32 : 0;
+            koff[h] = (8 * (c >> 2) + (c & 3)) * kts + f / 2;
+            ksoff[h] = f / CS_FP4_GROUP * (unsigned)F.ks_group + 8 * (c >> 2);
+        }
+        const int f = c * VF < hd ? c * VF : 0;
+        voff = 8 * g * vts + f / 2;
+        vsoff = f / CS_FP4_GROUP * (unsigned)F.vs_group + 8 * g;
     }
-#pragma unroll
-    for (int e = 0; e < 8; ++e) voff[e] = c * VF < hd ? (8 * g + e) * vts + c * VF / 2 : NOWHERE;
-    vsoff = c * VF < hd ? c * VF / CS_FP4_GROUP * vgs + 8 * g : NOWHERE;
 
     f32x4 oacc[MT][NT], lacc[NT];
     float m_run[NT];
@@ -144,59 +348,62 @@ __global__ __launch_bounds__(64 * F4N_WAVES, 2) void k_paged_fp4_narrow(cs_fp4_d
     const bf16x8 ones = (bf16x8){one, one, one, one, one, one, one, one};
     const float scale2 = A.scale2;
     const int kshift = 8 * (c & 3);
-    __syncthreads();
+    if (!QREG) __syncthreads();
 
     constexpr int STEP = 32 * F4N_WAVES;
-    // a lane holds the page of one of the wave's next 64 blocks
+    // A lane holds one of the wave's next 64 blocks: where in the pools it starts, so that a request costs the scalar
+    // unit no multiplications.  A block whose page does not exist is read from page 0 and masked; a lane that has none
+    // repeats the wave's last one.
     for (int seg0 = w_begin; seg0 < t_end; seg0 += 64 * STEP) {
         const int t_begin = seg0 + 32 * wave;
         const int n_all = t_begin < t_end ? min(64, (t_end - t_begin + STEP - 1) / STEP) : 0;
-        int page_l = -1;
+        if (n_all == 0) continue;
+        uint64_t at_k, at_v, at_ks, at_vs;
+        unsigned long long okay;
         {
-            const int64_t tb = (int64_t)t_begin + (int64_t)lane * STEP;
-            if (tb < t_end) page_l = tab[tb >> D.page_log2];
-            page_l = (unsigned)page_l < (unsigned)D.p.n_pages ? page_l : -1;
+            const int tb = t_begin + min(lane, n_all - 1) * STEP, slot = tb & (D.p.page_size - 1);
+            const int page = tab[tb >> D.page_log2];
+            const bool ok = (unsigned)page < (unsigned)D.p.n_pages;
+            const int64_t pg = ok ? page : 0;
+            okay = __ballot(ok);
+            at_k = (uint64_t)(Kh + pg * F.k_page + slot * F.k_token);
+            at_v = (uint64_t)(Vh + pg * F.v_page + slot * F.v_token);
+            at_ks = (uint64_t)(KSh + pg * F.ks_page + slot);
+            at_vs = (uint64_t)(VSh + pg * F.vs_page + slot);
         }
         auto at = [&](int i) { return t_begin + i * STEP; };
-        auto page_of = [&](int i) { return __builtin_amdgcn_readlane(page_l, i); };
-        auto codes = [&](const uint8_t* head, int64_t page_stride, unsigned ts, int i) {
-            const int t = at(i), page = i < n_all ? page_of(i) : -1, live = min(32, n_tok - t);
-            const unsigned bytes = page >= 0 && live > 0 ? (live - 1) * ts + row_bytes : 0;
-            return cs_rsrc(head + (page >= 0 ? page : 0) * page_stride + (int64_t)(t & (D.p.page_size - 1)) * ts, bytes);
-        };
-        auto scales = [&](const uint8_t* head, int64_t page_stride, unsigned gs, int i) {
-            const int t = at(i), page = i < n_all ? page_of(i) : -1;
-            return cs_rsrc(head + (page >= 0 ? page : 0) * page_stride + (t & (D.p.page_size - 1)), page >= 0 ? (n_groups - 1) * gs + 32 : 0);
+        auto from = [&](uint64_t a, int i) {
+            return cs_rsrc((const void*)((uint64_t)(unsigned)__builtin_amdgcn_readlane((int)(a >> 32), i & 63) << 32 |
+                                         (unsigned)__builtin_amdgcn_readlane((int)a, i & 63)), 0x80000000u);
         };
         auto ldk = [&](f4_keys<HD>& b, int i) {
-            const auto rs = codes(Kh, F.k_page, kts, i);
+            const auto p = from(at_k, i), f = from(at_ks, i);
 #pragma unroll
             for (int a = 0; a < 2; ++a)
 #pragma unroll
                 for (int h = 0; h < KB; ++h) {
                     if constexpr (HD == 64) {
-                        const auto x = __builtin_amdgcn_raw_buffer_load_b64(rs, koff[a][h], 0, 0);
+                        const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(p, koff[h], a * 4 * kts, 0));
                         b.k[a][h][0] = x[0];
                         b.k[a][h][1] = x[1];
-                    } else b.k[a][h] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rs, koff[a][h], 0, 0));
+                    } else b.k[a][h] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(p, koff[h], a * 4 * kts, 0));
                 }
-            const auto ss = scales(KSh, F.ks_page, kgs, i);
 #pragma unroll
-            for (int h = 0; h < KB; ++h) b.s[h] = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(ss, ksoff[h], 0, 0));
+            for (int h = 0; h < KB; ++h) b.s[h] = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(f, ksoff[h], 0, 0));
         };
         auto ldv = [&](f4_values<HD>& b, int i) {
-            const auto rs = codes(Vh, F.v_page, vts, i);
+            const auto p = from(at_v, i), f = from(at_vs, i);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                if constexpr (HD == 64) b.v[e][0] = __builtin_amdgcn_raw_buffer_load_b16(rs, voff[e], 0, 0);
-                else if constexpr (HD == 128) b.v[e][0] = __builtin_amdgcn_raw_buffer_load_b32(rs, voff[e], 0, 0);
+                if constexpr (HD == 64) b.v[e][0] = __builtin_amdgcn_raw_buffer_load_b16(p, voff, e * vts, 0);
+                else if constexpr (HD == 128) b.v[e][0] = __builtin_amdgcn_raw_buffer_load_b32(p, voff, e * vts, 0);
                 else {
-                    const auto x = __builtin_amdgcn_raw_buffer_load_b64(rs, voff[e], 0, 0);
+                    const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(p, voff, e * vts, 0));
                     b.v[e][0] = x[0];
                     b.v[e][VW - 1] = x[1];
                 }
             }
-            b.s = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(scales(VSh, F.vs_page, vgs, i), vsoff, 0, 0));
+            b.s = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(f, vsoff, 0, 0));
         };
         auto block = [&](f4_keys<HD>& kb, f4_values<HD>& vb, int i) {
             f32x4 sacc[2][NT];
@@ -214,7 +421,7 @@ __global__ __launch_bounds__(64 * F4N_WAVES, 2) void k_paged_fp4_narrow(cs_fp4_d
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                     for (int p = 0; p < NP; ++p) {
-                        const bf16x8 qb = *reinterpret_cast<const bf16x8*>(smem + p * QPLANE + (nt * 16 + c) * QROW + g * (HD / 2) + s * 16);
+                        const bf16x8 qb = QREG ? qreg[s] : *reinterpret_cast<const bf16x8*>(smem + p * QPLANE + (nt * 16 + c) * QROW + g * (HD / 2) + s * 16);
                         sacc[0][nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[0], qb, sacc[0][nt], 0, 0, 0);
                         sacc[1][nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[1], qb, sacc[1][nt], 0, 0, 0);
                     }
@@ -222,19 +429,20 @@ __global__ __launch_bounds__(64 * F4N_WAVES, 2) void k_paged_fp4_narrow(cs_fp4_d
             __builtin_amdgcn_sched_barrier(0);
             ldk(kb, i + AHEAD);
             __builtin_amdgcn_sched_barrier(0);
-            const int t0 = at(i), page = page_of(i);
-            if (t0 < open_lo || t0 + 32 > open_hi || page < 0) {
+            const int t0 = at(i);
+            const bool gone = !(okay >> i & 1);
+            if (t0 < open_lo || t0 + 32 > open_hi || gone) {
                 const int t = t0 + 8 * g;
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
-                        const bool sees = t + e <= q_last[nt] && t + e >= q_first[nt] && t + e < D.cap && page >= 0;
+                        const bool sees = t + e <= q_last[nt] && t + e >= q_last[nt] - back && t + e < cap && !gone;
                         sacc[e >> 2][nt][e & 3] = sees ? sacc[e >> 2][nt][e & 3] : -INFINITY;
                     }
-                // codes behind the last token have come as zeros, but scales and what has left every window may be
-                // anything, and 0 * anything must stay 0: with scale byte 0 every code is finite
-                const int e0 = min(max(w_first - t, 0), 8), e1 = min(max(n_tok - t, 0), 8);
+                // what lies behind the last token, in place of a page or before every window may have any scale, and 0 *
+                // anything must stay 0: with scale byte 0 every code is finite
+                const int e0 = min(max(w_first - t, 0), 8), e1 = gone ? 0 : min(max(n_tok - t, 0), 8);
                 const uint64_t from = e0 < 8 ? ~(uint64_t)0 << 8 * e0 : 0, to = e1 < 8 ? ~(~(uint64_t)0 << 8 * e1) : ~(uint64_t)0;
                 vb.s[0] &= (unsigned)(from & to);
                 vb.s[1] &= (unsigned)((from & to) >> 32);
@@ -335,7 +543,7 @@ __global__ __launch_bounds__(64 * F4N_WAVES, 2) void k_paged_fp4_narrow(cs_fp4_d
     for (int nt = 0; nt < NT; ++nt) l_run[nt] = lacc[nt][0];
 #pragma unroll
     for (int step = F4N_WAVES / 2; step > 0; step >>= 1) {
-        __syncthreads();             // (first: every wave is done with the query rows)
+        __syncthreads();             // (first: every wave is done with the query rows, and with the segment before)
         if (wave >= step && wave < 2 * step) {
             unsigned char* to = smem + (wave - step) * SLOT;
 #pragma unroll
@@ -361,16 +569,20 @@ __global__ __launch_bounds__(64 * F4N_WAVES, 2) void k_paged_fp4_narrow(cs_fp4_d
             }
         }
     }
-    if (wave) return;
+    if (wave) continue;
+    const f4_call& C2 = call();
+    const f4_shares& S = C2.S;
+    const int part = 2 * w + K.first, KVH = C2.F.d.p.n_kv_heads;
+    if (!K.whole && kvh == 0 && lane == 0) S.who[part] = make_int4(T.row0, T.n0, T.QR, K.number | K.of << 16);
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
         const int n = nt * 16 + c;
         if (n >= n_rows) continue;
-        const int i = (T.n0 + n) / A.G, h = kvh * A.G + T.n0 + n - i * A.G;
-        const int64_t r = T.row0 + i, row = ((int64_t)K.entry * KVH + kvh) * P.TR + n;
-        const bool whole = K.nsplit == 1;
+        const int i = (T.n0 + n) / C2.A.G, h = kvh * C2.A.G + T.n0 + n - i * C2.A.G;
+        const int64_t r = T.row0 + i, row = ((int64_t)part * KVH + kvh) * S.TR + n;
+        const bool whole = K.whole;
         const float inv = l_run[nt] > 0.f ? 1.0f / l_run[nt] : 0.f;           // a row that sees nothing: 0
-        if (g == 0 && !whole) P.pml[row] = make_float2(m_run[nt], l_run[nt]);
+        if (g == 0 && !whole) S.pml[row] = make_float2(m_run[nt], l_run[nt]);
 #pragma unroll
         for (int j = 0; j < 4; ++j)
 #pragma unroll
@@ -378,9 +590,71 @@ __global__ __launch_bounds__(64 * F4N_WAVES, 2) void k_paged_fp4_narrow(cs_fp4_d
                 const int d = (4 * g + j) * VF + u;
                 const f32x4 o = (f32x4){oacc[u][nt][j], oacc[u + 1][nt][j], oacc[u + 2][nt][j], oacc[u + 3][nt][j]};
                 if (d >= hd) continue;
-                if (whole) pa_store4((T_*)A.out + r * A.out_row + h * A.out_head + d, o * inv);
-                else pa_store4(P.po + row * hd + d, o);
+                if (whole) pa_store4((T_*)C2.A.out + r * C2.A.out_row + h * C2.A.out_head + d, o * inv);
+                else pa_store4(S.po + row * hd + d, o);
             }
+    }
+    }
+}
+
+// out[r][h] = sum_s 2^(m_s - M) O_s / sum_s 2^(m_s - M) l_s over the workgroups that have a part of a tile, which share
+// out its rows.  Parts are waited for, so a row's are spread over 2^teams_log2 teams of 2^lanes_log2 lanes, four of them a
+// team, as far as the workgroup has teams; a lane of a team has four of the hd features, and reads the (maximum,
+// sum) pairs of every lanes-th part, whose weights go round by shuffles.
+#define F4J_THREADS 256
+template <typename T_>
+__global__ __launch_bounds__(F4J_THREADS) void k_paged_fp4_join(cs_pages_dev D, pa_args A, f4_shares S, int lanes_log2) {
+    __shared__ f32x4 s_acc[F4J_THREADS];
+    __shared__ float s_l[F4J_THREADS];
+    const int KVH = D.p.n_kv_heads, kvh = blockIdx.x % KVH, w = blockIdx.x / KVH;
+    const int lanes = 1 << lanes_log2, sub = threadIdx.x & (lanes - 1), d = sub * 4, hd = D.p.head_dim;
+    for (int side = 0; side < 2; ++side) {
+        const int4 who = S.who[2 * w + side];
+        const int number = who.w & 0xffff, of = who.w >> 16, first = 2 * (w - number);
+        if (of <= 1) continue;
+        int teams_log2 = 0;
+        while (4 << teams_log2 < of && lanes << (teams_log2 + 1) <= F4J_THREADS) ++teams_log2;
+        const int teams = 1 << teams_log2, per = F4J_THREADS >> (lanes_log2 + teams_log2), team = threadIdx.x >> lanes_log2 & (teams - 1);
+        const int rows = min(S.TR, who.z - who.y);
+        for (int n0 = number * per; n0 < rows; n0 += of * per) {
+            const int n = n0 + (threadIdx.x >> (lanes_log2 + teams_log2));
+            // (part s: the first workgroup's beginning of the tile, then what the others have of one begun before)
+            auto at = [&](int s) { return ((int64_t)(first + (s ? 2 * s : 1)) * KVH + kvh) * S.TR + min(n, rows - 1); };
+            float M = -INFINITY;
+            for (int s = sub; s < of; s += lanes) M = fmaxf(M, S.pml[at(s)].x);
+            for (int o = lanes >> 1; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor(M, o, 64));
+            const float Ms = M == -INFINITY ? 0.f : M;
+            f32x4 acc = (f32x4){0.f, 0.f, 0.f, 0.f};
+            float l = 0.f;
+            for (int s0 = 0; s0 < of; s0 += lanes) {
+                float2 ml = make_float2(-INFINITY, 0.f);
+                if (s0 + sub < of) ml = S.pml[at(s0 + sub)];
+                const float f = __builtin_amdgcn_exp2f(ml.x - Ms), fl = f * ml.y;
+                const int ns = min(lanes, of - s0);
+                for (int s = team; s < ns; s += 4 * teams)
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) {
+                        // (past the last part: weight 0, its row once more; one that saw nothing has stored zeros)
+                        const int m = min(s + u * teams, ns - 1), from = (threadIdx.x & 63 & ~(lanes - 1)) + m;
+                        const float keep = s + u * teams < ns ? 1.f : 0.f;
+                        l += keep * __shfl(fl, from, 64);
+                        acc += keep * __shfl(f, from, 64) * *reinterpret_cast<const f32x4*>(S.po + at(s0 + m) * hd + min(d, hd - 4));
+                    }
+            }
+            if (teams > 1) {
+                __syncthreads();
+                s_acc[threadIdx.x] = acc;
+                s_l[threadIdx.x] = l;
+                __syncthreads();
+                if (team) continue;
+                for (int i = 1; i < teams; ++i) {
+                    acc += s_acc[threadIdx.x + i * lanes];
+                    l += s_l[threadIdx.x + i * lanes];
+                }
+            }
+            const int i = (who.y + n) / A.G, h = kvh * A.G + who.y + n - i * A.G;
+            if (n < rows && d < hd) pa_store4((T_*)A.out + (int64_t)(who.x + i) * A.out_row + h * A.out_head + d, acc * (l > 0.f ? 1.0f / l : 0.f));
+        }
     }
 }
 
@@ -568,8 +842,9 @@ __global__ __launch_bounds__(64 * F4W_WAVES) void k_paged_fp4_wide(cs_fp4_dev F,
     };
     typedef short s16x4 __attribute__((ext_vector_type(4)));
     typedef short s16x8 __attribute__((ext_vector_type(8)));
-    auto finish = [&](f32x4 (&sacc)[2][NT], const unsigned char* sp, int t0, bool masked, bool ok) {
-        if (masked) {
+    auto finish = [&](f32x4 (&sacc)[2][NT], const unsigned char* sp, int t0, auto masked_tag, bool ok) {
+        constexpr bool masked = decltype(masked_tag)::value;
+        if constexpr (masked) {
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -613,8 +888,13 @@ __global__ __launch_bounds__(64 * F4W_WAVES) void k_paged_fp4_wide(cs_fp4_dev F,
         __builtin_amdgcn_s_setprio(0);
     };
 
+    // The loop's bound and the positions come from a vector register that the compiler cannot see through: around branches
+    // it takes for uniform it splits the live ranges of the accumulators, copies and spills them.
+    int vzero;
+    asm volatile("v_mov_b32 %0, 0" : "=v"(vzero));
+    const int n_stages_v = n_stages + vzero;
     // positions that this wave's rows have: blocks outside what they see are not computed, blocks inside need no mask
-    const int p_lo = T.L + (T.n0 + wave * WROWS) / G, p_hi = T.L + min(T.rows - 1, (T.n0 + wave * WROWS + WROWS - 1) / G);
+    const int p_lo = T.L + (T.n0 + wave * WROWS) / G + vzero, p_hi = T.L + min(T.rows - 1, (T.n0 + wave * WROWS + WROWS - 1) / G) + vzero;
     const int w_lo = A.window ? p_lo - A.window + 1 : 0, w_hi = A.window ? p_hi - A.window + 1 : 0;
     const int p_end = T.n0 + wave * WROWS < T.QR ? min(p_hi, t_end - 1) : -1;       // a wave without rows multiplies nothing
     const int p_open = min(p_lo, D.cap - 1);
@@ -625,18 +905,22 @@ __global__ __launch_bounds__(64 * F4W_WAVES) void k_paged_fp4_wide(cs_fp4_dev F,
         request(1);
     }
     __syncthreads();
-    for (int i = 0; i < n_stages; ++i) {
-        if (i + 1 < n_stages) lay_down((i + 1) & 1);
+    const std::integral_constant<bool, false> plain_tag;
+    const std::integral_constant<bool, true> masked_tag;
+    for (int i = 0; i < n_stages_v; ++i) {
+        lay_down((i + 1) & 1);                                  // (past the last stage: what the last request has left, into a half that nobody reads)
         request(i + 2);
         const unsigned long long there_are = (i + 2) >> 5 == i >> 5 ? okay : old;
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
             const int t0 = w_begin + 64 * i + 32 * b;
-            if (t0 > p_end || t0 + 31 < w_lo) continue;
+            const int gone = 1 - ((int)(there_are >> ((2 * i + b) & 63)) & 1) + vzero;
             const unsigned char* sp = stage[i & 1] + b * HALF;
-            const bool ok = there_are >> ((2 * i + b) & 63) & 1;
-            scores(sp, sa);
-            finish(sa, sp, t0, t0 + 31 > p_open || t0 < w_hi || !ok, ok);
+            if ((t0 <= p_end) & (t0 + 31 >= w_lo)) {
+                scores(sp, sa);
+                if ((t0 + 31 > p_open) | (t0 < w_hi) | (gone != 0)) finish(sa, sp, t0, masked_tag, gone == 0);
+                else finish(sa, sp, t0, plain_tag, true);
+            }
         }
         __syncthreads();
     }
@@ -673,20 +957,41 @@ static int check_shape(const char* who, const cs_pages_fp4* p, int32_t q_dtype, 
     return CS_OK;
 }
 
+#define F4_SLOTS 512              // workgroups of the kernel of few rows that run at once
+#define F4_LEAST 8                // blocks below which a part of a tile costs more than it saves
+#define F4_JOIN 400               // what the merge costs, in tokens of a workgroup
 // How a call is cut: the same for the workspace and the launches.
 struct f4_cut {
     int hdt;
-    pa_part narrow, wide;
+    struct {
+        int nt, TR, qr_lo, qr_hi, tiles;      // tiles: an upper bound; 0: no launch
+        int W;                                // see f4_shares
+    } narrow;
+    pa_part wide;
     int64_t at_w, bytes;                      // where the second launch's partial results start; bytes in all
 };
+// Workgroups per KV head where all tokens are shared out: two for each compute unit in all, or as many rounds of them as
+// leave less than a tenth of the last one idle.
+static int f4_share_workgroups(int KVH) {
+    for (int slots = F4_SLOTS; slots < 8 * F4_SLOTS; slots *= 2)
+        if (slots / KVH * KVH * 10 >= slots * 9) return slots / KVH;
+    return std::max(1, 8 * F4_SLOTS / KVH);
+}
 #define F4N_MOST 48               // query rows up to which a stream takes the kernel of few rows
+// KV heads whose rows of codes lie in one cache line of 128 bytes
+static int f4_near(const cs_pages_fp4* p) {
+    int n = 1;
+    while (p->n_kv_heads % (2 * n) == 0 && 2 * n * p->k_head <= 128) n *= 2;
+    return n;
+}
 static f4_cut f4_make_cut(const cs_pages_fp4* p, bool f32, int H, bool has_row0, int R, int max_rows, int64_t max_len) {
     f4_cut c = {};
     const int KVH = p->n_kv_heads, G = H / KVH, B = p->batch, cap = p->table_pages * p->page_size;
     const int rows = has_row0 ? (max_rows ? std::min(max_rows, R) : R) : R / B;
     const int64_t qr = (int64_t)rows * G, all = (int64_t)R * G, len = max_len && max_len < cap ? max_len : cap;
     c.hdt = p->head_dim <= 64 ? 64 : p->head_dim <= 128 ? 128 : 256;
-    pa_part &N = c.narrow, &W = c.wide;
+    auto& N = c.narrow;
+    pa_part& W = c.wide;
     // Streams of up to n_most query rows per KV head go to the kernel of few rows.  Where a batch has
     // longer ones too, that kernel is made for single tokens: a tile of 48 rows would cost every one of
     // them three tiles' products.
@@ -707,7 +1012,14 @@ static f4_cut f4_make_cut(const cs_pages_fp4* p, bool f32, int H, bool has_row0,
         W.qr_hi = 0x7fffffff;
         W.tiles = (int)(has_row0 ? all / W.TR + std::min<int64_t>(B, all / (n_most + 1)) : B * cs_ceil_div(qr, W.TR));
     }
-    c.at_w = pa_ranges(N, len, B, KVH, p->head_dim, 512, 256, 512);
+    if (N.tiles) {
+        const int share = f4_share_workgroups(KVH);
+        const int64_t most = std::max<int64_t>(cs_ceil_div(len * N.tiles, share), 32 * F4_LEAST);
+        // (positions fit 31 bits whatever the row offsets say: no stream has more tiles than all rows together)
+        const bool fits = (int64_t)B * (all / N.TR + 1) * (cap / 32 + 1) < (int64_t)1 << 31;
+        if (fits && N.tiles < 2 * share && (2 * N.tiles <= share ? len - most : len / 2) > F4_JOIN) N.W = share;
+    }
+    c.at_w = N.W ? cs_round_up((int64_t)2 * N.W * KVH * N.TR * (p->head_dim * 4 + 8), 16) + (int64_t)2 * N.W * 16 : 0;
     c.bytes = c.at_w + pa_ranges(W, len, B, KVH, p->head_dim, 256, 128, 192);
     return c;
 }
@@ -723,8 +1035,8 @@ extern "C" int64_t cs_paged_fp4_attention_workspace(const cs_pages_fp4* p, int32
 }
 
 template <int HD, int NT, int NP>
-static int f4n_launch(const cs_fp4_dev& F, const pa_args& A, const pa_plan& P, dim3 grid, hipStream_t s) {
-    k_paged_fp4_narrow<HD, NT, NP><<<grid, 64 * F4N_WAVES, 0, s>>>(F, A, P);
+static int f4n_launch(const cs_fp4_dev& F, const pa_args& A, const f4_shares& S, dim3 grid, hipStream_t s) {
+    k_paged_fp4_narrow<HD, NT, NP><<<grid, 64 * F4N_WAVES, 0, s>>>(f4_call{F, A, S});
     return cs_launch_ok("k_paged_fp4_narrow");
 }
 template <int HD, int NT, int NP>
@@ -755,7 +1067,7 @@ extern "C" int cs_paged_fp4_attention(const cs_pages_fp4* p, int32_t q_dtype, co
     CS_REQUIRE(c.bytes <= 0 || (workspace && workspace_bytes >= c.bytes), CS_E_CAPACITY, "%s: the workspace has %lld bytes, %lld are needed",
                who, (long long)(workspace ? workspace_bytes : 0), (long long)c.bytes);
     CS_REQUIRE(((uintptr_t)workspace & 15) == 0, CS_E_ARG, "%s: the workspace is not aligned to 16 bytes", who);
-    const int64_t grid_n = (int64_t)c.narrow.entries * p->n_kv_heads, grid_w = (int64_t)c.wide.entries * p->n_kv_heads;
+    const int64_t grid_n = (int64_t)(c.narrow.W ? c.narrow.W : c.narrow.tiles) * p->n_kv_heads, grid_w = (int64_t)c.wide.entries * p->n_kv_heads;
     CS_REQUIRE(grid_n <= 0x7fffffff && grid_w <= 0x7fffffff, CS_E_UNSUPPORTED, "%s: too many tiles", who);
     int rc = CS_E_UNSUPPORTED;
     if (grid_w) {
@@ -768,13 +1080,23 @@ extern "C" int cs_paged_fp4_attention(const cs_pages_fp4* p, int32_t q_dtype, co
         CS_TRY(pm_launch(F.d, A, P, n, s));
     }
     if (grid_n) {
-        const pa_plan P = pa_plan_of(c.narrow, (char*)workspace, p->n_kv_heads, p->head_dim);
+        const auto& N = c.narrow;
+        const int64_t rows = (int64_t)2 * N.W * p->n_kv_heads * N.TR;
+        float* po = (float*)workspace;
+        const f4_shares S = {N.TR, N.qr_lo, N.qr_hi, N.W, F4_LEAST, N.W ? (N.W + 63) / 64 : N.tiles, f4_near(p), po, (float2*)(po + rows * p->head_dim),
+                             (int4*)((char*)workspace + cs_round_up(rows * (p->head_dim * 4 + 8), 16))};
         const dim3 n = cs_paged_grid(grid_n);
-#define FN(HD_, NT_) if (c.hdt == HD_ && c.narrow.nt == NT_) rc = f32 ? f4n_launch<HD_, NT_, 3>(F, A, P, n, s) : f4n_launch<HD_, NT_, 1>(F, A, P, n, s)
+#define FN(HD_, NT_) if (c.hdt == HD_ && N.nt == NT_) rc = f32 ? f4n_launch<HD_, NT_, 3>(F, A, S, n, s) : f4n_launch<HD_, NT_, 1>(F, A, S, n, s)
         FN(64, 1); FN(64, 2); FN(64, 3); FN(128, 1); FN(128, 2); FN(128, 3); FN(256, 1);
 #undef FN
         CS_TRY(rc);
-        CS_TRY(pm_launch(F.d, A, P, n, s));
+        if (N.W) {
+            int lanes = 0;
+            while (4 << lanes < p->head_dim) ++lanes;
+            if (f32) k_paged_fp4_join<float><<<n, F4J_THREADS, 0, s>>>(F.d, A, S, lanes);
+            else k_paged_fp4_join<bf16_t><<<n, F4J_THREADS, 0, s>>>(F.d, A, S, lanes);
+            CS_TRY(cs_launch_ok("k_paged_fp4_join"));
+        }
     }
     return CS_OK;
 }
