@@ -672,6 +672,7 @@ __global__ __launch_bounds__(64 * F4W_WAVES) void k_paged_fp4_wide(cs_fp4_dev F,
     typedef f4_qtype<NP> T_;
     constexpr int KS = HD / 32, MT = HD / 16;
     constexpr int WROWS = 16 * NT, TR = F4W_WAVES * WROWS;
+    constexpr int NB = HD <= 128 || NP == 1 ? 2 : 1;             // blocks of 32 tokens that go through the softmax together
     constexpr int DW = HD / 64;                                 // dwords of codes of a lane's piece of a row
     constexpr int HALF = 2 * KS * 1024, V_AT = 2 * HALF, STAGE_BYTES = 2 * V_AT;         // keys of a block; of a stage
     __shared__ __attribute__((aligned(16))) unsigned char stage[2][STAGE_BYTES];
@@ -718,31 +719,34 @@ __global__ __launch_bounds__(64 * F4W_WAVES) void k_paged_fp4_wide(cs_fp4_dev F,
     const uint8_t *Kh = F.k + kvh * F.k_head, *Vh = F.v + kvh * F.v_head, *KSh = F.ks + kvh * F.ks_head, *VSh = F.vs + kvh * F.vs_head;
     const int32_t* tab = D.p.table + T.b * D.p.table_stride;
 
-    // A lane has the page of one of the next 64 blocks of 32 tokens.
-    int page_l = -1;
+    // A lane has one of the next 64 blocks of 32 tokens: where in the pools it starts, so that a request costs the scalar
+    // unit no multiplications.  A block whose page does not exist is read from page 0 and laid down with scale byte 0, as are
+    // tokens behind the last one or before every window, whose scales may be anything: their codes are finite then.
+    uint64_t at_k = 0, at_v = 0, at_ks = 0, at_vs = 0;
     unsigned long long okay = 0, old = 0;                      // blocks that exist, of these and of the 64 before
     auto pages = [&](int blk0) {
         const int64_t t = (int64_t)w_begin + 32 * ((int64_t)blk0 + lane);
-        page_l = t < t_end ? tab[t >> D.page_log2] : -1;
-        const bool ok = (unsigned)page_l < (unsigned)D.p.n_pages;
+        const int page = t < t_end ? tab[t >> D.page_log2] : -1, slot = (int)t & (D.p.page_size - 32);
+        const bool ok = (unsigned)page < (unsigned)D.p.n_pages;
+        const int64_t pg = ok ? page : 0;
         old = okay;
         okay = __ballot(ok);
-        page_l = ok ? page_l : -1;
+        at_k = (uint64_t)(Kh + pg * F.k_page + slot * F.k_token);
+        at_v = (uint64_t)(Vh + pg * F.v_page + slot * F.v_token);
+        at_ks = (uint64_t)(KSh + pg * F.ks_page + slot);
+        at_vs = (uint64_t)(VSh + pg * F.vs_page + slot);
     };
     unsigned kc[DW], vc[DW], ksc, vsc;
     auto request = [&](int i) {
         if ((2 * i & 63) == 0) pages(2 * i);
-        const int t0 = w_begin + 64 * i + 32 * (wave >> 2);
-        const int page = __builtin_amdgcn_readlane(page_l, (2 * i + (wave >> 2)) & 63), slot = t0 & (D.p.page_size - 1);
-        const int64_t pg = page >= 0 ? page : 0;
-        const int live = min(32, n_lim - t0);
-        const bool some = page >= 0 && live > 0;
-        const auto rk = cs_rsrc(Kh + pg * F.k_page + (int64_t)slot * kts, some ? (live - 1) * kts + hd / 2 : 0);
-        const auto rv = cs_rsrc(Vh + pg * F.v_page + (int64_t)slot * vts, some ? (live - 1) * vts + hd / 2 : 0);
-        const auto rks = cs_rsrc(KSh + pg * F.ks_page + slot, some ? (hd / CS_FP4_GROUP - 1) * kgs + 32 : 0);
-        const auto rvs = cs_rsrc(VSh + pg * F.vs_page + slot, some ? (hd / CS_FP4_GROUP - 1) * vgs + 32 : 0);
-        const int t = t0 + (tok & 31);
-        const bool mine = t < n_lim && t >= w_first;           // (dead scales may be anything)
+        const int l = (2 * i + (wave >> 2)) & 63;
+        auto from = [&](uint64_t a) {
+            return cs_rsrc((const void*)((uint64_t)(unsigned)__builtin_amdgcn_readlane((int)(a >> 32), l) << 32 |
+                                         (unsigned)__builtin_amdgcn_readlane((int)a, l)), NOWHERE);
+        };
+        const auto rk = from(at_k), rv = from(at_v), rks = from(at_ks), rvs = from(at_vs);
+        const int t = w_begin + 64 * i + tok;
+        const bool mine = t < n_lim && t >= w_first && (okay >> l & 1);
         if constexpr (DW == 1) {
             kc[0] = __builtin_amdgcn_raw_buffer_load_b32(rk, koff, 0, 0);
             vc[0] = __builtin_amdgcn_raw_buffer_load_b32(rv, voff, 0, 0);
@@ -787,31 +791,34 @@ __global__ __launch_bounds__(64 * F4W_WAVES) void k_paged_fp4_wide(cs_fp4_dev F,
     const bf16_t one = (bf16_t)1.0f;
     const bf16x8 ones = (bf16x8){one, one, one, one, one, one, one, one};
 
-    auto scores = [&](const unsigned char* sp, f32x4 (&sacc)[2][NT]) {
+    auto scores = [&](const unsigned char* sp, f32x4 (&sacc)[2 * NB][NT]) {
         __builtin_amdgcn_s_setprio(1);
 #pragma unroll
         for (int s = 0; s < KS; ++s) {
-            const bf16x8 k0 = *reinterpret_cast<const bf16x8*>(sp + (s * 64 + lane) * 16);
-            const bf16x8 k1 = *reinterpret_cast<const bf16x8*>(sp + ((KS + s) * 64 + lane) * 16);
             const f32x4 zero4 = (f32x4){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
+            for (int a = 0; a < 2 * NB; ++a) {
+                const bf16x8 kf = *reinterpret_cast<const bf16x8*>(sp + (a >> 1) * HALF + (((a & 1) * KS + s) * 64 + lane) * 16);
 #pragma unroll
-                for (int p = 0; p < NP; ++p) {
-                    sacc[0][nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k0, qreg[nt][s][p], s + p == 0 ? zero4 : sacc[0][nt], 0, 0, 0);
-                    sacc[1][nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k1, qreg[nt][s][p], s + p == 0 ? zero4 : sacc[1][nt], 0, 0, 0);
-                }
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int p = 0; p < NP; ++p)
+                        sacc[a][nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qreg[nt][s][p], s + p == 0 ? zero4 : sacc[a][nt], 0, 0, 0);
+            }
         }
         __builtin_amdgcn_s_setprio(0);
     };
     // the running maximum of the tile rows moves (and O is rescaled) only when it is left behind by 2^8
-    auto reference = [&](const f32x4 (&sacc)[2][NT], bool masked) {
+    auto reference = [&](const f32x4 (&sacc)[2 * NB][NT], bool masked) {
         if (!masked) {
             bool over = false;
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
-                const float lm = fmaxf(fmaxf(fmaxf(sacc[0][nt][0], sacc[0][nt][1]), fmaxf(sacc[0][nt][2], sacc[0][nt][3])),
-                                       fmaxf(fmaxf(sacc[1][nt][0], sacc[1][nt][1]), fmaxf(sacc[1][nt][2], sacc[1][nt][3])));
+                float lm = -INFINITY;
+#pragma unroll
+                for (int a = 0; a < 2 * NB; ++a)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) lm = fmaxf(lm, sacc[a][nt][j]);
                 over |= !(lm <= thr[nt]);
             }
             if (!__any(over)) return;
@@ -820,9 +827,11 @@ __global__ __launch_bounds__(64 * F4W_WAVES) void k_paged_fp4_wide(cs_fp4_dev F,
         float alpha[NT];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-            float mx = fmaxf(fmaxf(sacc[0][nt][0], sacc[0][nt][1]), sacc[0][nt][2]);
-            mx = fmaxf(fmaxf(mx, sacc[0][nt][3]), sacc[1][nt][0]);
-            mx = fmaxf(fmaxf(mx, sacc[1][nt][1]), fmaxf(sacc[1][nt][2], sacc[1][nt][3]));
+            float mx = -INFINITY;
+#pragma unroll
+            for (int a = 0; a < 2 * NB; ++a)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) mx = fmaxf(mx, sacc[a][nt][j]);
             mx = fa_row4_max(mx) * scale2;
             const bool up = mx > m_run[nt] + FA_RESCALE_LOG2;
             const float m_new = up ? mx : m_run[nt];
@@ -842,49 +851,55 @@ __global__ __launch_bounds__(64 * F4W_WAVES) void k_paged_fp4_wide(cs_fp4_dev F,
     };
     typedef short s16x4 __attribute__((ext_vector_type(4)));
     typedef short s16x8 __attribute__((ext_vector_type(8)));
-    auto finish = [&](f32x4 (&sacc)[2][NT], const unsigned char* sp, int t0, auto masked_tag, bool ok) {
+    auto finish = [&](f32x4 (&sacc)[2 * NB][NT], const unsigned char* sp, int t0, auto masked_tag, int ok) {
         constexpr bool masked = decltype(masked_tag)::value;
         if constexpr (masked) {
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                for (int a = 0; a < 2; ++a)
+                for (int a = 0; a < 2 * NB; ++a)
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
                         const int t = t0 + 16 * a + 4 * g + j;
-                        const bool sees = t <= q_last[nt] && (A.window == 0 || t > q_last[nt] - A.window) && t < n_lim && ok;
+                        const bool sees = t <= q_last[nt] && (A.window == 0 || t > q_last[nt] - A.window) && t < n_lim && (ok >> (a >> 1) & 1);
                         sacc[a][nt][j] = sees ? sacc[a][nt][j] : -INFINITY;
                     }
         }
         reference(sacc, masked);
-        bf16x8 pb[NT][NP];
+        bf16x8 pb[NB][NT][NP];
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-            const float m_safe = m_run[nt] == -INFINITY ? 0.f : m_run[nt];
-            float x[8];
+        for (int b = 0; b < NB; ++b)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = __builtin_amdgcn_exp2f(fmaf(sacc[e >> 2][nt][e & 3], scale2, -m_safe));
-            f4_split8(x, pb[nt]);
-        }
+            for (int nt = 0; nt < NT; ++nt) {
+                const float m_safe = m_run[nt] == -INFINITY ? 0.f : m_run[nt];
+                float x[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[e] = __builtin_amdgcn_exp2f(fmaf(sacc[2 * b + (e >> 2)][nt][e & 3], scale2, -m_safe));
+                f4_split8(x, pb[b][nt]);
+            }
         __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt) {
-            s16x4 h[2];
+        for (int b = 0; b < NB; ++b)
 #pragma unroll
-            for (int a = 0; a < 2; ++a) {
-                const unsigned char* p = sp + V_AT + (a * KS + (mt >> 1)) * 1024 + (mt & 1) * 512 + lane * 8;
-                h[a] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(__attribute__((address_space(3))) unsigned char*)p);
+            for (int mt = 0; mt < MT; ++mt) {
+                s16x4 h[2];
+#pragma unroll
+                for (int a = 0; a < 2; ++a) {
+                    const unsigned char* p = sp + V_AT + b * HALF + (a * KS + (mt >> 1)) * 1024 + (mt & 1) * 512 + lane * 8;
+                    h[a] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(__attribute__((address_space(3))) unsigned char*)p);
+                }
+                const bf16x8 vf = __builtin_bit_cast(bf16x8, (s16x8){h[0][0], h[0][1], h[0][2], h[0][3], h[1][0], h[1][1], h[1][2], h[1][3]});
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int p = 0; p < NP; ++p) oacc[mt][nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pb[b][nt][p], oacc[mt][nt], 0, 0, 0);
             }
-            const bf16x8 vf = __builtin_bit_cast(bf16x8, (s16x8){h[0][0], h[0][1], h[0][2], h[0][3], h[1][0], h[1][1], h[1][2], h[1][3]});
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                for (int p = 0; p < NP; ++p) oacc[mt][nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pb[nt][p], oacc[mt][nt], 0, 0, 0);
-        }
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-            for (int p = 0; p < NP; ++p) lacc[nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pb[nt][p], lacc[nt], 0, 0, 0);
+                for (int p = 0; p < NP; ++p) lacc[nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pb[b][nt][p], lacc[nt], 0, 0, 0);
         __builtin_amdgcn_s_setprio(0);
     };
 
@@ -898,7 +913,7 @@ __global__ __launch_bounds__(64 * F4W_WAVES) void k_paged_fp4_wide(cs_fp4_dev F,
     const int w_lo = A.window ? p_lo - A.window + 1 : 0, w_hi = A.window ? p_hi - A.window + 1 : 0;
     const int p_end = T.n0 + wave * WROWS < T.QR ? min(p_hi, t_end - 1) : -1;       // a wave without rows multiplies nothing
     const int p_open = min(p_lo, D.cap - 1);
-    f32x4 sa[2][NT];
+    f32x4 sa[2 * NB][NT];
     if (n_stages > 0) {
         request(0);
         lay_down(0);
@@ -908,18 +923,21 @@ __global__ __launch_bounds__(64 * F4W_WAVES) void k_paged_fp4_wide(cs_fp4_dev F,
     const std::integral_constant<bool, false> plain_tag;
     const std::integral_constant<bool, true> masked_tag;
     for (int i = 0; i < n_stages_v; ++i) {
-        lay_down((i + 1) & 1);                                  // (past the last stage: what the last request has left, into a half that nobody reads)
-        request(i + 2);
-        const unsigned long long there_are = (i + 2) >> 5 == i >> 5 ? okay : old;
+        const unsigned long long there_are = (i + 1) >> 5 == i >> 5 ? okay : old;
+        const int exist = (int)(there_are >> ((2 * i) & 63)) & 3;
 #pragma unroll
-        for (int b = 0; b < 2; ++b) {
-            const int t0 = w_begin + 64 * i + 32 * b;
-            const int gone = 1 - ((int)(there_are >> ((2 * i + b) & 63)) & 1) + vzero;
+        for (int b = 0; b < 2; b += NB) {
+            const int t0 = w_begin + 64 * i + 32 * b, ok = NB == 2 ? exist : exist >> b & 1;
+            const int gone = ((2 * NB - 1) & ~ok) + vzero;
             const unsigned char* sp = stage[i & 1] + b * HALF;
-            if ((t0 <= p_end) & (t0 + 31 >= w_lo)) {
+            if (b + NB == 2) {                                  // (past the last stage: what the last request has left, into a half that nobody reads)
+                lay_down((i + 1) & 1);
+                request(i + 2);
+            }
+            if ((t0 <= p_end) & (t0 + 32 * NB - 1 >= w_lo)) {
                 scores(sp, sa);
-                if ((t0 + 31 > p_open) | (t0 < w_hi) | (gone != 0)) finish(sa, sp, t0, masked_tag, gone == 0);
-                else finish(sa, sp, t0, plain_tag, true);
+                if ((t0 + 32 * NB - 1 > p_open) | (t0 < w_hi) | (gone != 0)) finish(sa, sp, t0, masked_tag, ok);
+                else finish(sa, sp, t0, plain_tag, ok);
             }
         }
         __syncthreads();
