@@ -236,7 +236,9 @@ __global__ __launch_bounds__(64 * F4N_WAVES, 2) void k_paged_fp4_narrow(f4_call 
     constexpr int KB = HD == 256 ? 2 : 1;                       // 32-feature pieces of a lane's key row (HD 64: half of one)
     constexpr int VW = HD == 256 ? 2 : 1;                       // dwords of a lane's value row (HD 64: half of one)
     constexpr bool QREG = NT == 1 && NP == 1;                   // the query fragments stay in registers, else they are read from LDS
-    constexpr int AHEAD = HD == 256 || NT > 1 || NP > 1 ? 2 : 4;         // blocks in flight
+    // blocks in flight (with one more: 48 rows 57 us for 53, 16 rows of 256 features spill; with one less: 16 rows of 256
+    // features 43 -> 85 us, others no change)
+    constexpr int AHEAD = NT > 1 ? 1 : HD == 256 || NP > 1 ? 2 : 3;
     constexpr int ROWS = 16 * NT, QROW = HD * 2 + 16, QPLANE = ROWS * QROW;
     constexpr int SLOT = NT * (MT * 1024 + 512);                // a wave's (O, maximum, sum)
     constexpr int LDS_BYTES = 2 * SLOT > NP * QPLANE ? 2 * SLOT : NP * QPLANE;
@@ -336,17 +338,17 @@ __global__ __launch_bounds__(64 * F4N_WAVES, 2) void k_paged_fp4_narrow(f4_call 
     }
 
     f32x4 oacc[MT][NT], lacc[NT];
-    float m_run[NT];
+    float m_run[NT], thr[NT];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
-        m_run[nt] = -INFINITY;
+        m_run[nt] = thr[nt] = -INFINITY;
         lacc[nt] = (f32x4){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) oacc[mt][nt] = (f32x4){0.f, 0.f, 0.f, 0.f};
     }
     const bf16_t one = (bf16_t)1.0f;
     const bf16x8 ones = (bf16x8){one, one, one, one, one, one, one, one};
-    const float scale2 = A.scale2;
+    const float scale2 = A.scale2, inv_scale2 = 1.0f / A.scale2;
     const int kshift = 8 * (c & 3);
     if (!QREG) __syncthreads();
 
@@ -422,16 +424,16 @@ __global__ __launch_bounds__(64 * F4N_WAVES, 2) void k_paged_fp4_narrow(f4_call 
 #pragma unroll
                     for (int p = 0; p < NP; ++p) {
                         const bf16x8 qb = QREG ? qreg[s] : *reinterpret_cast<const bf16x8*>(smem + p * QPLANE + (nt * 16 + c) * QROW + g * (HD / 2) + s * 16);
-                        sacc[0][nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[0], qb, sacc[0][nt], 0, 0, 0);
-                        sacc[1][nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[1], qb, sacc[1][nt], 0, 0, 0);
+#pragma unroll
+                        for (int a = 0; a < 2; ++a) sacc[a][nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[a], qb, sacc[a][nt], 0, 0, 0);
                     }
             }
             __builtin_amdgcn_sched_barrier(0);
             ldk(kb, i + AHEAD);
             __builtin_amdgcn_sched_barrier(0);
             const int t0 = at(i);
-            const bool gone = !(okay >> i & 1);
-            if (t0 < open_lo || t0 + 32 > open_hi || gone) {
+            const bool gone = !(okay >> i & 1), masked = t0 < open_lo || t0 + 32 > open_hi || gone;
+            if (masked) {
                 const int t = t0 + 8 * g;
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
@@ -447,36 +449,52 @@ __global__ __launch_bounds__(64 * F4N_WAVES, 2) void k_paged_fp4_narrow(f4_call 
                 vb.s[0] &= (unsigned)(from & to);
                 vb.s[1] &= (unsigned)((from & to) >> 32);
             }
-            bool moved = false;
-            float alpha[NT];
+            // the reference maximum of a row moves (and O is rescaled) only when it is left behind by 2^8
+            bool over = masked;
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                float lm = -INFINITY;
+#pragma unroll
+                for (int a = 0; a < 2; ++a)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) lm = fmaxf(lm, sacc[a][nt][j]);
+                over |= !(lm <= thr[nt]);
+            }
+            if (__any(over)) {
+                bool moved = false;
+                float alpha[NT];
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+                    float mx = -INFINITY;
+#pragma unroll
+                    for (int a = 0; a < 2; ++a)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) mx = fmaxf(mx, sacc[a][nt][j]);
+                    mx = fa_row4_max(mx) * scale2;
+                    const bool up = mx > m_run[nt] + FA_RESCALE_LOG2;
+                    const float m_new = up ? mx : m_run[nt];
+                    alpha[nt] = up ? __builtin_amdgcn_exp2f(m_run[nt] - (m_new == -INFINITY ? 0.f : m_new)) : 1.0f;
+                    moved |= up;
+                    m_run[nt] = m_new;
+                    thr[nt] = m_new == -INFINITY ? -INFINITY : (m_new + FA_RESCALE_LOG2) * inv_scale2;
+                }
+                if (__any(moved)) {
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) {
+                        lacc[nt] *= alpha[nt];
+#pragma unroll
+                        for (int mt = 0; mt < MT; ++mt) oacc[mt][nt] *= alpha[nt];
+                    }
+                }
+            }
             bf16x8 pb[NT][NP];
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
+                const float m_safe = m_run[nt] == -INFINITY ? 0.f : m_run[nt];
                 float sv[8];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) sv[e] = sacc[e >> 2][nt][e & 3];
-                float mx = fmaxf(fmaxf(sv[0], sv[1]), sv[2]);
-                mx = fmaxf(fmaxf(mx, sv[3]), sv[4]);
-                mx = fmaxf(fmaxf(mx, sv[5]), fmaxf(sv[6], sv[7]));
-                mx = fa_row4_max(mx) * scale2;
-                // the reference maximum follows the true one only when it is left behind by 2^8
-                const bool up = mx > m_run[nt] + FA_RESCALE_LOG2;
-                const float m_new = up ? mx : m_run[nt];
-                const float m_safe = m_new == -INFINITY ? 0.f : m_new;
-                alpha[nt] = up ? __builtin_amdgcn_exp2f(m_run[nt] - m_safe) : 1.0f;
-                moved |= up;
-                m_run[nt] = m_new;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) sv[e] = __builtin_amdgcn_exp2f(fmaf(sv[e], scale2, -m_safe));
+                for (int e = 0; e < 8; ++e) sv[e] = __builtin_amdgcn_exp2f(fmaf(sacc[e >> 2][nt][e & 3], scale2, -m_safe));
                 f4_split8(sv, pb[nt]);
-            }
-            if (__any(moved)) {
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt) {
-                    lacc[nt] *= alpha[nt];
-#pragma unroll
-                    for (int mt = 0; mt < MT; ++mt) oacc[mt][nt] *= alpha[nt];
-                }
             }
             // (the row sum is that of the rounded probabilities)
 #pragma unroll
