@@ -46,18 +46,22 @@ __device__ __forceinline__ void f4_split(const float* p, bf16x8 (&o)[3]) {
 // ---- which tiles and tokens a workgroup of the kernel of few rows has ----------------------------------------
 // The G * rows query rows of a stream's KV head (row n: block row n / G, head n % G of the group) are cut into
 // tiles of TR; streams with qr_lo < G * rows <= qr_hi take part.  W workgroups per KV head are as many as run at
-// once, and all tokens are cut among them on the device, from the lengths, by every workgroup for itself:
-//   pieces: a workgroup has one piece of one tile, at most `piece` blocks of 32 tokens, the smallest size with no more
-//           than W pieces; each lane tries another one;
+// once, and the tokens are cut among them on the device, from the lengths, by every workgroup for itself:
+//   pieces: a workgroup has one piece of one tile, at most `piece` blocks of 32 tokens, with no more than W pieces
+//           in all; each lane prices another size, whole tiles among them;
 //   shares: the blocks of all tiles are laid end to end and each workgroup takes as many of them: the end of one tile,
 //           whole ones, the beginning of another.  For streams of different lengths, where pieces are uneven, and
 //           for more tiles than workgroups.
-// What a workgroup has of a tile that it does not have alone is a partial result, at most two of them, which a merge
-// joins.  (W 0: a workgroup each tile, no partial results.)
+// A cut's price, in blocks of a workgroup that runs alone, is made of its longest workgroup's and of what all tokens cost
+// the chip (`bound` times their blocks), as the cube root of their cubes' sum: the larger one, and some more where both
+// are alike, for a workgroup is slower among others; and the merge's if there is one.  What a workgroup has of a tile that
+// it does not have alone is a partial result, at most two of them, which the merge joins.  (W 0: a workgroup each
+// tile, no partial results.)
 struct f4_shares {
     int TR, qr_lo, qr_hi;
     int W, least;             // workgroups per KV head; fewest blocks of a piece or a share
     int step;                 // distance of the numbers of pieces tried
+    float bound, join;        // what a block of all tokens costs the chip, and a merge, in blocks of a workgroup
     int near;                 // neighbouring KV heads that run on one die
     float* po;                // [2 W][KVH][TR][hd] partial outputs; 2w: of a tile that an earlier workgroup has begun, 2w + 1: of one that w begins
     float2* pml;              // [2 W][KVH][TR] their (maximum, sum)
@@ -68,6 +72,9 @@ struct f4_call {
     pa_args A;
     f4_shares S;
 };
+__device__ __forceinline__ float f4_price(float longest, float chip) {
+    return __builtin_amdgcn_exp2f(__builtin_amdgcn_logf(longest * longest * longest + chip * chip * chip) * (1.0f / 3));
+}
 struct f4_segment {
     int b, n0;                // stream, first query row
     int off, n;               // first block of the tile's, blocks (W 0: all of them)
@@ -147,12 +154,16 @@ __device__ __forceinline__ f4_walk f4_start(const cs_pages_dev& D, int G, int wi
             const int blocks = __builtin_amdgcn_readlane(k.e.y, i), q = (int)((float)blocks * inv), r = blocks - q * cut;
             count += __builtin_amdgcn_readlane(k.e.x, i) * (q + (r > 0) + (r > cut));             // (q is off by one at most)
         }
-        const int best = __builtin_amdgcn_readlane(pa_wave_reduce(count <= S.W ? cut : 0x7fffffff, 0x7fffffff, [](int a, int b) { return min(a, b); }), 63);
-        if (best <= k.share + F4_SEGMENT) {
-            k.piece = best;
+        const float least = (float)(all - F4_SEGMENT * tiles) * S.bound;
+        const float cost = f4_price((float)cut, least) + (cut < longest ? S.join + (float)n * 0.1f : 0.f);
+        // (costs are positive: their bits are ordered as they are)
+        const int bits = count <= S.W ? __float_as_int(cost) : 0x7f800000;
+        const int best = __builtin_amdgcn_readlane(pa_wave_reduce(bits, 0x7f800000, [](int a, int b) { return min(a, b); }), 63);
+        if (__int_as_float(best) <= f4_price((float)(k.share + F4_SEGMENT), least) + S.join) {
+            k.piece = __builtin_amdgcn_readlane(cut, __ffsll(__ballot(bits == best)) - 1);
             k.share = 1;
             k.start = 0;
-            k.units = (k.e.y + best - 1) / best;
+            k.units = (k.e.y + k.piece - 1) / k.piece;
             k.upto = pa_wave_scan(k.e.x * k.units);
             all = __builtin_amdgcn_readlane(k.upto, 63);
         }
@@ -995,13 +1006,13 @@ static int check_shape(const char* who, const cs_pages_fp4* p, int32_t q_dtype, 
 
 #define F4_SLOTS 512              // workgroups of the kernel of few rows that run at once
 #define F4_LEAST 8                // blocks below which a part of a tile costs more than it saves
-#define F4_JOIN 400               // what the merge costs, in tokens of a workgroup
 // How a call is cut: the same for the workspace and the launches.
 struct f4_cut {
     int hdt;
     struct {
         int nt, TR, qr_lo, qr_hi, tiles;      // tiles: an upper bound; 0: no launch
         int W;                                // see f4_shares
+        float bound, join;
     } narrow;
     pa_part wide;
     int64_t at_w, bytes;                      // where the second launch's partial results start; bytes in all
@@ -1049,11 +1060,22 @@ static f4_cut f4_make_cut(const cs_pages_fp4* p, bool f32, int H, bool has_row0,
         W.tiles = (int)(has_row0 ? all / W.TR + std::min<int64_t>(B, all / (n_most + 1)) : B * cs_ceil_div(qr, W.TR));
     }
     if (N.tiles) {
-        const int share = f4_share_workgroups(KVH);
-        const int64_t most = std::max<int64_t>(cs_ceil_div(len * N.tiles, share), 32 * F4_LEAST);
+        // What a block of 32 tokens takes a workgroup that runs alone (captured calls: 4.3, 5.2 and 6.6 ns a token of 64, 128
+        // and 256 features, 16 bfloat16 rows; 8.6 with 48 rows, 8.3 and 19.2 with 16 and 48 float32 rows), and what it costs the
+        // chip: its bytes at 5 TB/s, or one of the 256 compute units for as long.
+        const float alone = 0.032f * (3.6f + 0.0125f * c.hdt) * (0.7f + 0.32f * N.nt * (f32 ? 3 : 1));
+        const float chip = std::max(0.00087f * p->head_dim / 128, alone / 256);
+        N.bound = KVH * chip / alone;
+        N.join = 5.0f / alone;                                   // (a merge: 5 us; one that finds nothing to do: 3)
+        const int share = f4_share_workgroups(KVH), tiles = N.tiles;
+        auto price = [&](float longest, float all) { return std::cbrt(longest * longest * longest + all * all * all); };
+        const float blocks = cs_ceil_div(len, 32), chip_all = blocks * tiles * N.bound, whole = price(blocks, chip_all);
+        const float cut = price(std::max(blocks * tiles / share, (float)F4_LEAST), chip_all) + N.join;
         // (positions fit 31 bits whatever the row offsets say: no stream has more tiles than all rows together)
         const bool fits = (int64_t)B * (all / N.TR + 1) * (cap / 32 + 1) < (int64_t)1 << 31;
-        if (fits && N.tiles < 2 * share && (2 * N.tiles <= share ? len - most : len / 2) > F4_JOIN) N.W = share;
+        // Streams of one length gain by that; others may where the longest alone takes ten times what a merge costs.  Twice as
+        // many tiles as workgroups even out by themselves.
+        if (fits && tiles < 2 * share && (cut < whole || (tiles > 1 && blocks > 10 * N.join))) N.W = share;
     }
     c.at_w = N.W ? cs_round_up((int64_t)2 * N.W * KVH * N.TR * (p->head_dim * 4 + 8), 16) + (int64_t)2 * N.W * 16 : 0;
     c.bytes = c.at_w + pa_ranges(W, len, B, KVH, p->head_dim, 256, 128, 192);
@@ -1119,7 +1141,7 @@ extern "C" int cs_paged_fp4_attention(const cs_pages_fp4* p, int32_t q_dtype, co
         const auto& N = c.narrow;
         const int64_t rows = (int64_t)2 * N.W * p->n_kv_heads * N.TR;
         float* po = (float*)workspace;
-        const f4_shares S = {N.TR, N.qr_lo, N.qr_hi, N.W, F4_LEAST, N.W ? (N.W + 63) / 64 : N.tiles, f4_near(p), po, (float2*)(po + rows * p->head_dim),
+        const f4_shares S = {N.TR, N.qr_lo, N.qr_hi, N.W, F4_LEAST, N.W ? (N.W + 63) / 64 : N.tiles, N.bound, N.join, f4_near(p), po, (float2*)(po + rows * p->head_dim),
                              (int4*)((char*)workspace + cs_round_up(rows * (p->head_dim * 4 + 8), 16))};
         const dim3 n = cs_paged_grid(grid_n);
 #define FN(HD_, NT_) if (c.hdt == HD_ && N.nt == NT_) rc = f32 ? f4n_launch<HD_, NT_, 3>(F, A, S, n, s) : f4n_launch<HD_, NT_, 1>(F, A, S, n, s)
