@@ -1078,7 +1078,10 @@ static f4_cut f4_make_cut(const cs_pages_fp4* p, bool f32, int H, bool has_row0,
         if (fits && tiles < 2 * share && (cut < whole || (tiles > 1 && blocks > 10 * N.join))) N.W = share;
     }
     c.at_w = N.W ? cs_round_up((int64_t)2 * N.W * KVH * N.TR * (p->head_dim * 4 + 8), 16) + (int64_t)2 * N.W * 16 : 0;
-    c.bytes = c.at_w + pa_ranges(W, len, B, KVH, p->head_dim, 256, 128, 192);
+    // A workgroup's ends and the merge in tokens of the kernel for many rows (with 128 and 192 for bfloat16 queries too: 4 x
+    // 300 rows of 32 heads behind 1000 tokens 52 -> 70 us, behind 16000 344 -> 399, 33 rows of 16 heads of 64 behind 300
+    // 14 -> 15; with 256 and 400 for float32 ones 33 rows of 8 heads behind 300 24 -> 26, 100 rows 25 -> 29).
+    c.bytes = c.at_w + (f32 ? pa_ranges(W, len, B, KVH, p->head_dim, 256, 128, 192) : pa_ranges(W, len, B, KVH, p->head_dim, 256, 256, 400));
     return c;
 }
 
