@@ -251,8 +251,9 @@ __global__ __launch_bounds__(64 * F4N_WAVES, 2) void k_paged_fp4_narrow(f4_call 
     // features 43 -> 85 us, others no change)
     constexpr int AHEAD = NT > 1 ? 1 : HD == 256 || NP > 1 ? 2 : 3;
     constexpr int ROWS = 16 * NT, QROW = HD * 2 + 16, QPLANE = ROWS * QROW;
-    constexpr int SLOT = NT * (MT * 1024 + 512);                // a wave's (O, maximum, sum)
-    constexpr int LDS_BYTES = 2 * SLOT > NP * QPLANE ? 2 * SLOT : NP * QPLANE;
+    constexpr int SLOT = NT * (2 * VF / 4 * 1024 + 512);        // half of a wave's O, with its maximum and sum
+    constexpr int LDS_BYTES = F4N_WAVES * SLOT > NP * QPLANE ? F4N_WAVES * SLOT : NP * QPLANE;
+    static_assert(F4N_WAVES == 4, "two exchanges");
     __shared__ __attribute__((aligned(16))) unsigned char smem[LDS_BYTES];
     // The arguments fill the scalar registers several times over.  Read anew for every segment and behind its loop, they
     // are not carried through it.
@@ -300,6 +301,12 @@ __global__ __launch_bounds__(64 * F4N_WAVES, 2) void k_paged_fp4_narrow(f4_call 
     const int open_lo = A.window ? T.L + i_hi - A.window + 1 : 0, open_hi = min(T.L + i_lo + 1, D.cap);
     const int w_first = A.window ? T.L + i_lo - A.window + 1 : 0;       // tokens before it are seen by no row of the tile
 
+    const int32_t* tab = D.p.table + T.b * D.p.table_stride;
+    constexpr int STEP = 32 * F4N_WAVES;
+    // the page of the lane's first block: on its way while the query rows are
+    int page_next = 0;
+    if (w_begin + 32 * wave < t_end) page_next = tab[min(w_begin + 32 * wave + lane * STEP, (t_end - 1) & ~31) >> D.page_log2];
+
     bf16x8 qreg[KS];
     if constexpr (QREG) {
         const int i = (T.n0 + c) / A.G, h = kvh * A.G + T.n0 + c - i * A.G;
@@ -309,19 +316,27 @@ __global__ __launch_bounds__(64 * F4N_WAVES, 2) void k_paged_fp4_narrow(f4_call 
             qreg[s] = (bf16x8){0, 0, 0, 0, 0, 0, 0, 0};
             if (c < n_rows && g * (HD / 4) + s * 8 < hd) qreg[s] = *reinterpret_cast<const bf16x8*>(qp + s * 8);
         }
-    } else
-    // query rows into LDS
-    for (int idx = tid; idx < ROWS * (HD / 8); idx += 64 * F4N_WAVES) {
-        const int n = idx / (HD / 8), seg = idx % (HD / 8);
-        bf16x8 v[NP];
+    } else {
+        // query rows into LDS, all loads before the first store
+        constexpr int EACH = (ROWS * (HD / 8) + 64 * F4N_WAVES - 1) / (64 * F4N_WAVES);
+        bf16x8 v[EACH][NP];
 #pragma unroll
-        for (int p = 0; p < NP; ++p) v[p] = (bf16x8){0, 0, 0, 0, 0, 0, 0, 0};
-        if (n < n_rows && seg * 8 < hd) {
-            const int i = (T.n0 + n) / A.G, h = kvh * A.G + T.n0 + n - i * A.G;
-            f4_split((const T_*)A.q + (T.row0 + i) * A.q_row + h * A.q_head + seg * 8, v);
+        for (int x = 0; x < EACH; ++x) {
+            const int idx = tid + x * 64 * F4N_WAVES, n = idx / (HD / 8), seg = idx % (HD / 8);
+#pragma unroll
+            for (int p = 0; p < NP; ++p) v[x][p] = (bf16x8){0, 0, 0, 0, 0, 0, 0, 0};
+            if (n < n_rows && seg * 8 < hd) {
+                const int i = (T.n0 + n) / A.G, h = kvh * A.G + T.n0 + n - i * A.G;
+                f4_split((const T_*)A.q + (T.row0 + i) * A.q_row + h * A.q_head + seg * 8, v[x]);
+            }
         }
 #pragma unroll
-        for (int p = 0; p < NP; ++p) *reinterpret_cast<bf16x8*>(smem + p * QPLANE + n * QROW + seg * 16) = v[p];
+        for (int x = 0; x < EACH; ++x) {
+            const int idx = tid + x * 64 * F4N_WAVES, n = idx / (HD / 8), seg = idx % (HD / 8);
+            if (n < ROWS)
+#pragma unroll
+                for (int p = 0; p < NP; ++p) *reinterpret_cast<bf16x8*>(smem + p * QPLANE + n * QROW + seg * 16) = v[x][p];
+        }
     }
     int q_last[NT];                                     // the last token that the lane's query rows see, and how many before it
     const int back = A.window ? A.window - 1 : 0x3fffffff;
@@ -332,7 +347,6 @@ __global__ __launch_bounds__(64 * F4N_WAVES, 2) void k_paged_fp4_narrow(f4_call 
     }
 
     const uint8_t *Kh = F.k + kvh * F.k_head, *Vh = F.v + kvh * F.v_head, *KSh = F.ks + kvh * F.ks_head, *VSh = F.vs + kvh * F.vs_head;
-    const int32_t* tab = D.p.table + T.b * D.p.table_stride;
     // (features that the head does not have are read at feature 0: their query elements are 0, their outputs are not stored)
     unsigned koff[KB], ksoff[KB], voff, vsoff;
     const unsigned kts = (unsigned)F.k_token, vts = (unsigned)F.v_token;
@@ -363,7 +377,6 @@ __global__ __launch_bounds__(64 * F4N_WAVES, 2) void k_paged_fp4_narrow(f4_call 
     const int kshift = 8 * (c & 3);
     if (!QREG) __syncthreads();
 
-    constexpr int STEP = 32 * F4N_WAVES;
     // A lane holds one of the wave's next 64 blocks: where in the pools it starts, so that a request costs the scalar
     // unit no multiplications.  A block whose page does not exist is read from page 0 and masked; a lane that has none
     // repeats the wave's last one.
@@ -375,7 +388,7 @@ __global__ __launch_bounds__(64 * F4N_WAVES, 2) void k_paged_fp4_narrow(f4_call 
         unsigned long long okay;
         {
             const int tb = t_begin + min(lane, n_all - 1) * STEP, slot = tb & (D.p.page_size - 1);
-            const int page = tab[tb >> D.page_log2];
+            const int page = seg0 == w_begin ? page_next : tab[tb >> D.page_log2];
             const bool ok = (unsigned)page < (unsigned)D.p.n_pages;
             const int64_t pg = ok ? page : 0;
             okay = __ballot(ok);
@@ -565,63 +578,74 @@ __global__ __launch_bounds__(64 * F4N_WAVES, 2) void k_paged_fp4_narrow(f4_call 
             if (i + j < n_all) block(kb[j], vb[j], i + j);
     }
 
-    // the waves' (maximum, sum, O) joined in two steps, a lane each time with the same lane of another wave;
-    // oacc[u][nt][j]: query row nt*16 + c, feature (4g + j) * VF + u
-    float l_run[NT];
+    // The waves' (maximum, sum, O) are joined in two exchanges, first with the wave two away, then with the neighbour, of
+    // half of what there is each time, so that wave w ends with element j = w of every accumulator.  oacc[u][nt][j]:
+    // query row nt*16 + c, feature (4g + j) * VF + u
+    float l_run[NT], mine2[MT][NT][2], mine1[MT][NT];
+    auto swap = [&](int partner, auto send, auto keep, auto n_tag) {
+        constexpr int N = decltype(n_tag)::value;               // elements of an accumulator that are sent, and kept
+        __syncthreads();             // (first: every wave is done with the query rows, or the exchange before)
+        unsigned char* to = smem + partner * SLOT;
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) l_run[nt] = lacc[nt][0];
+        for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
-    for (int step = F4N_WAVES / 2; step > 0; step >>= 1) {
-        __syncthreads();             // (first: every wave is done with the query rows, and with the segment before)
-        if (wave >= step && wave < 2 * step) {
-            unsigned char* to = smem + (wave - step) * SLOT;
+            for (int j = 0; j < N; ++j)
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-#pragma unroll
-                for (int mt = 0; mt < MT; ++mt) *reinterpret_cast<f32x4*>(to + ((nt * MT + mt) * 64 + lane) * 16) = oacc[mt][nt];
-                *reinterpret_cast<float2*>(to + NT * MT * 1024 + (nt * 64 + lane) * 8) = make_float2(m_run[nt], l_run[nt]);
-            }
+                for (int u = 0; u < VF; u += 4)
+                    *reinterpret_cast<f32x4*>(to + (((nt * N + j) * (VF / 4) + u / 4) * 64 + lane) * 16) =
+                        (f32x4){send(u, nt, j), send(u + 1, nt, j), send(u + 2, nt, j), send(u + 3, nt, j)};
+            *reinterpret_cast<float2*>(to + SLOT - NT * 512 + (nt * 64 + lane) * 8) = make_float2(m_run[nt], l_run[nt]);
         }
         __syncthreads();
-        if (wave < step) {
-            const unsigned char* from = smem + wave * SLOT;
+        const unsigned char* from = smem + wave * SLOT;
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-                const float2 ml = *reinterpret_cast<const float2*>(from + NT * MT * 1024 + (nt * 64 + lane) * 8);
-                const float M = fmaxf(m_run[nt], ml.x), Ms = M == -INFINITY ? 0.f : M;
-                const float f0 = __builtin_amdgcn_exp2f(m_run[nt] - Ms), f1 = __builtin_amdgcn_exp2f(ml.x - Ms);
-                m_run[nt] = M;
-                l_run[nt] = f0 * l_run[nt] + f1 * ml.y;
+        for (int nt = 0; nt < NT; ++nt) {
+            const float2 ml = *reinterpret_cast<const float2*>(from + SLOT - NT * 512 + (nt * 64 + lane) * 8);
+            const float M = fmaxf(m_run[nt], ml.x), Ms = M == -INFINITY ? 0.f : M;
+            const float f0 = __builtin_amdgcn_exp2f(m_run[nt] - Ms), f1 = __builtin_amdgcn_exp2f(ml.x - Ms);
+            m_run[nt] = M;
+            l_run[nt] = f0 * l_run[nt] + f1 * ml.y;
 #pragma unroll
-                for (int mt = 0; mt < MT; ++mt)
-                    oacc[mt][nt] = f0 * oacc[mt][nt] + f1 * *reinterpret_cast<const f32x4*>(from + ((nt * MT + mt) * 64 + lane) * 16);
-            }
+            for (int j = 0; j < N; ++j)
+#pragma unroll
+                for (int u = 0; u < VF; u += 4) {
+                    const f32x4 o = *reinterpret_cast<const f32x4*>(from + (((nt * N + j) * (VF / 4) + u / 4) * 64 + lane) * 16);
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) keep(u + x, nt, j, f0, f1 * o[x]);
+                }
         }
-    }
-    if (wave) continue;
+    };
+    // (by masks: a choice between two elements of an accumulator becomes an index into it, which registers do not have)
+    const unsigned high = wave >= 2 ? ~0u : 0u, odd = wave & 1 ? ~0u : 0u;
+    auto pick = [](unsigned m, float a, float b) { return __uint_as_float((__float_as_uint(a) & m) | (__float_as_uint(b) & ~m)); };
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) l_run[nt] = lacc[nt][0];
+    swap(wave ^ 2, [&](int u, int nt, int j) { return pick(high, oacc[u][nt][j], oacc[u][nt][2 + j]); },
+         [&](int u, int nt, int j, float f, float add) { mine2[u][nt][j] = f * pick(high, oacc[u][nt][2 + j], oacc[u][nt][j]) + add; },
+         std::integral_constant<int, 2>());
+    swap(wave ^ 1, [&](int u, int nt, int) { return pick(odd, mine2[u][nt][0], mine2[u][nt][1]); },
+         [&](int u, int nt, int, float f, float add) { mine1[u][nt] = f * pick(odd, mine2[u][nt][1], mine2[u][nt][0]) + add; },
+         std::integral_constant<int, 1>());
     const f4_call& C2 = call();
     const f4_shares& S = C2.S;
-    const int part = 2 * w + K.first, KVH = C2.F.d.p.n_kv_heads;
-    if (!K.whole && kvh == 0 && lane == 0) S.who[part] = make_int4(T.row0, T.n0, T.QR, K.number | K.of << 16);
+    const int part = 2 * w + K.first, KVH = C2.F.d.p.n_kv_heads, j = wave;
+    if (!K.whole && kvh == 0 && tid == 0) S.who[part] = make_int4(T.row0, T.n0, T.QR, K.number | K.of << 16);
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
         const int n = nt * 16 + c;
         if (n >= n_rows) continue;
         const int i = (T.n0 + n) / C2.A.G, h = kvh * C2.A.G + T.n0 + n - i * C2.A.G;
         const int64_t r = T.row0 + i, row = ((int64_t)part * KVH + kvh) * S.TR + n;
-        const bool whole = K.whole;
         const float inv = l_run[nt] > 0.f ? 1.0f / l_run[nt] : 0.f;           // a row that sees nothing: 0
-        if (g == 0 && !whole) S.pml[row] = make_float2(m_run[nt], l_run[nt]);
+        if (tid < 16 && !K.whole) S.pml[row] = make_float2(m_run[nt], l_run[nt]);
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-#pragma unroll
-            for (int u = 0; u < VF; u += 4) {
-                const int d = (4 * g + j) * VF + u;
-                const f32x4 o = (f32x4){oacc[u][nt][j], oacc[u + 1][nt][j], oacc[u + 2][nt][j], oacc[u + 3][nt][j]};
-                if (d >= hd) continue;
-                if (whole) pa_store4((T_*)C2.A.out + r * C2.A.out_row + h * C2.A.out_head + d, o * inv);
-                else pa_store4(S.po + row * hd + d, o);
-            }
+        for (int u = 0; u < VF; u += 4) {
+            const int d = (4 * g + j) * VF + u;
+            const f32x4 o = (f32x4){mine1[u][nt], mine1[u + 1][nt], mine1[u + 2][nt], mine1[u + 3][nt]};
+            if (d >= hd) continue;
+            if (K.whole) pa_store4((T_*)C2.A.out + r * C2.A.out_row + h * C2.A.out_head + d, o * inv);
+            else pa_store4(S.po + row * hd + d, o);
+        }
     }
     }
 }
