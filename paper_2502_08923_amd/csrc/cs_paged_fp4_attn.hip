@@ -60,7 +60,7 @@ __device__ __forceinline__ void f4_split(const float* p, bf16x8 (&o)[3]) {
 struct f4_shares {
     int TR, qr_lo, qr_hi;
     int W, least;             // workgroups per KV head; fewest blocks of a piece or a share
-    int step;                 // distance of the numbers of pieces tried
+    int step;                 // distance of the numbers of pieces tried (W 0: workgroups per KV head)
     float bound, join;        // what a block of all tokens costs the chip, and a merge, in blocks of a workgroup
     int near;                 // neighbouring KV heads that run on one die
     float* po;                // [2 W][KVH][TR][hd] partial outputs; 2w: of a tile that an earlier workgroup has begun, 2w + 1: of one that w begins
@@ -125,13 +125,28 @@ __device__ __forceinline__ f4_walk f4_start(const cs_pages_dev& D, int G, int wi
     k.e = k.rows = make_int2(0, 0), k.len = k.units = k.upto = 0;
     const int B = D.p.batch;
     if (!S.W) {
-        if (!D.row0) {                                          // equal rows: the stream is known
-            const int tiles = f4_extent(D, G, window, S, D.rows, 0).x;
-            const int b = __builtin_amdgcn_readfirstlane(w / max(tiles, 1));
-            k.b0 = b & ~63;
-            k.before = k.b0 * tiles;
-            if (b >= B) k.end = k.p;
+        // The workgroup's stream (b0) and tile (before).  Equal rows: by division.  Streams of at most one tile: one each.  Else
+        // stream b has the workgroups from row0[b] * G / TR + b on, which are at least as many as its tiles, and is searched
+        // for, 64 places at a time.
+        if (!D.row0) {
+            const int tiles = max(f4_extent(D, G, window, S, D.rows, 0).x, 1);
+            k.b0 = __builtin_amdgcn_readfirstlane(w / tiles);
+            k.before = w - k.b0 * tiles;
+        } else if (S.qr_hi <= S.TR) k.b0 = w;
+        else {
+            auto from = [&](int b) { return (int)((int64_t)cs_stream_rows(D, b).x * G / S.TR) + b; };
+            int lo = 0, n = B;
+            while (n > 1) {
+                const int step = (n + 63) >> 6, b = lo + lane * step;
+                const int c = __popcll(__ballot(b < lo + n && from(min(b, B - 1)) <= w));
+                const int skip = max(c - 1, 0) * step;
+                lo += skip;
+                n = min(n - skip, step);
+            }
+            k.b0 = lo;
+            k.before = w - __builtin_amdgcn_readfirstlane(from(lo));
         }
+        if (k.b0 >= B || k.before < 0) k.end = k.p;
         return k;
     }
     int all = 0, tiles = 0;
@@ -176,6 +191,18 @@ __device__ __forceinline__ f4_walk f4_start(const cs_pages_dev& D, int G, int wi
 }
 __device__ __forceinline__ bool f4_next(const cs_pages_dev& D, int G, int window, const f4_shares& S, int w, f4_walk& k, int lane, f4_segment& o) {
     if (k.p >= k.end) return false;
+    if (!S.W) {
+        k.p = k.end;
+        const int2 rows = cs_stream_rows(D, k.b0);
+        o.b = k.b0;
+        o.row0 = __builtin_amdgcn_readfirstlane(rows.x), o.rows = __builtin_amdgcn_readfirstlane(rows.y);
+        o.len = __builtin_amdgcn_readfirstlane(cs_stream_len(D, k.b0));
+        o.n0 = k.before * S.TR;
+        o.off = 0, o.n = 1;
+        o.first = o.whole = true;
+        o.number = 0, o.of = 1;
+        return k.before < f4_extent(D, G, window, S, o.rows, o.len).x;
+    }
     for (;;) {
         if (!k.have) f4_look_at(D, G, window, S, k, lane);
         const int all = __builtin_amdgcn_readlane(k.upto, 63);
@@ -185,11 +212,14 @@ __device__ __forceinline__ bool f4_next(const cs_pages_dev& D, int G, int window
         k.have = false;
         if (k.b0 >= D.p.batch) return false;                    // (more workgroups than tiles)
     }
-    const int l = __ffsll(__ballot(k.before + k.upto > k.p)) - 1;
+    const unsigned long long past = __ballot(k.before + k.upto > k.p);
+    if (!past) return false;                                    // (row offsets that make no sense: sums past 2^31)
+    const int l = __ffsll(past) - 1;
     const int tiles = __builtin_amdgcn_readlane(k.e.x, l), blocks = __builtin_amdgcn_readlane(k.e.y, l), units = __builtin_amdgcn_readlane(k.units, l);
     o.row0 = __builtin_amdgcn_readlane(k.rows.x, l), o.rows = __builtin_amdgcn_readlane(k.rows.y, l), o.len = __builtin_amdgcn_readlane(k.len, l);
     const unsigned at = k.p - (k.before + __builtin_amdgcn_readlane(k.upto, l) - tiles * units);
     const int tile = __builtin_amdgcn_readfirstlane(tiles == 1 ? 0 : at / (unsigned)units), off = at - tile * units;
+    if ((unsigned)tile >= (unsigned)tiles) return false;        // (as above)
     const int n = min(units - off, k.end - k.p);
     o.b = k.b0 + l;
     o.n0 = tile * S.TR;
@@ -718,7 +748,8 @@ __global__ __launch_bounds__(F4J_THREADS) void k_paged_fp4_join(cs_pages_dev D, 
 // multiply out of this one.
 //   keys: 16 tokens x 32 features in fragment order, a lane's 16 bytes are what it multiplies
 //   values: 16 tokens x 32 features as two 16 x 16 squares of 32-byte rows for the transposing LDS read
-// What is dead or behind every window is laid down as zeros, so only the scores have a mask.
+// What is dead or behind every window is laid down under scale byte 0, finite whatever it is, so only the scores
+// have a mask.
 #define F4W_WAVES 8
 template <int HD, int NT, int NP>
 __global__ __launch_bounds__(64 * F4W_WAVES) void k_paged_fp4_wide(cs_fp4_dev F, pa_args A, pa_plan P) {
@@ -1035,7 +1066,7 @@ struct f4_cut {
     int hdt;
     struct {
         int nt, TR, qr_lo, qr_hi, tiles;      // tiles: an upper bound; 0: no launch
-        int W;                                // see f4_shares
+        int W, groups;                        // see f4_shares; workgroups per KV head
         float bound, join;
     } narrow;
     pa_part wide;
@@ -1100,6 +1131,8 @@ static f4_cut f4_make_cut(const cs_pages_fp4* p, bool f32, int H, bool has_row0,
         // Streams of one length gain by that; others may where the longest alone takes ten times what a merge costs.  Twice as
         // many tiles as workgroups even out by themselves.
         if (fits && tiles < 2 * share && (cut < whole || (tiles > 1 && blocks > 10 * N.join))) N.W = share;
+        // (without shares: as f4_start counts them)
+        N.groups = N.W ? N.W : !has_row0 || N.qr_hi <= N.TR ? (has_row0 ? B : tiles) : (int)(all / N.TR) + B;
     }
     c.at_w = N.W ? cs_round_up((int64_t)2 * N.W * KVH * N.TR * (p->head_dim * 4 + 8), 16) + (int64_t)2 * N.W * 16 : 0;
     // A workgroup's ends and the merge in tokens of the kernel for many rows (with 128 and 192 for bfloat16 queries too: 4 x
@@ -1152,7 +1185,7 @@ extern "C" int cs_paged_fp4_attention(const cs_pages_fp4* p, int32_t q_dtype, co
     CS_REQUIRE(c.bytes <= 0 || (workspace && workspace_bytes >= c.bytes), CS_E_CAPACITY, "%s: the workspace has %lld bytes, %lld are needed",
                who, (long long)(workspace ? workspace_bytes : 0), (long long)c.bytes);
     CS_REQUIRE(((uintptr_t)workspace & 15) == 0, CS_E_ARG, "%s: the workspace is not aligned to 16 bytes", who);
-    const int64_t grid_n = (int64_t)(c.narrow.W ? c.narrow.W : c.narrow.tiles) * p->n_kv_heads, grid_w = (int64_t)c.wide.entries * p->n_kv_heads;
+    const int64_t grid_n = (int64_t)c.narrow.groups * p->n_kv_heads, grid_w = (int64_t)c.wide.entries * p->n_kv_heads;
     CS_REQUIRE(grid_n <= 0x7fffffff && grid_w <= 0x7fffffff, CS_E_UNSUPPORTED, "%s: too many tiles", who);
     int rc = CS_E_UNSUPPORTED;
     if (grid_w) {
@@ -1168,7 +1201,7 @@ extern "C" int cs_paged_fp4_attention(const cs_pages_fp4* p, int32_t q_dtype, co
         const auto& N = c.narrow;
         const int64_t rows = (int64_t)2 * N.W * p->n_kv_heads * N.TR;
         float* po = (float*)workspace;
-        const f4_shares S = {N.TR, N.qr_lo, N.qr_hi, N.W, F4_LEAST, N.W ? (N.W + 63) / 64 : N.tiles, N.bound, N.join, f4_near(p), po, (float2*)(po + rows * p->head_dim),
+        const f4_shares S = {N.TR, N.qr_lo, N.qr_hi, N.W, F4_LEAST, N.W ? (N.W + 63) / 64 : N.groups, N.bound, N.join, f4_near(p), po, (float2*)(po + rows * p->head_dim),
                              (int4*)((char*)workspace + cs_round_up(rows * (p->head_dim * 4 + 8), 16))};
         const dim3 n = cs_paged_grid(grid_n);
 #define FN(HD_, NT_) if (c.hdt == HD_ && N.nt == NT_) rc = f32 ? f4n_launch<HD_, NT_, 3>(F, A, S, n, s) : f4n_launch<HD_, NT_, 1>(F, A, S, n, s)

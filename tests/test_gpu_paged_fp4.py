@@ -504,6 +504,20 @@ def test_attention_many_ragged_streams(B, dtype):
 
 
 @pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("B", [1, 64, 66, 200, 4200])
+def test_attention_several_tiles_of_many_streams(B, dtype):
+    """Hints that are too small leave streams several tiles of 16 query rows and one workgroup each, found from the row offsets; some
+    streams have no rows, also the first and the last."""
+    rows = [(b * 5) % 12 if b % 7 else 0 for b in range(B)]
+    rows[0] = 9 if B == 1 else 0
+    lens = [(13 * b) % 60 for b in range(B)]
+    c = Cache(lens, rows, 1, 32, 32, dtype, seed=B, pad=2, spare=0)
+    c.check(4, max_rows=1, max_len=16)
+    if B == 200:
+        c.check(8, max_rows=4, max_len=16)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
 def test_attention_scale_and_peaked_scores(dtype):
     c = Cache([300, 1], [5, 2], 2, 64, 32, dtype)
     c.check(4, scale=0.01)
