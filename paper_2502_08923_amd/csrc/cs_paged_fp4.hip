@@ -173,6 +173,17 @@ __device__ __forceinline__ unsigned f4_quad_max(unsigned v) {
     return max(v, (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, 0x4e, 0xf, 0xf, true));    // lanes 2 3 0 1
 }
 
+// The workgroup's turn.  Dies take workgroups in turn, eight of them, each with a cache of its own: RUN neighbours, whose
+// rows share lines of scales, are eight workgroups apart.  (Read of 145 thousand rows of 8 heads, pages of 64: runs of 1 124 us, 8
+// 112, 64 108, 256 110; append of 11 thousand 14.1, 13.5, 13.8, 14.1, of 4096 7.8, 7.6, 7.4, 7.8.)
+#define F4_APPEND_RUN 8
+#define F4_READ_RUN 64
+template <int RUN>
+__device__ __forceinline__ int f4_turn() {
+    const int n = gridDim.x * gridDim.z, wg = (int)cs_paged_wg(), i = wg & (8 * RUN - 1);
+    return (wg | (8 * RUN - 1)) < n ? wg - i + (i & 7) * RUN + (i >> 3) : wg;
+}
+
 // ---- append -----------------------------------------------------------------------------
 
 template <typename TI>
@@ -180,7 +191,7 @@ __global__ __launch_bounds__(F4_THREADS) void k_paged_fp4_append(cs_fp4_dev F, f
     __shared__ f4_places to;
     const cs_pages_dev& D = F.d;
     const int tid = threadIdx.x, KVH = D.p.n_kv_heads;
-    const int r0 = (int)cs_paged_wg() * A.rpw, nr = min(A.rpw, D.R - r0);
+    const int r0 = f4_turn<F4_APPEND_RUN>() * A.rpw, nr = min(A.rpw, D.R - r0);
     // rows behind the last stream are not read; the others are in flight while their places are looked up
     const int live = D.row0 ? min(nr, min(max(D.row0[D.p.batch], 0), D.R) - r0) : nr;
     for (int round = 0; round * (F4_THREADS >> A.lanes_log2) < 2 * KVH; ++round) {
@@ -237,7 +248,7 @@ __global__ __launch_bounds__(F4_THREADS) void k_paged_fp4_append(cs_fp4_dev F, f
 }
 
 // ---- read -------------------------------------------------------------------------------
-// (stores that pass the caches by: 12 streams of up to 18431 tokens 169 -> 124 us, a 45 MB read 14.0 -> 12.2)
+// (Stores that pass the caches by: 12 streams of up to 18431 tokens 169 -> 124 us, before neighbours ran on one die, a 45 MB read 14.0 -> 12.2)
 __device__ __forceinline__ void f4_store(bf16_t* p, bf16x8 v) { __builtin_nontemporal_store(__builtin_bit_cast(u32x4, v), reinterpret_cast<u32x4*>(p)); }
 __device__ __forceinline__ void f4_store(float* p, bf16x8 v) {
 #pragma unroll
@@ -250,7 +261,7 @@ __global__ __launch_bounds__(F4_THREADS) void k_paged_fp4_read(cs_fp4_dev F, f4_
     __shared__ f4_places from;
     const cs_pages_dev& D = F.d;
     const int tid = threadIdx.x, KVH = D.p.n_kv_heads;
-    const int r0 = (int)cs_paged_wg() * A.rpw, nr = min(A.rpw, D.R - r0);
+    const int r0 = f4_turn<F4_READ_RUN>() * A.rpw, nr = min(A.rpw, D.R - r0);
     if (tid < CS_WAVE) {
         const int2 at = f4_place(D, A.first, r0, nr, tid);
         if (tid < nr) from.set(F, tid, at);
