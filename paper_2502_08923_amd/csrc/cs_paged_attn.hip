@@ -971,7 +971,8 @@ __global__ __launch_bounds__(64 * PF_WAVES, !TOKENS && HD <= 128 ? 2 : 1) void k
 // features, four each; a lane reads the (max, sum) pairs of every lanes-th range, and the weights go
 // round by shuffles.  The workgroups are those of the kernel before it: the ones that had the ranges of
 // a tile share out its rows (4 ranges of 8 x 44 rows and 8 heads: 6 us, a launch's own 3 among them; 13
-// ranges of 37 float32 tiles and 2 heads, 962 workgroups, 11.6 us).
+// ranges of 37 float32 tiles and 2 heads, 962 workgroups, 11.6 us).  As many of them as the grid is high
+// stand in for one of these.
 #define PM_THREADS 256
 template <typename T_>
 __global__ __launch_bounds__(PM_THREADS) void k_paged_merge(cs_pages_dev D, pa_args A, pa_plan P, int lanes_log2) {
@@ -982,7 +983,7 @@ __global__ __launch_bounds__(PM_THREADS) void k_paged_merge(cs_pages_dev D, pa_a
     if (nsplit <= 1) return;
     const int lanes = 1 << lanes_log2, sub = threadIdx.x & (lanes - 1), d = sub * 4, per = PM_THREADS >> lanes_log2, hd = D.p.head_dim;
     const int64_t step = (int64_t)KVH * P.TR;                      // from one range's row to the next one's
-    for (int n = split * per + (threadIdx.x >> lanes_log2); n < P.TR && who.y + n < who.z; n += nsplit * per) {
+    for (int n = (split * gridDim.y + blockIdx.y) * per + (threadIdx.x >> lanes_log2); n < P.TR && who.y + n < who.z; n += nsplit * per * gridDim.y) {
         const int64_t at = ((int64_t)(entry - split) * KVH + kvh) * P.TR + n;
         float M = -INFINITY;
         for (int s = sub; s < nsplit; s += lanes) M = fmaxf(M, P.pml[at + s * step].x);
