@@ -10,8 +10,8 @@
 // there, so scale and codes are exact integer and power-of-two arithmetic and one rounding.  A thread keeps its head
 // and segment and goes from row to row; the places of up to 64 rows are looked up by a wave at once, a lane a row, and
 // go round through LDS.  (With a division and three 64-bit products per (row, head) pair instead, the vector unit was
-// the bound: append of 11 thousand rows of 8 heads of 128 16.9 us -> 12.8, read of 111 thousand 282 -> 204, and 123 with
-// stores past the caches: 4.7 and 6.1 TB/s.)  88 rows take 3.6 us either way, a launch's latency.
+// the bound: append of 11 thousand rows of 8 heads of 128 16.9 us -> 12.8, read of 145 thousand 282 -> 204, 123 with
+// stores past the caches, 108 with neighbours on one die: 4.2 and 7.0 TB/s.)  88 rows take 3.6 us either way, a launch's latency.
 #include <algorithm>
 
 #include "cs_paged_fp4.h"
@@ -68,7 +68,7 @@ int cs_fp4_view(const char* who, const cs_pages_fp4* p, const int32_t* d_row0, i
 #define F4_THREADS 256
 #define F4_ROWS 64            // most rows of a workgroup: a lane each for their places
 // Rows of a thread in flight, and in all.  (Append of 160 thousand rows of one head of 64: 12.9 us with two in flight, 16.1 with
-// four, 17.4 with eight, 11 thousand of 8 heads of 128 14.3, 14.5 and 16.9; read of 111 thousand rows of 8 heads 226, 204 and
+// four, 17.4 with eight, 11 thousand of 8 heads of 128 14.3, 14.5 and 16.9; read of 145 thousand rows of 8 heads 226, 204 and
 // 197, of 11 thousand 13.8, 13.9 and 14.9.  16 rows of a thread instead of eight: no change or 2 % slower, four: up to 30 %.)
 #define F4_APPEND_BATCH 2
 #define F4_READ_BATCH 4

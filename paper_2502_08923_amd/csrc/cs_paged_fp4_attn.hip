@@ -264,6 +264,13 @@ __device__ __forceinline__ int2 f4_whose(unsigned wg, int KVH, int W_all, int ne
 // eight bytes of the page.  Of those value rows a lane loads HD / 16 features each, makes them bfloat16 and
 // turns pairs of tokens with byte permutes into the A fragments: fragment u has feature c * HD / 16 + u in row
 // c.  A page holds whole blocks, so every load has one page, a uniform base, and nothing to check.
+//
+// Single tokens are bound by memory: 64 streams of 8191 tokens, 8 heads of 128, 107 us = 5.3 TB/s of codes and scales; 64 of 2 to 8
+// thousand over token-major pages of 32, where a head's codes are half lines, 95 us = 3.8 TB/s with 1.04 times the bytes read (two
+// heads in one workgroup: 149 us for 138 on one die).  48 rows are bound by instructions: 8 x 11 rows behind 18431 48.5 us, the
+// vector unit 60 % and the matrix unit 30 % busy; a block is 64 conversions, 32 permutes, 24 exponentials and 51 products a wave.
+// Two workgroups a compute unit: registers for three spill, with one 48 rows take 65 us for 57, with their queries in registers 100.
+// 64 tokens a softmax step instead of 32: no gain.
 #define F4N_WAVES 4
 template <int HD>
 struct f4_keys { u32x4 k[2][HD == 256 ? 2 : 1]; u32x2 s[HD == 256 ? 2 : 1]; };
@@ -683,7 +690,8 @@ __global__ __launch_bounds__(64 * F4N_WAVES, 2) void k_paged_fp4_narrow(f4_call 
 // out[r][h] = sum_s 2^(m_s - M) O_s / sum_s 2^(m_s - M) l_s over the workgroups that have a part of a tile, which share
 // out its rows.  Parts are waited for, so a row's are spread over 2^teams_log2 teams of 2^lanes_log2 lanes, four of them a
 // team, as far as the workgroup has teams; a lane of a team has four of the hd features, and reads the (maximum,
-// sum) pairs of every lanes-th part, whose weights go round by shuffles.
+// sum) pairs of every lanes-th part, whose weights go round by shuffles.  (Eight parts of 8 x 44 rows and 8 heads of 128,
+// 11 MB: 6.5 us, a launch's own 3 among them.)
 #define F4J_THREADS 256
 template <typename T_>
 __global__ __launch_bounds__(F4J_THREADS) void k_paged_fp4_join(cs_pages_dev D, pa_args A, f4_shares S, int lanes_log2) {
@@ -750,6 +758,12 @@ __global__ __launch_bounds__(F4J_THREADS) void k_paged_fp4_join(cs_pages_dev D, 
 //   values: 16 tokens x 32 features as two 16 x 16 squares of 32-byte rows for the transposing LDS read
 // What is dead or behind every window is laid down under scale byte 0, finite whatever it is, so only the scores
 // have a mask.
+//
+// 16 x 33 rows of 28 heads behind 65535: 498 us a call = 1.0 PFLOP/s; 4096 rows on an empty cache 145 us = 0.95; 2048 rows behind 16384
+// 1.05 (an 8192^3 library product: 1.22).  Matrix and vector unit are each busy half of the time and overlap little.  64 tokens a
+// softmax step instead of 32: 578 -> 497 us.  Tried against that: the waves of a SIMD at different points of the
+// loop with a third stage in LDS (1 to 3 % slower), priorities fixed by wave (2 to 8 %) or none (1 to 2 %), laying down after the scores (4 %) or
+// skewed between the halves of the workgroup (15 %).
 #define F4W_WAVES 8
 template <int HD, int NT, int NP>
 __global__ __launch_bounds__(64 * F4W_WAVES) void k_paged_fp4_wide(cs_fp4_dev F, pa_args A, pa_plan P) {
