@@ -266,8 +266,8 @@ __device__ __forceinline__ int2 f4_whose(unsigned wg, int KVH, int W_all, int ne
 // c.  A page holds whole blocks, so every load has one page, a uniform base, and nothing to check.
 //
 // Single tokens are bound by memory: 64 streams of 8191 tokens, 8 heads of 128, 107 us = 5.3 TB/s of codes and scales; 64 of 2 to 8
-// thousand over token-major pages of 32, where a head's codes are half lines, 95 us = 3.8 TB/s with 1.04 times the bytes read (two
-// heads in one workgroup: 149 us for 138 on one die).  48 rows are bound by instructions: 8 x 11 rows behind 18431 48.5 us, the
+// thousand over token-major pages of 32, where a head's codes are half lines, 92 us = 3.9 TB/s with 1.04 times the bytes read (two
+// heads in one workgroup: 149 us for 138 on one die; in one wave 98 for 97; four or all eight on one die: no change).  48 rows are bound by instructions: 8 x 11 rows behind 18431 48.5 us, the
 // vector unit 60 % and the matrix unit 30 % busy; a block is 64 conversions, 32 permutes, 24 exponentials and 51 products a wave.
 // Two workgroups a compute unit: registers for three spill, with one 48 rows take 65 us for 57, with their queries in registers 100.
 // 64 tokens a softmax step instead of 32: no gain.
@@ -277,7 +277,7 @@ struct f4_keys { u32x4 k[2][HD == 256 ? 2 : 1]; u32x2 s[HD == 256 ? 2 : 1]; };
 template <int HD>
 struct f4_values { unsigned v[8][HD == 256 ? 2 : 1]; u32x2 s; };
 
-template <int HD, int NT, int NP>
+template <int HD, int NT, int NP, bool KLDS>
 __global__ __launch_bounds__(64 * F4N_WAVES, 2) void k_paged_fp4_narrow(f4_call C) {
     typedef f4_qtype<NP> T_;
     constexpr int KS = HD / 32, MT = HD / 16, VF = HD / 16;
@@ -292,6 +292,13 @@ __global__ __launch_bounds__(64 * F4N_WAVES, 2) void k_paged_fp4_narrow(f4_call 
     constexpr int LDS_BYTES = F4N_WAVES * SLOT > NP * QPLANE ? F4N_WAVES * SLOT : NP * QPLANE;
     static_assert(F4N_WAVES == 4, "two exchanges");
     __shared__ __attribute__((aligned(16))) unsigned char smem[LDS_BYTES];
+    // KLDS, where key rows lie apart: sixteen of them are requested with four neighbouring lanes on the 64 bytes of each, so that
+    // neighbours share lines, and go to the lanes that multiply them through LDS of the wave's own.  (Requested by those
+    // lanes themselves: 64 single tokens of 2 to 8 thousand over token-major pages 97.4 us for 94.1, 1024 of 100 100 for 95;
+    // head-major pages 1 % slower, more rows and the values the same way no change.)
+    static_assert(!KLDS || HD == 128, "a lane's key row is one load");
+    constexpr int KROW = HD / 2 + 16, KTILE = 16 * KROW;
+    __shared__ __attribute__((aligned(16))) unsigned char kmem[KLDS ? F4N_WAVES * 2 * KTILE : 16];
     // The arguments fill the scalar registers several times over.  Read anew for every segment and behind its loop, they
     // are not carried through it.
     typedef const __attribute__((address_space(4))) f4_call* call_ptr;
@@ -392,6 +399,10 @@ __global__ __launch_bounds__(64 * F4N_WAVES, 2) void k_paged_fp4_narrow(f4_call 
         for (int h = 0; h < KB; ++h) {
             const int f = g * (HD / 4) + h * 32 < hd ? g * (HD / 4) + h * 32 : 0;
             koff[h] = (8 * (c >> 2) + (c & 3)) * kts + f / 2;
+            if (KLDS) {
+                const int r = lane >> 2, fr = (lane & 3) * 32 < hd ? (lane & 3) * 32 : 0;
+                koff[h] = (8 * (r >> 2) + (r & 3)) * kts + fr / 2;
+            }
             ksoff[h] = f / CS_FP4_GROUP * (unsigned)F.ks_group + 8 * (c >> 2);
         }
         const int f = c * VF < hd ? c * VF : 0;
@@ -474,6 +485,14 @@ __global__ __launch_bounds__(64 * F4N_WAVES, 2) void k_paged_fp4_narrow(f4_call 
             for (int a = 0; a < 2; ++a)
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) sacc[a][nt] = (f32x4){0.f, 0.f, 0.f, 0.f};
+            if constexpr (KLDS) {
+                unsigned char* t = kmem + wave * 2 * KTILE;
+#pragma unroll
+                for (int a = 0; a < 2; ++a) *reinterpret_cast<u32x4*>(t + a * KTILE + (lane >> 2) * KROW + (lane & 3) * 16) = kb.k[a][0];
+                __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+#pragma unroll
+                for (int a = 0; a < 2; ++a) kb.k[a][0] = *reinterpret_cast<const u32x4*>(t + a * KTILE + c * KROW + g * 16);
+            }
 #pragma unroll
             for (int s = 0; s < KS; ++s) {
                 const int h = s / 4, d = s % 4;
@@ -1166,9 +1185,9 @@ extern "C" int64_t cs_paged_fp4_attention_workspace(const cs_pages_fp4* p, int32
     return f4_make_cut(p, q_dtype == CS_F32, n_heads, has_row0 != 0, R, max_rows, max_len).bytes;
 }
 
-template <int HD, int NT, int NP>
+template <int HD, int NT, int NP, bool KLDS = false>
 static int f4n_launch(const cs_fp4_dev& F, const pa_args& A, const f4_shares& S, dim3 grid, hipStream_t s) {
-    k_paged_fp4_narrow<HD, NT, NP><<<grid, 64 * F4N_WAVES, 0, s>>>(f4_call{F, A, S});
+    k_paged_fp4_narrow<HD, NT, NP, KLDS><<<grid, 64 * F4N_WAVES, 0, s>>>(f4_call{F, A, S});
     return cs_launch_ok("k_paged_fp4_narrow");
 }
 template <int HD, int NT, int NP>
@@ -1221,7 +1240,9 @@ extern "C" int cs_paged_fp4_attention(const cs_pages_fp4* p, int32_t q_dtype, co
                              (int4*)((char*)workspace + cs_round_up(rows * (p->head_dim * 4 + 8), 16))};
         const dim3 n = cs_paged_grid(grid_n);
 #define FN(HD_, NT_) if (c.hdt == HD_ && N.nt == NT_) rc = f32 ? f4n_launch<HD_, NT_, 3>(F, A, S, n, s) : f4n_launch<HD_, NT_, 1>(F, A, S, n, s)
-        FN(64, 1); FN(64, 2); FN(64, 3); FN(128, 1); FN(128, 2); FN(128, 3); FN(256, 1);
+        if (c.hdt == 128 && N.nt == 1 && !f32 && p->k_token > p->head_dim / 2) rc = f4n_launch<128, 1, 1, true>(F, A, S, n, s);
+        else FN(128, 1);
+        FN(64, 1); FN(64, 2); FN(64, 3); FN(128, 2); FN(128, 3); FN(256, 1);
 #undef FN
         CS_TRY(rc);
         if (N.W) {

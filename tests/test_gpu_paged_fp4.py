@@ -441,6 +441,18 @@ def test_attention_evicted_pages(P, rows, dtype):
         assert bool((got[0] == 0).all())
 
 
+@pytest.mark.parametrize("order", ["token", "both"])
+@pytest.mark.parametrize("H,KVH,hd", [(8, 2, 128), (3, 1, 128), (16, 8, 128), (6, 2, 96)])
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_attention_few_rows_of_pages_whose_rows_lie_apart(H, KVH, hd, order, dtype):
+    lens, rows = [0, 31, 32, 700, 3001, 5, 129], [1, 1, 4, 2, 1, 0, 3]
+    c = Cache(lens, rows, KVH, hd, 32, dtype, seed=hd + H, order=order, pad=2, holes=[(3, 1), (4, 0), (4, 93)])
+    c.check(H)
+    c.check(H, max_rows=4, max_len=3002)
+    c.check(H, window=50)
+    Cache([9000, 77], [1, 1], KVH, hd, 64, dtype, seed=hd, order=order).check(H)
+
+
 @pytest.mark.parametrize("dtype", [BF, F32])
 def test_attention_shared_prefix(dtype):
     Cache([150, 200, 133], [4, 1, 40], 2, 64, 32, dtype, order="both", shared=4).check(8)
