@@ -248,20 +248,36 @@ __global__ __launch_bounds__(F4_THREADS) void k_paged_fp4_append(cs_fp4_dev F, f
 }
 
 // ---- read -------------------------------------------------------------------------------
-// (Stores that pass the caches by: 12 streams of up to 18431 tokens 169 -> 124 us, before neighbours ran on one die, a 45 MB read 14.0 -> 12.2)
-__device__ __forceinline__ void f4_store(bf16_t* p, bf16x8 v) { __builtin_nontemporal_store(__builtin_bit_cast(u32x4, v), reinterpret_cast<u32x4*>(p)); }
-__device__ __forceinline__ void f4_store(float* p, bf16x8 v) {
+// What a lane has of a row, segment `seg` of `segs` with eight elements each, as numbers.  Stores pass the caches by (12 streams of up
+// to 18431 tokens, bfloat16: 165 us through them, 108 past).  A float32 row is twice as long as what one store of its lanes holds: one has
+// the first half of the row, one the second, and a lane asks another (`first` and on) for its four codes, for stores that
+// leave every other 16 bytes out reach memory in parts (35 thousand rows of 8 heads of 128: 53 us, 153 with such stores, 91 with
+// those through the caches).  Halves that are no whole lines go through the caches for the same reason: WHOLE false, heads of 96 41 us for
+// 51, of 160 44 for 52, of 64 28 for 29; of 128 and 256 73 for 53.
+template <bool WHOLE>
+__device__ __forceinline__ void f4_store(bf16_t* row, int seg, int, int, unsigned codes, unsigned scale) {
+    __builtin_nontemporal_store(__builtin_bit_cast(u32x4, cs_fp4_decode(codes, scale << 23)), reinterpret_cast<u32x4*>(row + seg * 8));
+}
+template <bool WHOLE>
+__device__ __forceinline__ void f4_store(float* row, int seg, int segs, int first, unsigned codes, unsigned scale) {
 #pragma unroll
-    for (int u = 0; u < 8; u += 4)
-        __builtin_nontemporal_store((f32x4){(float)v[u], (float)v[u + 1], (float)v[u + 2], (float)v[u + 3]}, reinterpret_cast<f32x4*>(p + u));
+    for (int half = 0; half < 2; ++half) {
+        const int q = half * segs + seg, from = first + (q >> 1);
+        const bf16x8 v = cs_fp4_decode(__shfl(codes, from, CS_WAVE) >> 16 * (q & 1), __shfl(scale, from, CS_WAVE) << 23);
+        const f32x4 o = (f32x4){(float)v[0], (float)v[1], (float)v[2], (float)v[3]};
+        f32x4* at = reinterpret_cast<f32x4*>(row + q * 4);
+        if constexpr (WHOLE) __builtin_nontemporal_store(o, at);
+        else *at = o;
+    }
 }
 
-template <typename TO>
+template <typename TO, bool WHOLE>
 __global__ __launch_bounds__(F4_THREADS) void k_paged_fp4_read(cs_fp4_dev F, f4_args A) {
     __shared__ f4_places from;
     const cs_pages_dev& D = F.d;
     const int tid = threadIdx.x, KVH = D.p.n_kv_heads;
     const int r0 = f4_turn<F4_READ_RUN>() * A.rpw, nr = min(A.rpw, D.R - r0);
+    const int first_lane = tid & (CS_WAVE - 1) & -(1 << A.lanes_log2);               // of the row's
     if (tid < CS_WAVE) {
         const int2 at = f4_place(D, A.first, r0, nr, tid);
         if (tid < nr) from.set(F, tid, at);
@@ -271,7 +287,7 @@ __global__ __launch_bounds__(F4_THREADS) void k_paged_fp4_read(cs_fp4_dev F, f4_
         const f4_mine M(A, KVH, tid, round);
         if (!M.on) continue;
         const f4_side& side = A.s[M.is_v];
-        TO* dst = (TO*)side.rows + (int64_t)(r0 + M.r) * side.row + (int64_t)M.g * side.head + M.seg * 8;
+        TO* dst = (TO*)side.rows + (int64_t)(r0 + M.r) * side.row + (int64_t)M.g * side.head;
         const int64_t dst_step = M.step * side.row;
         const uint8_t* codes_at = (M.is_v ? F.v + M.g * F.v_head : F.k + M.g * F.k_head) + M.seg * 4;
         const uint8_t* scales_at = M.is_v ? F.vs + M.g * F.vs_head + (M.seg >> 2) * F.vs_group : F.ks + M.g * F.ks_head + (M.seg >> 2) * F.ks_group;
@@ -290,7 +306,7 @@ __global__ __launch_bounds__(F4_THREADS) void k_paged_fp4_read(cs_fp4_dev F, f4_
             }
 #pragma unroll
             for (int u = 0; u < F4_READ_BATCH; ++u) {
-                if (mine[u]) f4_store(dst, cs_fp4_decode(codes[u], scale[u] << 23));
+                if (mine[u]) f4_store<WHOLE>(dst, M.seg, A.segs, first_lane, codes[u], scale[u]);
                 dst += dst_step;
             }
         }
@@ -355,7 +371,8 @@ extern "C" int cs_paged_fp4_read(const cs_pages_fp4* p, int32_t dst_dtype, void*
     A.rpw = f4_rows_of(A, p, R);
     const dim3 grid = cs_paged_grid(cs_ceil_div(R, A.rpw));
     hipStream_t s = (hipStream_t)stream;
-    if (dst_dtype == CS_BF16) k_paged_fp4_read<bf16_t><<<grid, F4_THREADS, 0, s>>>(F, A);
-    else k_paged_fp4_read<float><<<grid, F4_THREADS, 0, s>>>(F, A);
+    if (dst_dtype == CS_BF16) k_paged_fp4_read<bf16_t, true><<<grid, F4_THREADS, 0, s>>>(F, A);
+    else if (A.segs % 16 == 0) k_paged_fp4_read<float, true><<<grid, F4_THREADS, 0, s>>>(F, A);
+    else k_paged_fp4_read<float, false><<<grid, F4_THREADS, 0, s>>>(F, A);
     return cs_launch_ok("k_paged_fp4_read");
 }
