@@ -1228,9 +1228,9 @@ extern "C" int cs_paged_fp4_attention(const cs_pages_fp4* p, int32_t q_dtype, co
         FW(64, 1); FW(64, 2); FW(128, 1); FW(128, 2); FW(256, 1);
 #undef FW
         CS_TRY(rc);
-        // (a merge waits for its loads: four workgroups for one where the chip has room for them: 700 and 438 float32 rows behind
-        // 3001 and 1876 83 -> 76.5 us, with two 79, with eight 76; 16 x 33 rows of 28 heads behind 65535 502 -> 498)
-        CS_TRY(pm_launch(F.d, A, P, dim3(n.x, (unsigned)std::clamp<int64_t>(1024 / grid_w, 1, 4), n.z), s));
+        // (a merge waits for its loads: up to eight workgroups for one, where the chip has room for them: 700 and 438 float32 rows behind
+        // 3001 and 1876 83 -> 76 us, with two 79; 6 x 3269 rows of 4 heads 166 -> 163; 16 x 33 of 28 heads behind 65535 502 -> 497)
+        CS_TRY(pm_launch(F.d, A, P, dim3(n.x, (unsigned)std::clamp<int64_t>(4096 / grid_w, 1, 8), n.z), s));
     }
     if (grid_n) {
         const auto& N = c.narrow;
