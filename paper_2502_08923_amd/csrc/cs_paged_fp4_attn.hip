@@ -1141,11 +1141,18 @@ static f4_cut f4_make_cut(const cs_pages_fp4* p, bool f32, int H, bool has_row0,
         // Tiles of half the rows where whole ones, cut into ranges of 256 tokens of what a row sees on
         // average, leave the chip unfilled
         const bool unfilled = (all / (F4W_WAVES * 32) + 1) * KVH * std::max<int64_t>(1, (len - rows / 2) / 256) < 256;
-        W.nt = c.hdt == 256 || f32 || unfilled ? 1 : 2;
+        auto tiles = [&](int TR) { return has_row0 ? all / TR + std::min<int64_t>(B, all / (n_most + 1)) : B * cs_ceil_div(qr, TR); };
+        // Of 64 features and half the rows two workgroups run on a compute unit at once, and whole tiles that fill the chip come out
+        // more even: 2500 rows of 28 heads, 4 KV heads 74 -> 50 us, behind 4000 195 -> 173, 8 x 700 behind 1000 113 -> 102, behind
+        // 16000 1024 -> 883.  Up to twice as many as compute units are cut over a long context, into more partial results
+        // then (2500 rows of 28 heads behind 16000 484 -> 561), as are fewer (8 x 700 rows of 4 heads behind 4000 67 -> 80).
+        const int64_t items = tiles(F4W_WAVES * 32) * KVH;
+        const bool even = c.hdt == 64 && items >= (len <= 8192 ? 256 : 512);
+        W.nt = c.hdt == 256 || f32 || unfilled || even ? 1 : 2;
         W.TR = F4W_WAVES * 16 * W.nt;
         W.qr_lo = has_row0 ? n_most : 0;
         W.qr_hi = 0x7fffffff;
-        W.tiles = (int)(has_row0 ? all / W.TR + std::min<int64_t>(B, all / (n_most + 1)) : B * cs_ceil_div(qr, W.TR));
+        W.tiles = (int)tiles(W.TR);
     }
     if (N.tiles) {
         // What a block of 32 tokens takes a workgroup that runs alone (captured calls: 4.3, 5.2 and 6.6 ns a token of 64, 128
