@@ -63,6 +63,7 @@ struct f4_shares {
     int step;                 // distance of the numbers of pieces tried (W 0: workgroups per KV head)
     float bound, join;        // what a block of all tokens costs the chip, and a merge, in blocks of a workgroup
     int near;                 // neighbouring KV heads that run on one die
+    int most;                 // units of all tiles that ascending row offsets can lead to
     float* po;                // [2 W][KVH][TR][hd] partial outputs; 2w: of a tile that an earlier workgroup has begun, 2w + 1: of one that w begins
     float2* pml;              // [2 W][KVH][TR] their (maximum, sum)
     int4* who;                // [2 W] (first row, first query row, query rows, number | workgroups of the tile << 16) for the merge; 0: nothing
@@ -95,8 +96,11 @@ __device__ __forceinline__ int2 f4_extent(const cs_pages_dev& D, int G, int wind
     return make_int2((int)((qr + S.TR - 1) / S.TR), S.W ? max((span + 31) >> 5, 1) : 1);
 }
 
-// Positions count units: blocks of all tiles (shares) or pieces; a lane looks at one of 64 streams.  (The host makes
-// sure that they fit 31 bits.)
+// Positions count units: blocks of all tiles (shares) or pieces; a lane looks at one of 64 streams.  Units that ascending row
+// offsets lead to are at most `most`, which the host keeps below 2^29.  Others may claim rows many times over: sums of units
+// stay at 2^30 then, and streams whose sum passes `most` have no work, so that no position ever wraps.
+#define F4_MANY (1 << 30)
+__device__ __forceinline__ int f4_add(int a, int b) { return (int)min((unsigned)a + (unsigned)b, (unsigned)F4_MANY); }
 struct f4_walk {
     int p, end;               // position and end of the workgroup's share
     int share;                // units of a share (pieces: 1)
@@ -108,6 +112,7 @@ struct f4_walk {
     int units, upto;          // a lane's: units of a tile; of these streams up to and with its own
     bool have;
 };
+template <bool ANY>                       // whatever the row offsets are
 __device__ __forceinline__ void f4_look_at(const cs_pages_dev& D, int G, int window, const f4_shares& S, f4_walk& k, int lane) {
     k.e = k.rows = make_int2(0, 0), k.len = 0;
     if (k.b0 + lane < D.p.batch) {
@@ -116,7 +121,9 @@ __device__ __forceinline__ void f4_look_at(const cs_pages_dev& D, int G, int win
         k.e = f4_extent(D, G, window, S, k.rows.y, k.len);
     }
     k.units = (k.e.y + k.start + k.piece - 1) / k.piece;
-    k.upto = pa_wave_scan(k.e.x * k.units);
+    // (a product below 2^30 in float32 is below 2^30 + 2^7)
+    if constexpr (ANY) k.upto = pa_wave_reduce((float)k.e.x * (float)k.units < (float)F4_MANY ? k.e.x * k.units : F4_MANY, 0, f4_add);
+    else k.upto = pa_wave_scan(k.e.x * k.units);
     k.have = true;
 }
 __device__ __forceinline__ f4_walk f4_start(const cs_pages_dev& D, int G, int window, const f4_shares& S, int w, int lane) {
@@ -152,13 +159,14 @@ __device__ __forceinline__ f4_walk f4_start(const cs_pages_dev& D, int G, int wi
     int all = 0, tiles = 0;
     k.start = F4_SEGMENT;
     for (; k.b0 < B; k.b0 += 64) {
-        f4_look_at(D, G, window, S, k, lane);
-        all += __builtin_amdgcn_readlane(k.upto, 63);
+        f4_look_at<true>(D, G, window, S, k, lane);
+        all = f4_add(all, __builtin_amdgcn_readlane(k.upto, 63));
         if (B <= 64) {
             tiles = __builtin_amdgcn_readlane(pa_wave_scan(k.e.x), 63);
             break;
         }
     }
+    if (all > S.most) all = 0, tiles = S.W + 1;                 // (row offsets that make no sense: nothing to share out)
     k.share = max((all + S.W - 1) / S.W, S.least);
     if (B <= 64 && tiles <= S.W) {
         const int longest = __builtin_amdgcn_readlane(pa_wave_reduce(k.e.y, 0, [](int a, int b) { return max(a, b); }), 63);
@@ -204,7 +212,7 @@ __device__ __forceinline__ bool f4_next(const cs_pages_dev& D, int G, int window
         return k.before < f4_extent(D, G, window, S, o.rows, o.len).x;
     }
     for (;;) {
-        if (!k.have) f4_look_at(D, G, window, S, k, lane);
+        if (!k.have) f4_look_at<false>(D, G, window, S, k, lane);
         const int all = __builtin_amdgcn_readlane(k.upto, 63);
         if (k.p < k.before + all) break;
         k.before += all;
@@ -213,13 +221,12 @@ __device__ __forceinline__ bool f4_next(const cs_pages_dev& D, int G, int window
         if (k.b0 >= D.p.batch) return false;                    // (more workgroups than tiles)
     }
     const unsigned long long past = __ballot(k.before + k.upto > k.p);
-    if (!past) return false;                                    // (row offsets that make no sense: sums past 2^31)
+    if (!past) return false;
     const int l = __ffsll(past) - 1;
     const int tiles = __builtin_amdgcn_readlane(k.e.x, l), blocks = __builtin_amdgcn_readlane(k.e.y, l), units = __builtin_amdgcn_readlane(k.units, l);
     o.row0 = __builtin_amdgcn_readlane(k.rows.x, l), o.rows = __builtin_amdgcn_readlane(k.rows.y, l), o.len = __builtin_amdgcn_readlane(k.len, l);
     const unsigned at = k.p - (k.before + __builtin_amdgcn_readlane(k.upto, l) - tiles * units);
     const int tile = __builtin_amdgcn_readfirstlane(tiles == 1 ? 0 : at / (unsigned)units), off = at - tile * units;
-    if ((unsigned)tile >= (unsigned)tiles) return false;        // (as above)
     const int n = min(units - off, k.end - k.p);
     o.b = k.b0 + l;
     o.n0 = tile * S.TR;
@@ -1099,7 +1106,7 @@ struct f4_cut {
     int hdt;
     struct {
         int nt, TR, qr_lo, qr_hi, tiles;      // tiles: an upper bound; 0: no launch
-        int W, groups;                        // see f4_shares; workgroups per KV head
+        int W, most, groups;                  // see f4_shares; workgroups per KV head
         float bound, join;
     } narrow;
     pa_part wide;
@@ -1166,11 +1173,13 @@ static f4_cut f4_make_cut(const cs_pages_fp4* p, bool f32, int H, bool has_row0,
         auto price = [&](float longest, float all) { return std::cbrt(longest * longest * longest + all * all * all); };
         const float blocks = cs_ceil_div(len, 32), chip_all = blocks * tiles * N.bound, whole = price(blocks, chip_all);
         const float cut = price(std::max(blocks * tiles / share, (float)F4_LEAST), chip_all) + N.join;
-        // (positions fit 31 bits whatever the row offsets say: no stream has more tiles than all rows together)
-        const bool fits = (int64_t)B * (all / N.TR + 1) * (cap / 32 + 1) < (int64_t)1 << 31;
+        // (Tables of 2^24 tokens and 960 tiles; wider ones with more tiles leave each one whole.  A bound that let every stream have all
+        // rows left 15 single tokens beside 8192 rows uncut from 2^19 on, 32 heads over 2 KV heads: 2350 -> 2413 us.)
+        const int64_t most = (int64_t)tiles * (cap / 32 + 1 + F4_SEGMENT);
+        const bool fits = most < 1 << 29;
         // Streams of one length gain by that; others may where the longest alone takes ten times what a merge costs.  Twice as
         // many tiles as workgroups even out by themselves.
-        if (fits && tiles < 2 * share && (cut < whole || (tiles > 1 && blocks > 10 * N.join))) N.W = share;
+        if (fits && tiles < 2 * share && (cut < whole || (tiles > 1 && blocks > 10 * N.join))) N.W = share, N.most = (int)most;
         // (without shares: as f4_start counts them)
         N.groups = N.W ? N.W : !has_row0 || N.qr_hi <= N.TR ? (has_row0 ? B : tiles) : (int)(all / N.TR) + B;
     }
@@ -1243,7 +1252,7 @@ extern "C" int cs_paged_fp4_attention(const cs_pages_fp4* p, int32_t q_dtype, co
         const auto& N = c.narrow;
         const int64_t rows = (int64_t)2 * N.W * p->n_kv_heads * N.TR;
         float* po = (float*)workspace;
-        const f4_shares S = {N.TR, N.qr_lo, N.qr_hi, N.W, F4_LEAST, N.W ? (N.W + 63) / 64 : N.groups, N.bound, N.join, f4_near(p), po, (float2*)(po + rows * p->head_dim),
+        const f4_shares S = {N.TR, N.qr_lo, N.qr_hi, N.W, F4_LEAST, N.W ? (N.W + 63) / 64 : N.groups, N.bound, N.join, f4_near(p), N.most, po, (float2*)(po + rows * p->head_dim),
                              (int4*)((char*)workspace + cs_round_up(rows * (p->head_dim * 4 + 8), 16))};
         const dim3 n = cs_paged_grid(grid_n);
 #define FN(HD_, NT_) if (c.hdt == HD_ && N.nt == NT_) rc = f32 ? f4n_launch<HD_, NT_, 3>(F, A, S, n, s) : f4n_launch<HD_, NT_, 1>(F, A, S, n, s)

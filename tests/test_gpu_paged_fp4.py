@@ -864,3 +864,47 @@ def test_attention_of_the_most_workgroups(dtype):
         want += p[t][..., None] * v[:, t]
         mag += p[t][..., None] * v[:, t].abs()
     c.close(out, want, mag, d[..., None])
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_attention_of_few_rows_over_a_wide_table(dtype):
+    """Streams beside the block of a prompt are cut over their tokens whatever the width of the table: the same room, the same bits."""
+    B = 40
+    lens, rows = [(97 * b) % 700 for b in range(B)], [b % 5 for b in range(B)]
+    lens[1], lens[2], rows[0] = 9000, 5000, 600
+    c = Cache(lens, rows, 2, 128, 32, dtype, seed=4, pad=1)
+    call = dict(max_rows=600, max_len=9002)
+    q, got = c.check(8, **call)
+    wide = torch.full((B, 1 << 19), -1, dtype=torch.int32, device=DEV)
+    wide[:, :c.table.shape[1]] = c.table
+    pages = c.handle(table=wide)
+    need = [cs.cs_paged_fp4_attention_workspace(p, 8, c.R, row0=True, dtype=dtype, **call) for p in (c.pages, pages)]
+    assert need[0] == need[1] > 0
+    again = torch.full_like(got, 123.0)
+    cs.cs_paged_fp4_attention(pages, q, row0=c.row0, out=again, **call)
+    assert torch.equal(again, got)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("columns", [128, 2048])
+def test_row_offsets_that_claim_rows_many_times_over_stay_inside(columns, dtype):
+    """Every other stream claims all rows, over contexts so long that the blocks of all claims pass what 31 bits hold (2048 columns)."""
+    B, R, P, H = 900, 100, 1024, 16
+    k = torch.zeros((1, 1, P, 32), dtype=torch.uint8, device=DEV)
+    scale = torch.full((1, 1, 2, P), 127, dtype=torch.uint8, device=DEV)
+    pages = cs.PagesFP4(k, k, scale, scale, torch.full((B, columns), -1, dtype=torch.int32, device=DEV),
+                        torch.full((B,), columns * P, dtype=torch.int32, device=DEV))
+    q = randn((R, H, 64), gen(1), dtype)
+    for hint in (1, 0):
+        guard = Guarded()
+        need = cs.cs_paged_fp4_attention_workspace(pages, H, R, row0=True, max_rows=hint, dtype=dtype)
+        assert need > 0
+        ws, out = guard.like((need,), torch.uint8, 0xFF), guard.like(q.shape, dtype, 5.0)
+        row0 = torch.tensor([0, R] * (B // 2) + [0], dtype=torch.int32, device=DEV)
+        cs.cs_paged_fp4_attention(pages, q, row0=row0, max_rows=hint, out=out, workspace=ws)
+        guard.check()
+        # ascending ones: the rows see no page
+        row0 = torch.tensor([min(b, R) for b in range(B + 1)], dtype=torch.int32, device=DEV)
+        cs.cs_paged_fp4_attention(pages, q, row0=row0, max_rows=hint, out=out, workspace=ws)
+        assert bool((out == 0).all())
+        guard.check()

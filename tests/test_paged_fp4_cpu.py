@@ -134,6 +134,22 @@ def test_the_workspace_does_not_grow_with_the_table(lib, H, KVH, hd, t):
                     assert 0 <= need <= 1 << 29, (table, batch, R, has_row0, need)
 
 
+@pytest.mark.parametrize("t", [0, 1])
+@pytest.mark.parametrize("H,KVH,singles,block,longest", [(32, 2, 15, 8192, 8192), (32, 2, 23, 8192, 8192), (64, 8, 31, 4096, 4096), (32, 8, 15, 2048, 2048),
+                                                         (16, 1, 400, 0, 1), (32, 2, 100, 0, 2), (32, 8, 15, 8192, 0)])
+def test_a_wide_table_does_not_take_the_cut_of_tokens_away(lib, H, KVH, singles, block, longest, t):
+    """Streams that bring few rows are cut over their tokens whatever the width of the table and however long the blocks beside them: the
+    partial results that there is room for are those over a table just as wide as the contexts."""
+    hd, P, R = 128, 64, singles + block
+    d = dict(k_page=KVH * P * 64, k_head=P * 64, k_token=64, v_page=KVH * P * 64, v_head=P * 64, v_token=64, n_kv_heads=KVH, head_dim=hd, page_size=P,
+             ks_page=KVH * P * 4, ks_head=P * 4, ks_group=P, vs_page=KVH * P * 4, vs_head=P * 4, vs_group=P, batch=singles + (block > 0))
+    need = []
+    for table in (1 << 15, 1 << 18, 1 << 19, 1 << 20, 1 << 21, 1 << 24):
+        p = pages(table_pages=table // P, table_stride=table // P, **d)
+        need.append(lib.cs_paged_fp4_attention_workspace(C.byref(p), t, H, 1, R, longest, 20000))
+    assert need[0] > 0 and need == need[:1] * len(need), need
+
+
 def _handle(**kw):
     d = dict(k=torch.zeros((4, 1, 32, 32), dtype=torch.uint8), k_scale=torch.zeros((4, 1, 2, 32), dtype=torch.uint8),
              table=torch.zeros((1, 2), dtype=torch.int32), length=torch.zeros(1, dtype=torch.int32))
