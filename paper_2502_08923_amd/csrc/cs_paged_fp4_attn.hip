@@ -221,12 +221,13 @@ __device__ __forceinline__ bool f4_next(const cs_pages_dev& D, int G, int window
         if (k.b0 >= D.p.batch) return false;                    // (more workgroups than tiles)
     }
     const unsigned long long past = __ballot(k.before + k.upto > k.p);
-    if (!past) return false;
+    if (!past) return false;                                    // (offsets or lengths that change while the call runs)
     const int l = __ffsll(past) - 1;
     const int tiles = __builtin_amdgcn_readlane(k.e.x, l), blocks = __builtin_amdgcn_readlane(k.e.y, l), units = __builtin_amdgcn_readlane(k.units, l);
     o.row0 = __builtin_amdgcn_readlane(k.rows.x, l), o.rows = __builtin_amdgcn_readlane(k.rows.y, l), o.len = __builtin_amdgcn_readlane(k.len, l);
     const unsigned at = k.p - (k.before + __builtin_amdgcn_readlane(k.upto, l) - tiles * units);
     const int tile = __builtin_amdgcn_readfirstlane(tiles == 1 ? 0 : at / (unsigned)units), off = at - tile * units;
+    if ((unsigned)tile >= (unsigned)tiles) return false;        // (as above)
     const int n = min(units - off, k.end - k.p);
     o.b = k.b0 + l;
     o.n0 = tile * S.TR;
