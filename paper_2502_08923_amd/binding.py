@@ -933,7 +933,7 @@ def cs_paged_fp4_read(pages: PagesFP4, first: Optional[torch.Tensor] = None, R: 
     """The values of R tokens as rows (k, v) [R][KVH][hd]: row i of stream b is what the cache holds at position first[b] + i (int32
     [batch]; None: the lengths).  row0: int32 [batch + 1] offsets of the streams' rows, None: equal shares.  In new tensors of
     `dtype` (bfloat16 by default; both types hold the values exactly), or in out = (k_out, v_out), where R is their rows.  Rows
-    without a page are zeros, rows behind the last stream are left as they were."""
+    without a page are zeros; rows behind the last stream are left as they were in out, and zeros in new tensors."""
     ko, vo = out if out is not None else (None, None)
     _forward_only(ko, vo)
     dev = _device_of((pages.k, first, row0, ko, vo))
@@ -945,7 +945,8 @@ def cs_paged_fp4_read(pages: PagesFP4, first: Optional[torch.Tensor] = None, R: 
         if R is None:
             raise ValueError("R says how many rows are read, where there is no out")
         want = (R, c.n_kv_heads, c.head_dim)
-        ko, vo = (torch.zeros if row0 is not None else torch.empty)((2, *want), dtype=dtype or torch.bfloat16, device=pages.device).unbind()
+        nobodys = row0 is not None or c.batch == 0               # rows that no stream has are not written
+        ko, vo = (torch.zeros if nobodys else torch.empty)((2, *want), dtype=dtype or torch.bfloat16, device=pages.device).unbind()
     else:
         if ko is None or vo is None or ko.dtype != vo.dtype or (dtype is not None and ko.dtype != dtype):
             raise TypeError("out must be (k_out, v_out) of one type, dtype if that is given")

@@ -908,3 +908,23 @@ def test_row_offsets_that_claim_rows_many_times_over_stay_inside(columns, dtype)
         cs.cs_paged_fp4_attention(pages, q, row0=row0, max_rows=hint, out=out, workspace=ws)
         assert bool((out == 0).all())
         guard.check()
+
+
+def poisoned(shape, dtype):
+    """The allocator's next tensor of this size is likely to be one that held NaN."""
+    for _ in range(4):
+        torch.full(shape, math.nan, dtype=dtype, device=DEV)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_new_tensors_of_a_read_are_zeros_where_nobody_writes(dtype):
+    """Rows behind the last stream, and all rows where there is no stream."""
+    c = Cache([20, 3], [2, 1], 2, 64, 32, dtype, pad=5)
+    none = c.handle(table=c.table[:0], length=c.length[:0])
+    poisoned((2, 8, 2, 64), dtype)
+    k, v = cs.cs_paged_fp4_read(none, R=8, dtype=dtype)
+    assert bool((k == 0).all()) and bool((v == 0).all())
+    poisoned((2, 8, 2, 64), dtype)
+    k, v = cs.cs_paged_fp4_read(c.pages, R=8, row0=c.row0, dtype=dtype)
+    assert bool((k[3:] == 0).all()) and bool((v[3:] == 0).all())
+    assert torch.equal(k[:2].double(), c.k_tok[0][:, 20:].transpose(0, 1))
