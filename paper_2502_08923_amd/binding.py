@@ -974,9 +974,10 @@ def cs_paged_fp4_attention_workspace(pages: PagesFP4, n_heads: int, R: int, row0
 def cs_paged_fp4_attention(pages: PagesFP4, q: torch.Tensor, row0: Optional[torch.Tensor] = None, scale: Optional[float] = None,
                            window: int = 0, max_rows: int = 0, max_len: int = 0, out: Optional[torch.Tensor] = None,
                            workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
-    """q [R][H][hd], bfloat16 or float32, rotated.  Returns [R][H][hd] of that type (in `out` if given, which may be q; rows behind
-    the last stream are left as they were).  The other arguments are those of cs_paged_attention; a workspace of its own is as
-    large as cs_paged_fp4_attention_workspace says."""
+    """q [R][H][hd], bfloat16 or float32, rotated.  Returns [R][H][hd] of that type, in `out` if given, which may be q.  Rows behind the
+    last stream are left as they were in `out`; a new tensor has zeros there, which costs a fill where row0 is given.  The other
+    arguments are those of cs_paged_attention; a workspace of its own is as large as
+    cs_paged_fp4_attention_workspace says."""
     _forward_only(q, out)
     dev = _device_of((pages.k, q, row0, out, workspace))
     if _elsewhere(dev, stream):
@@ -989,7 +990,8 @@ def cs_paged_fp4_attention(pages: PagesFP4, q: torch.Tensor, row0: Optional[torc
     if hd != c.head_dim:
         raise ValueError(f"q must have the cache's head_dim, {c.head_dim}")
     if out is None:
-        out = q.new_empty(qs)
+        # (rows that no stream has are not written)
+        out = q.new_zeros(qs) if row0 is not None or c.batch == 0 else q.new_empty(qs)
     elif out.dtype != q.dtype:
         raise TypeError("out must have the type of q")
     lib, r0 = load_library(), pages._row0(row0)

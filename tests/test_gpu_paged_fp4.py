@@ -928,3 +928,19 @@ def test_new_tensors_of_a_read_are_zeros_where_nobody_writes(dtype):
     k, v = cs.cs_paged_fp4_read(c.pages, R=8, row0=c.row0, dtype=dtype)
     assert bool((k[3:] == 0).all()) and bool((v[3:] == 0).all())
     assert torch.equal(k[:2].double(), c.k_tok[0][:, 20:].transpose(0, 1))
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("rows", [[2, 1], [90, 40]])
+def test_a_new_output_of_the_attention_is_zeros_where_nobody_writes(rows, dtype):
+    """Rows behind the last stream, and all rows where there is no stream."""
+    c = Cache([20, 3], rows, 2, 64, 32, dtype, pad=5)
+    q, want = c.check(4)
+    live = sum(rows)
+    poisoned(q.shape, dtype)
+    got = cs.cs_paged_fp4_attention(c.pages, q, row0=c.row0)
+    assert torch.equal(got[:live], want[:live]) and bool((got[live:] == 0).all())
+    none = c.handle(table=c.table[:0], length=c.length[:0])
+    for row0 in (None, c.row0[:1]):
+        poisoned(q.shape, dtype)
+        assert bool((cs.cs_paged_fp4_attention(none, q, row0=row0) == 0).all())
