@@ -1,6 +1,6 @@
-"""Attention over a paged cache held in 4 bits, where its results are known to a few roundings: every token counts once.
-Bounds over sums of thousands of terms, as the other tests have them, leave room for a token that is lost or counted twice where
-the work is cut."""
+"""Attention over a paged cache held in 4 bits, where its results are known to a few roundings: every token counts once, and float32
+queries and probabilities keep all their bits.  Bounds over sums of thousands of terms, as the other tests have them, leave
+room for a token that is lost or counted twice where the work is cut, and for a query in fewer parts."""
 import math
 
 import pytest
@@ -160,3 +160,54 @@ def test_every_token_counts_once_behind_a_long_context():
     Marked([45000, 30], [1, 1], 1, 256, 64, BF).count(4, max_rows=1, max_len=45001)
     Marked([100001, 70000], [3, 1], 1, 128, 128, F32).count(4, max_rows=3, max_len=100004)
     Marked([65535], [33], 1, 128, 128, F32).count(7, max_rows=33, max_len=65568)
+
+
+class Pair(Cache):
+    """Two tokens of one block share all probability, p = exp(y) and 1 before they are divided by their sum, y the query's first
+    feature: their keys are 1 and 0 there, and 0 in the feature where the other tokens have -6 * 2^10 and the query 1 (their
+    probability is 0 in float32).  Each carries a 1 in a feature of its own."""
+
+    def __init__(self, lens, rows, KVH, hd, P, **kw):
+        super().__init__(lens, rows, KVH, hd, P, F32, **kw)
+        table = self.table.tolist()
+        for b, (L, r) in enumerate(zip(lens, rows)):
+            first = L // 2 & ~31                           # (the pair is in the context: all new rows see it)
+            assert L >= 32
+            for j in range(-(-(L + r) // P)):
+                page = table[b][j]
+                self.ks[page], self.vs[page] = 127, 127
+                self.ks[page, :, 1] = 137
+                self.k[page, :, :, 16] = 15                # feature 32: -6
+                self.v[page] = 0
+            for t, own in ((first + 3, 0), (first + 20, hd // 2 - 1)):
+                page, slot = table[b][t // P], t % P
+                self.k[page, :, slot, 16] = 0
+                self.k[page, :, slot, 0] = 2 if own == 0 else 0
+                self.v[page, :, slot, own] = 2
+
+    def query(self, H, seed):
+        """y in -4 .. 4 with all 24 bits of a float32"""
+        q = torch.zeros((self.R, H, self.hd), dtype=F32, device=DEV)
+        q[..., 0] = torch.rand((self.R, H), generator=gen(seed), device=DEV) * 8 - 4
+        q[..., 32] = 1
+        return q
+
+
+@pytest.mark.parametrize("H,KVH,hd,order", [(8, 2, 128, "head"), (8, 2, 128, "token"), (7, 1, 64, "head"), (4, 2, 256, "head"), (3, 3, 96, "both")])
+@pytest.mark.parametrize("lens,rows", [([40, 700, 33], [4, 4, 4]), ([3000, 64], [6, 11]), ([9000], [16]), ([700, 100], [90, 300]), ([4000], [160])])
+def test_float32_queries_and_probabilities_keep_all_their_bits(lens, rows, H, KVH, hd, order):
+    """The scores are y and 0 exactly (y's parts add up without a rounding), with scale 1.  In powers of two they are off by u |x|
+    (log2 e) and u |x| more (the differences to the maximum), |x| < 5.8, and the two exp2 by 2 u each: the ratio of the two probabilities by less
+    than 0.7 (2 * 5.8 + 1) u + 4 u < 13 u.  Sums of 3 parts of 2 tokens: 6 roundings each for both sums, 2 u each where a
+    matrix unit cuts off, 24 u; division and product 3 u: 40 u.  (A query without its third part changes the ratio by up to 256 u,
+    a probability without it by up to 128 u.)"""
+    c = Pair(lens, rows, KVH, hd, 32, order=order, seed=hd)
+    for seed, call in ((1, {}), (2, dict(max_rows=max(rows), max_len=max(a + b for a, b in zip(lens, rows)))), (3, dict(max_rows=max(rows), max_len=16))):
+        q = c.query(H, seed)
+        got = cs.cs_paged_fp4_attention(c.pages, q, row0=c.row0, scale=1.0, **call).double()
+        y = q[..., 0].double()
+        for feature, want in ((0, torch.sigmoid(y)), (hd - 2, torch.sigmoid(-y))):
+            err = (got[..., feature] - want).abs() / want
+            assert bool((err <= 40 * U).all()), float(err.max() / U)
+        got[..., 0] = got[..., hd - 2] = 0
+        assert bool((got == 0).all())
