@@ -559,7 +559,8 @@ int cs_paged_fp4_read(const cs_pages_fp4* p, int32_t dst_dtype, void* k, int64_t
 /* cs_paged_attention over such a cache: same rows, mask, scale, hints, workspace rules and results, k and v being
  * the values of the codes.  q_dtype CS_F32 or CS_BF16 is the type of q and out.  With CS_BF16 queries the
  * probabilities are rounded to bfloat16 for the product with V; float32 queries and probabilities go into the
- * products as three bfloat16 parts, which is all of them. */
+ * products as three bfloat16 parts, which is all of them (of a query between 2^-100 and 2^127 in size; of
+ * smaller ones what lies below 2^-126 may be lost, larger ones may round to an infinity). */
 int64_t cs_paged_fp4_attention_workspace(const cs_pages_fp4* p, int32_t q_dtype, int32_t n_heads, int32_t has_row0, int32_t R,
                                          int32_t max_rows, int64_t max_len);
 int cs_paged_fp4_attention(const cs_pages_fp4* p, int32_t q_dtype, const void* q, int64_t q_row, int64_t q_head, int32_t n_heads,

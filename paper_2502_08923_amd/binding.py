@@ -845,7 +845,7 @@ def cs_paged_attention(pages: Pages, q: torch.Tensor, row0: Optional[torch.Tenso
                        window: int = 0, max_rows: int = 0, max_len: int = 0, out: Optional[torch.Tensor] = None,
                        workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """q [R][H][hd] of the cache's type, rotated.  Returns [R][H][hd] (in `out` if given, which may be q; rows behind the last
-    stream are left as they were).  scale: 1/sqrt(head_dim) by default.  max_rows, max_len: hints, see copyspec.h.
+    stream are left as they were, in a new tensor not set).  scale: 1/sqrt(head_dim) by default.  max_rows, max_len: hints, see copyspec.h.
     workspace: a contiguous tensor of at least the size that cs_paged_attention_workspace gives; by default one is allocated
     for the call."""
     _forward_only(q)

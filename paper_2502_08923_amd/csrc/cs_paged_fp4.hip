@@ -67,9 +67,10 @@ int cs_fp4_view(const char* who, const cs_pages_fp4* p, const int32_t* d_row0, i
 // ---- rows and their places --------------------------------------------------------------
 #define F4_THREADS 256
 #define F4_ROWS 64            // most rows of a workgroup: a lane each for their places
-// Rows of a thread in flight, and in all.  (Append of 160 thousand rows of one head of 64: 12.9 us with two in flight, 16.1 with
-// four, 17.4 with eight, 11 thousand of 8 heads of 128 14.3, 14.5 and 16.9; read of 145 thousand rows of 8 heads 226, 204 and
-// 197, of 11 thousand 13.8, 13.9 and 14.9.  16 rows of a thread instead of eight: no change or 2 % slower, four: up to 30 %.)
+// Rows of a thread in flight, and in all.  (Captured calls.  Append with two, four and eight in flight: 160 thousand rows of one head of
+// 64 12.7, 14.9 and 16.3 us, 11 thousand of 8 heads of 128 13.1, 13.8 and 18.1; read with two, four and eight: 145 thousand rows of 8
+// heads 108.5, 107.9 and 108.5, 11 thousand 12.5, 12.4 and 12.6.  Four, eight and 16 rows of a thread, for both: the same append 14.6,
+// 13.4 and 13.8, the same reads 103, 108 and 112, and 11.2, 12.4 and 12.6.)
 #define F4_APPEND_BATCH 2
 #define F4_READ_BATCH 4
 #define F4_PASSES 8

@@ -273,12 +273,16 @@ __device__ __forceinline__ int2 f4_whose(unsigned wg, int KVH, int W_all, int ne
 // turns pairs of tokens with byte permutes into the A fragments: fragment u has feature c * HD / 16 + u in row
 // c.  A page holds whole blocks, so every load has one page, a uniform base, and nothing to check.
 //
-// Single tokens are bound by memory: 64 streams of 8191 tokens, 8 heads of 128, 107 us = 5.3 TB/s of codes and scales; 64 of 2 to 8
-// thousand over token-major pages of 32, where a head's codes are half lines, 92 us = 3.9 TB/s with 1.04 times the bytes read (two
-// heads in one workgroup: 149 us for 138 on one die; in one wave 98 for 97; four or all eight on one die: no change).  48 rows are bound by instructions: 8 x 11 rows behind 18431 48.5 us, the
-// vector unit 60 % and the matrix unit 30 % busy; a block is 64 conversions, 32 permutes, 24 exponentials and 51 products a wave.
-// Two workgroups a compute unit: registers for three spill, with one 48 rows take 65 us for 57, with their queries in registers 100.
-// 64 tokens a softmax step instead of 32: no gain.
+// Single tokens are bound by memory: 64 streams of 8191 tokens, 8 heads of 128, 108 us = 5.3 TB/s of codes and scales; 64 of 2 to 8
+// thousand over token-major pages of 32, where a head's codes are half lines, 94 us = 3.8 TB/s with 1.03 times the bytes read (tried at
+// earlier states: two heads in one workgroup 149 us against 138 on one die; in one wave 98 against 97; four or all eight on one die no
+// change).  48 rows: 8 x 11 rows behind 18431 51 to 54 us a captured call, 48 for the kernel and 6 for the join under the profiler.  Neither
+// unit is full (vector 60 %, matrix 30 % busy); a block is 64 conversions, 32 permutes, 24 exponentials and 51 products a wave, two waves
+// a SIMD, and about 14 us do not grow with the context: launches, the look-up of the cut, the exchange, the join.
+// Two workgroups a compute unit: with registers for three 48 rows take 93 us for 51, for one 75 (single tokens over token-major
+// pages 127 and 86 for 94, of 256 features 124 and 50 for 45, of 64 features 45 and 47 for 47).  Of 256 features and one part 9 registers
+// spill, of 48 float32 rows and 128 features 7.  (Queries in registers and 64 tokens a softmax step, tried at an earlier state: 100 us for
+// 57, no gain.)
 #define F4N_WAVES 4
 template <int HD>
 struct f4_keys { u32x4 k[2][HD == 256 ? 2 : 1]; u32x2 s[HD == 256 ? 2 : 1]; };
@@ -292,8 +296,8 @@ __global__ __launch_bounds__(64 * F4N_WAVES, 2) void k_paged_fp4_narrow(f4_call 
     constexpr int KB = HD == 256 ? 2 : 1;                       // 32-feature pieces of a lane's key row (HD 64: half of one)
     constexpr int VW = HD == 256 ? 2 : 1;                       // dwords of a lane's value row (HD 64: half of one)
     constexpr bool QREG = NT == 1 && NP == 1;                   // the query fragments stay in registers, else they are read from LDS
-    // blocks in flight (with one more: 48 rows 57 us for 53, 16 rows of 256 features spill; with one less: 16 rows of 256
-    // features 43 -> 85 us, others no change)
+    // blocks in flight (captured calls.  One more: 48 rows 59 us for 51, single tokens of 256 features 67 for 45, which spill more,
+    // of 128 features 96 for 94.  One less: of 256 features 42.5 for 45, 16 rows 47 for 51 and in float32 50 for 53; others within 2 %)
     constexpr int AHEAD = NT > 1 ? 1 : HD == 256 || NP > 1 ? 2 : 3;
     constexpr int ROWS = 16 * NT, QROW = HD * 2 + 16, QPLANE = ROWS * QROW;
     constexpr int SLOT = NT * (2 * VF / 4 * 1024 + 512);        // half of a wave's O, with its maximum and sum
@@ -1100,7 +1104,9 @@ static int check_shape(const char* who, const cs_pages_fp4* p, int32_t q_dtype, 
     return CS_OK;
 }
 
-#define F4_SLOTS 512              // workgroups of the kernel of few rows that run at once
+// Workgroups of the kernel of few rows that run at once: two a compute unit.  (Of 64 features and up to 32 rows three fit; they are
+// priced as two.)
+#define F4_SLOTS 512
 #define F4_LEAST 8                // blocks below which a part of a tile costs more than it saves
 // How a call is cut: the same for the workspace and the launches.
 struct f4_cut {
@@ -1147,7 +1153,8 @@ static f4_cut f4_make_cut(const cs_pages_fp4* p, bool f32, int H, bool has_row0,
     }
     if (qr > n_most) {
         // Tiles of half the rows where whole ones, cut into ranges of 256 tokens of what a row sees on
-        // average, leave the chip unfilled
+        // average, leave the chip unfilled.  (The price of a cut seldom goes as fine: 1581 rows of 16 heads on an empty cache are 112
+        // whole tiles, their ranges and a merge, 49 us for 8 us of multiplies.)
         const bool unfilled = (all / (F4W_WAVES * 32) + 1) * KVH * std::max<int64_t>(1, (len - rows / 2) / 256) < 256;
         auto tiles = [&](int TR) { return has_row0 ? all / TR + std::min<int64_t>(B, all / (n_most + 1)) : B * cs_ceil_div(qr, TR); };
         // Of 64 features and half the rows two workgroups run on a compute unit at once, and whole tiles that fill the chip come out
@@ -1187,7 +1194,8 @@ static f4_cut f4_make_cut(const cs_pages_fp4* p, bool f32, int H, bool has_row0,
     c.at_w = N.W ? cs_round_up((int64_t)2 * N.W * KVH * N.TR * (p->head_dim * 4 + 8), 16) + (int64_t)2 * N.W * 16 : 0;
     // A workgroup's ends and the merge in tokens of the kernel for many rows (with 128 and 192 for bfloat16 queries too: 4 x
     // 300 rows of 32 heads behind 1000 tokens 52 -> 70 us, behind 16000 344 -> 399, 33 rows of 16 heads of 64 behind 300
-    // 14 -> 15; with 256 and 400 for float32 ones 33 rows of 8 heads behind 300 24 -> 26, 100 rows 25 -> 29).
+    // 14 -> 15; with 256 and 400 for float32 ones 33 rows of 8 heads behind 300 24 -> 26, 100 rows 25 -> 29).  256 workgroups
+    // run at once, one a compute unit; the two of 64 features and half the rows count as one.
     c.bytes = c.at_w + (f32 ? pa_ranges(W, len, B, KVH, p->head_dim, 256, 128, 192) : pa_ranges(W, len, B, KVH, p->head_dim, 256, 256, 400));
     return c;
 }
